@@ -15,10 +15,12 @@ Modules
   bf16       round-to-nearest-even onto the bfloat16 grid (8 significant bits)
   ikbo       the three operators and the decomposed forms used as pins
   pipelines  the five benchmark pipelines composed from the operators
+  history    attention over a request's own history; the cache of pages, row by row
 
 Parity status: every function here is pinned by tests/test_oracle_pins.py
+(history: tests/test_oracle_history.py)
 against brute-force loops, closed forms or the paper's printed numbers; none
 is "parity unpinned".
 """
 
-from . import bf16, ikbo, pipelines  # noqa: F401
+from . import bf16, history, ikbo, pipelines  # noqa: F401

@@ -1,4 +1,5 @@
-"""ctypes loader for librocs.so and the declarations of its C ABI (include/rocs.h)."""
+"""ctypes loader for librocs.so and the declarations of its C ABI (include/rocs.h
+and include/rocs_history.h)."""
 
 import ctypes
 import os
@@ -59,6 +60,28 @@ SIGNATURES = {
     "rocs_validate_offsets": (_i32, [_vp, _i64, _i64, _vp]),
 }
 
+# name -> (restype, argtypes), mirroring include/rocs_history.h
+HISTORY_SIGNATURES = {
+    "rocs_history_workspace_size": (_size, [_i64, _i64, _i32, _i32, _i32, _i64, _i32]),
+    "rocs_history_attention": (_i32, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64,
+                                      _i64, _i64, _i32, _i32, _i32, _f32, _f32, _i32, _i64, _i32,
+                                      _vp, _vp, _size, _vp]),
+    "rocs_paged_attention": (_i32, [_vp, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp,
+                                    _vp, _vp, _i64, _i64, _i64, _i32, _i32, _i32, _i32, _f32, _f32,
+                                    _i32, _i64, _i32, _vp, _vp, _size, _vp]),
+    "rocs_cache_workspace_size": (_size, [_i64, _i64]),
+    "rocs_cache_reserve": (_i32, [_vp, _vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp,
+                                  _vp, _vp, _size, _vp]),
+    "rocs_cache_write": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _vp]),
+    "rocs_cache_fork": (_i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i64,
+                               _i64, _vp, _vp, _size, _vp]),
+    "rocs_cache_free": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp]),
+    "rocs_cache_compact": (_i32, [_vp, _i64, _i64, _vp, _i64, _i32, _vp, _i64, _i64, _vp, _vp,
+                                  _size, _vp]),
+    "rocs_cache_copy": (_i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp]),
+}
+CACHE_NO_PAGES, CACHE_TABLE_FULL, CACHE_BAD_SLOT = 1, 2, 3   # status[0] of the page operators
+
 ABI_VERSION = 5
 NOALLOC_SCRATCH_BYTES = 16 << 20   # ROCS_NOALLOC_SCRATCH_BYTES
 
@@ -84,7 +107,7 @@ def load(path=LIB_PATH):
             f"{path} is missing: build it with `python -c 'import __graft_entry__ as g; "
             "g.build()'` (hipcc, gfx950). There is no fallback implementation.")
     lib = ctypes.CDLL(path)
-    for name, (res, args) in SIGNATURES.items():
+    for name, (res, args) in {**SIGNATURES, **HISTORY_SIGNATURES}.items():
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args

@@ -11,10 +11,13 @@
 
 #include "../../include/rocs.h"
 #include "kernels.h"
+#include "status.h"
 
 namespace {
-
 thread_local std::string g_error;
+}  // namespace
+
+namespace rocs {
 
 int32_t fail(rocs_status s, const char* fmt, ...) {
   char buf[512];
@@ -40,23 +43,9 @@ int32_t launch_failed(const char* name, hipError_t e) {
   return fail(ROCS_ERR_HIP, "%s: %s", name, hipGetErrorString(e));
 }
 
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+}  // namespace rocs
 
-// Byte ranges [a, a + an) and [b, b + bn) intersect.
-bool overlap(const void* a, size_t an, const void* b, size_t bn) {
-  if (a == nullptr || b == nullptr || an == 0 || bn == 0) return false;
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + bn && y < x + an;
-}
-
-size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
-
-bool valid_dtype(int32_t d) { return d == ROCS_DTYPE_F32 || d == ROCS_DTYPE_BF16; }
-size_t esize(int32_t d) { return d == ROCS_DTYPE_BF16 ? 2 : 4; }
-
-constexpr int64_t kMaxI32 = 2147483647;
-
-}  // namespace
+using namespace rocs;
 
 extern "C" {
 

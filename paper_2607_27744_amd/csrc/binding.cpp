@@ -15,7 +15,7 @@
 #include <ATen/Functions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include "../../include/rocs.h"
+#include "../../include/rocs_history.h"
 
 namespace {
 
@@ -507,12 +507,276 @@ PyObject* attention(PyObject* const* a) {
   return res ? pair(result(a[11], out), result(a[12], sum)) : result(a[11], out);
 }
 
+// --- attention over histories, the cache's pages -----------------------------
+
+// Row stride of [.., rows, heads, d] with dense rows (0: a single row).
+int64_t row_stride(const Ten& t) {
+  const int64_t n = t->dim(), h = t->size(n - 2), d = t->size(n - 1);
+  need((d == 1 || t->stride(n - 1) == 1) && (h == 1 || t->stride(n - 2) == d));
+  if (t->size(n - 3) <= 1) return 0;
+  need(t->stride(n - 3) >= h * d);
+  return t->stride(n - 3);
+}
+
+void int_vector(const Ten& t, int64_t n) {
+  need(!t || (t->scalar_type() == c10::kInt && t->dim() == 1 && t->is_contiguous() &&
+              t->numel() == n));
+}
+
+int32_t truth(PyObject* o) {
+  need(o == Py_True || o == Py_False);
+  return o == Py_True;
+}
+
+// None (0) or a count of at least 0.
+int64_t count_of(PyObject* o) {
+  const int64_t v = o == Py_None ? 0 : integer(o);
+  need(v >= 0);
+  return v;
+}
+
+// The caller's workspace, or a new one of `bytes`.
+Ten scratch(Call& c, PyObject* o, size_t bytes) {
+  Ten ws = c.get(o);
+  if (!ws && bytes > 0) return c.or_new(Py_None, {(int64_t)bytes}, c10::kByte);
+  need(!ws || ws->is_contiguous());
+  return ws;
+}
+
+// The kernels run on the current device; ops.py takes calls on another.
+void on_current_device(const Call& c) {
+  PyObject* v = PyObject_CallNoArgs(g_get_device);
+  if (v == nullptr) throw PyError();
+  const long dev = PyLong_AsLong(v);
+  Py_DECREF(v);
+  need(dev == c.dev.index());
+}
+
+struct Rules {
+  int64_t n, r, most;
+  int32_t h, hk, d, code, causal;
+  float cap, scale;
+};
+
+// What both attentions check alike; k: packed rows or pages.
+Rules rules(const Ten& q, const Ten& k, const Ten& v, const Ten& off, const Ten& prefix,
+            const Ten& slopes, PyObject* cap, PyObject* causal, PyObject* most, PyObject* scale) {
+  Rules x;
+  need(q->dim() == 3 && k->sizes() == v->sizes());
+  const int64_t h = q->size(1), d = q->size(2), hk = k->size(k->dim() - 2);
+  need(k->size(k->dim() - 1) == d && hk >= 1 && h <= INT32_MAX && d <= INT32_MAX && h % hk == 0);
+  x.code = dtype_code(q);
+  need(k->scalar_type() == q->scalar_type() && v->scalar_type() == q->scalar_type());
+  x.n = q->size(0);
+  x.h = (int32_t)h;
+  x.hk = (int32_t)hk;
+  x.d = (int32_t)d;
+  x.r = off->numel() - 1;
+  need(x.r >= 0);
+  offsets(off, x.r);
+  int_vector(prefix, x.r);
+  need(!slopes || (slopes->scalar_type() == c10::kFloat && slopes->dim() == 1 &&
+                   slopes->size(0) == h && slopes->is_contiguous()));
+  x.cap = scale_of(cap);
+  need(x.cap >= 0.f && x.cap < 3.4e38f);
+  x.causal = truth(causal);
+  x.most = count_of(most);
+  x.scale = scale_of(scale);
+  return x;
+}
+
+// q, k, v, q_offsets, kv_offsets, causal, prefix_lens, q_docs, kv_docs, slopes,
+// cap, max_kv_len, scale, out, workspace, stream
+PyObject* history(PyObject* const* a) {
+  Call c(a[15]);
+  const Ten q = c.must(a[0]), k = c.must(a[1]), v = c.must(a[2]), qo = c.must(a[3]),
+            ko = c.must(a[4]), prefix = c.get(a[6]), qd = c.get(a[7]), kd = c.get(a[8]),
+            slopes = c.get(a[9]);
+  on_current_device(c);
+  need(k->dim() == 3);
+  const Rules x = rules(q, k, v, qo, prefix, slopes, a[10], a[5], a[11], a[12]);
+  const int64_t rows = k->size(0);
+  offsets(ko, x.r);
+  need((bool)qd == (bool)kd);
+  int_vector(qd, x.n);
+  int_vector(kd, rows);
+  const int64_t qs = row_stride(q), ks = row_stride(k);
+  need(row_stride(v) == ks);
+  const Ten out = c.or_new(a[13], q->sizes(), q->scalar_type());
+  const Ten ws = scratch(c, a[14], rocs_history_workspace_size(x.r, x.n, x.h, x.hk, x.d,
+                                                               x.most > 0 ? x.most : rows, x.code));
+  void* s = stream_of(c.stream);
+  run("rocs_history_attention", rocs_history_attention, q.ptr(), qs, k.ptr(), v.ptr(), ks,
+      qo.i32(), ko.i32(), prefix.i32(), qd.i32(), kd.i32(), slopes.f32(), x.r, x.n, rows, x.h,
+      x.hk, x.d, x.scale, x.cap, x.causal, x.most, x.code, data(out), data(ws), nbytes(ws), s);
+  return result(a[13], out);
+}
+
+// q, k_pages, v_pages, page_table, kv_lens, q_offsets, slots, causal,
+// prefix_lens, slopes, cap, max_kv_len, scale, out, workspace, stream
+PyObject* paged(PyObject* const* a) {
+  Call c(a[15]);
+  const Ten q = c.must(a[0]), k = c.must(a[1]), v = c.must(a[2]), table = c.must(a[3]),
+            lens = c.must(a[4]), qo = c.must(a[5]), slots = c.get(a[6]), prefix = c.get(a[8]),
+            slopes = c.get(a[9]);
+  on_current_device(c);
+  need(k->dim() == 4);
+  const Rules x = rules(q, k, v, qo, prefix, slopes, a[10], a[7], a[11], a[12]);
+  const int64_t pages = k->size(0), page = k->size(1);
+  need(pages >= 1 && page >= 1 && page <= INT32_MAX);
+  need(table->scalar_type() == c10::kInt && table->dim() == 2 && table->is_contiguous() &&
+       table->size(1) >= 1);
+  const int64_t n_slots = table->size(0), width = table->size(1);
+  need(width <= INT32_MAX / page);
+  int_vector(lens, n_slots);
+  int_vector(slots, x.r);
+  need(slots || x.r <= n_slots);
+  const int64_t qs = row_stride(q), ks = row_stride(k);
+  need(row_stride(v) == ks);
+  int64_t ps = 0;
+  if (pages > 1) {
+    ps = k->stride(0);
+    need(v->stride(0) == ps && ps >= (page - 1) * ks + (int64_t)x.hk * x.d);
+  }
+  const int64_t all = width * page, bound = x.most > 0 && x.most < all ? x.most : all;
+  const Ten out = c.or_new(a[13], q->sizes(), q->scalar_type());
+  const Ten ws = scratch(c, a[14],
+                         rocs_history_workspace_size(x.r, x.n, x.h, x.hk, x.d, bound, x.code));
+  void* s = stream_of(c.stream);
+  run("rocs_paged_attention", rocs_paged_attention, q.ptr(), qs, k.ptr(), v.ptr(), ps, ks,
+      table.i32(), width, lens.i32(), slots.i32(), n_slots, qo.i32(), prefix.i32(), slopes.f32(),
+      x.r, x.n, pages, (int32_t)page, x.h, x.hk, x.d, x.scale, x.cap, x.causal, x.most, x.code,
+      data(out), data(ws), nbytes(ws), s);
+  return result(a[13], out);
+}
+
+// A cache's bookkeeping, changed in place.
+struct State {
+  int32_t *table, *lens, *refs;
+  int64_t slots, width, pages;
+};
+State state_of(Call& c, PyObject* table, PyObject* lens, PyObject* refs) {
+  const Ten t = c.must(table), l = c.must(lens), r = c.must(refs);
+  on_current_device(c);
+  need(t->scalar_type() == c10::kInt && t->dim() == 2 && t->is_contiguous() && t->size(0) >= 1 &&
+       t->size(1) >= 1);
+  int_vector(l, t->size(0));
+  int_vector(r, r->numel());
+  need(r->numel() >= 1);
+  return {static_cast<int32_t*>(t.ptr()), static_cast<int32_t*>(l.ptr()),
+          static_cast<int32_t*>(r.ptr()), t->size(0), t->size(1), r->numel()};
+}
+
+// layers, page size and row bytes of a pool [layers, pages, page_size, ...].
+struct Layers {
+  int64_t layers, page, row_bytes;
+};
+Layers layers_of(const Ten& pool, int64_t pages) {
+  need(pool->dim() >= 4 && pool->is_contiguous() && pool->size(1) == pages && pool->numel() > 0 &&
+       pool->size(2) <= INT32_MAX);
+  const int64_t l = pool->size(0), p = pool->size(2);
+  return {l, p, pool->numel() / (l * pages * p) * (int64_t)pool->element_size()};
+}
+
+// slots, row_offsets, num_rows, page_table, lens, refs, page_size, rows,
+// status, workspace, stream
+PyObject* cache_reserve(PyObject* const* a) {
+  Call c(a[10]);
+  const Ten slots = c.must(a[0]), off = c.must(a[1]);
+  const int64_t n = slots->numel(), m = integer(a[2]), page = integer(a[6]);
+  int_vector(slots, n);
+  offsets(off, n);
+  need(m >= 0 && (n > 0 || m == 0) && page >= 1 && page <= INT32_MAX);
+  const State st = state_of(c, a[3], a[4], a[5]);
+  const Ten rows = c.or_new(a[7], {m}, c10::kInt), status = c.or_new(a[8], {2}, c10::kInt);
+  const Ten ws = scratch(c, a[9], rocs_cache_workspace_size(n, st.pages));
+  void* s = stream_of(c.stream);
+  run("rocs_cache_reserve", rocs_cache_reserve, slots.i32(), off.i32(), n, m, st.table, st.width,
+      st.lens, st.slots, st.refs, st.pages, (int32_t)page, static_cast<int32_t*>(data(rows)),
+      static_cast<int32_t*>(data(status)), data(ws), nbytes(ws), s);
+  return pair(result(a[7], rows), result(a[8], status));
+}
+
+// x, rows, pool, stream
+PyObject* cache_write(PyObject* const* a) {
+  Call c(a[3]);
+  const Ten x = c.must(a[0]), rows = c.must(a[1]), pool = c.must(a[2]);
+  on_current_device(c);
+  need(pool->dim() >= 3 && pool->is_contiguous() && pool->numel() > 0 &&
+       x->scalar_type() == pool->scalar_type() && x->dim() >= 2);
+  const int64_t pool_rows = pool->size(0) * pool->size(1), width = pool->numel() / pool_rows;
+  const int64_t m = x->size(0), size = x->element_size();
+  need(x->numel() == m * width && m > 0);
+  int_vector(rows, m);
+  int64_t dense = 1;                       // every dimension after the first is dense
+  for (int64_t i = x->dim() - 1; i > 0; --i) {
+    need(x->size(i) == 1 || x->stride(i) == dense);
+    dense *= x->size(i);
+  }
+  need(m == 1 || x->stride(0) >= width);
+  void* s = stream_of(c.stream);
+  run("rocs_cache_write", rocs_cache_write, x.ptr(), (m > 1 ? x->stride(0) : width) * size,
+      rows.i32(), m, pool.ptr(), pool_rows, width * size, s);
+  Py_INCREF(a[2]);
+  return a[2];
+}
+
+// parents, children, page_table, lens, refs, pool, status, workspace, stream
+PyObject* cache_fork(PyObject* const* a) {
+  Call c(a[8]);
+  const Ten par = c.must(a[0]), kid = c.must(a[1]);
+  const int64_t n = par->numel();
+  int_vector(par, n);
+  int_vector(kid, n);
+  const State st = state_of(c, a[2], a[3], a[4]);
+  const Ten pool = c.must(a[5]);
+  const Layers l = layers_of(pool, st.pages);
+  const Ten status = c.or_new(a[6], {2}, c10::kInt);
+  const Ten ws = scratch(c, a[7], rocs_cache_workspace_size(n, st.pages));
+  void* s = stream_of(c.stream);
+  run("rocs_cache_fork", rocs_cache_fork, par.i32(), kid.i32(), n, st.table, st.width, st.lens,
+      st.slots, st.refs, st.pages, (int32_t)l.page, pool.ptr(), l.layers, l.row_bytes,
+      static_cast<int32_t*>(data(status)), data(ws), nbytes(ws), s);
+  return result(a[6], status);
+}
+
+// slots, page_table, lens, refs, page_size, stream
+PyObject* cache_free(PyObject* const* a) {
+  Call c(a[5]);
+  const Ten slots = c.must(a[0]);
+  const int64_t n = slots->numel(), page = integer(a[4]);
+  int_vector(slots, n);
+  need(page >= 1 && page <= INT32_MAX);
+  const State st = state_of(c, a[1], a[2], a[3]);
+  void* s = stream_of(c.stream);
+  run("rocs_cache_free", rocs_cache_free, slots.i32(), n, st.table, st.width, st.lens, st.slots,
+      st.refs, st.pages, (int32_t)page, s);
+  Py_RETURN_TRUE;
+}
+
+// page_table, lens, refs, pool, status, workspace, stream
+PyObject* cache_compact(PyObject* const* a) {
+  Call c(a[6]);
+  const State st = state_of(c, a[0], a[1], a[2]);
+  const Ten pool = c.must(a[3]);
+  const Layers l = layers_of(pool, st.pages);
+  const Ten status = c.or_new(a[4], {2}, c10::kInt);
+  const Ten ws = scratch(c, a[5], rocs_cache_workspace_size(0, st.pages));
+  void* s = stream_of(c.stream);
+  run("rocs_cache_compact", rocs_cache_compact, st.table, st.width, st.slots, st.refs, st.pages,
+      (int32_t)l.page, pool.ptr(), l.layers, l.row_bytes, static_cast<int32_t*>(data(status)),
+      data(ws), nbytes(ws), s);
+  return result(a[4], status);
+}
+
 #define ROCS_ENTRY(name, n) \
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<n, name>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     ROCS_ENTRY(linear, 12),   ROCS_ENTRY(glm_linear, 14), ROCS_ENTRY(mlp2, 13),
     ROCS_ENTRY(fm_linear, 10), ROCS_ENTRY(lcb, 11),        ROCS_ENTRY(plan, 7),
-    ROCS_ENTRY(attention, 16), {nullptr, nullptr, 0, nullptr}};
+    ROCS_ENTRY(attention, 16), ROCS_ENTRY(history, 16),    ROCS_ENTRY(paged, 16),
+    ROCS_ENTRY(cache_reserve, 11), ROCS_ENTRY(cache_write, 4), ROCS_ENTRY(cache_fork, 9),
+    ROCS_ENTRY(cache_free, 6), ROCS_ENTRY(cache_compact, 7), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,272 @@
+// Attention of a request's own rows over its history, packed or paged: the rule
+// that cuts a call up, the general kernel and the join of a split history.
+#include "history_device.h"
+#include "launch.h"
+#include "status.h"
+
+namespace rocs {
+namespace {
+
+// ---------------------------------------------------------------------------
+// General kernel: any dtype, head_dim <= 256, strides and page sizes.
+//
+// A workgroup takes 16 rows (token, head) of one request and K/V head; its four
+// waves share the keys in blocks of 16 and merge their partial softmaxes
+// through LDS. Scores and outputs run on the fp32 matrix instructions
+// (16x16x4; bf16 converts exactly): S^T = K Q^T leaves lane (l16, g) keys
+// 4 g .. + 3 of row l16, the B operand of O^T = V^T P^T as it stands. A score
+// is summed in 4 accumulators a 64 dims, added pairwise: shorter chains.
+// Loads are clamped into the history, never skipped, so they are in flight
+// together; a key that a row does not see gets the weight 0.
+// What bounds it: the latency of a wave's loads, and the fp32 matrix rate (an
+// eighth of bf16's) at long histories.
+// ---------------------------------------------------------------------------
+constexpr int kGenTile = 16;
+
+template <typename T, bool VEC>
+__device__ __forceinline__ f32x4 row4(const T* row, int d, int D) {
+  if constexpr (VEC) {                     // D and d are multiples of four
+    const f32x4 v = load4_f32<T, true>(row + min(d, D - 4), 4);
+    return d < D ? v : f32x4{0.f, 0.f, 0.f, 0.f};
+  } else {
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = load_f32(row + min(d + i, D - 1));
+      v[i] = d + i < D ? x : 0.f;
+    }
+    return v;
+  }
+}
+
+// DP: head_dim rounded up to 32, 64, 128 or 256. VEC: rows of q, k and v are
+// aligned to four elements and head_dim is a multiple of four.
+template <typename T, int DP, bool VEC>
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void history_general(
+    const HistArgs a) {
+  constexpr int NB = DP / 16;              // 16-dim blocks
+  constexpr int CB = sizeof(T) == 2 || DP == 32 ? 1 : DP == 64 ? 4 : 8;
+  constexpr int LP = DP + 4;               // LDS row (floats), padded against bank conflicts
+  __shared__ __attribute__((aligned(16))) float po[4][kGenTile][LP];
+  __shared__ float pm[4][kGenTile], pl[4][kGenTile];
+  __shared__ int odd[kGenTile];            // rows to form again
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int hk = blockIdx.y, split = blockIdx.z;
+  const HistTile t = hist_tile(a, blockIdx.x, kGenTile);
+  if (t.rows <= 0) return;
+  const int D = a.D;
+  if (tid < kGenTile) odd[tid] = 0;
+  const int row = t.row0 + min(l16, t.rows - 1);         // clamped; extra rows never stored
+  const int token = row / a.G, h = hk * a.G + row % a.G;
+  const int pos = position_of(t, token), lim = limit_of(a, t, token);
+  const float slope = a.slopes != nullptr ? a.slopes[h] : 0.f;
+  const int doc = a.q_docs != nullptr ? a.q_docs[t.q0 + token] : 0;
+  const int lo = split * a.chunk;
+  const int most = limit_of(a, t, (t.row0 + t.rows - 1) / a.G);    // the tile's last row sees most
+  const int hi = split_end(a, split, most);
+  const T* q = static_cast<const T*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)h * D;
+  const T* k = static_cast<const T*>(a.k) + (int64_t)hk * D;
+  const T* v = static_cast<const T*>(a.v) + (int64_t)hk * D;
+  f32x4 qf[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) qf[b] = row4<T, VEC>(q, 16 * b + 4 * g, D);
+  float m = -INFINITY, lsum = 0.f;
+  f32x4 o[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int kb = lo + 16 * wave; kb < hi; kb += 64) {
+    const T* kr = k + key_row(a, t, min(kb + l16, hi - 1));
+    const T* vr[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vr[i] = v + key_row(a, t, min(kb + 4 * g + i, hi - 1));
+    f32x4 part[CB][4] = {};
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const f32x4 kf = row4<T, VEC>(kr, 16 * b + 4 * g, D);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        part[b % CB][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i], qf[b][i], part[b % CB][i],
+                                                               0, 0, 0);
+    }
+#pragma unroll
+    for (int c = 1; c < CB; c *= 2)
+#pragma unroll
+      for (int b = 0; b + c < CB; b += 2 * c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[b][i] += part[b + c][i];
+    f32x4 s4 = (part[0][0] + part[0][1]) + (part[0][2] + part[0][3]);
+    bool seen[4];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = kb + 4 * g + i;
+      seen[i] = j < lim && j < hi;
+      if (a.q_docs != nullptr) seen[i] = seen[i] && a.kv_docs[t.kv0 + min(j, hi - 1)] == doc;
+      float s = s4[i] * a.scale;
+      if (a.cap > 0.f) s = a.cap * tanhf(s / a.cap);
+      if (a.slopes != nullptr) s -= slope * fabsf((float)(pos - j));
+      s4[i] = seen[i] ? s : -INFINITY;
+      mx = fmaxf(mx, s4[i]);
+    }
+    const float mn = fmaxf(m, max_across_rows(mx));
+    const float ms = mn == -INFINITY ? 0.f : mn;         // no finite score yet: weights 0
+    const float alpha = expf(m - ms);
+    f32x4 p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = seen[i] ? expf(s4[i] - ms) : 0.f;
+    lsum = lsum * alpha + ((p[0] + p[1]) + (p[2] + p[3]));
+    m = mn;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int dim = 16 * b + l16;
+      o[b] *= alpha;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float vf = load_f32(vr[i] + min(dim, D - 1));
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(kb + 4 * g + i < hi && dim < D ? vf : 0.f,
+                                                    p[i], o[b], 0, 0, 0);
+      }
+    }
+  }
+  lsum = sum_across_rows(lsum);
+  if (g == 0) {
+    pm[wave][l16] = m;
+    pl[wave][l16] = lsum;
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+    *reinterpret_cast<f32x4*>(&po[wave][l16][16 * b + 4 * g]) = o[b];
+  __syncthreads();
+  // Merge the four partial softmaxes, four dims a step.
+  const int64_t part0 = (int64_t)split * a.N * a.H;
+  for (int idx = tid; idx < t.rows * (DP / 4); idx += 256) {
+    const int i = idx / (DP / 4), d0 = 4 * (idx % (DP / 4));
+    if (d0 >= D) continue;
+    const float mx = fmaxf(fmaxf(pm[0][i], pm[1][i]), fmaxf(pm[2][i], pm[3][i]));
+    const float ms = mx == -INFINITY ? 0.f : mx;
+    float l = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = expf(pm[w][i] - ms);
+      l += pl[w][i] * f;
+      y += *reinterpret_cast<const f32x4*>(&po[w][i][d0]) * f;
+    }
+    if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3]))) odd[i] = 1;
+    const int rw = t.row0 + i;
+    const int64_t at = (t.q0 + rw / a.G) * a.H + hk * a.G + rw % a.G;
+    if (a.splits > 1) {
+      if (d0 == 0) {
+        a.part_ml[2 * (part0 + at)] = mx * kLog2e;
+        a.part_ml[2 * (part0 + at) + 1] = l;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (d0 + e < D && l != 0.f) a.part_o[(part0 + at) * D + d0 + e] = y[e];
+    } else {
+      T* out = static_cast<T*>(a.out) + at * D;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (d0 + e < D) out[d0 + e] = from_f32<T>(l == 0.f ? 0.f : y[e] / l);
+    }
+  }
+  __syncthreads();
+  for (int i = wave; i < t.rows; i += 4)
+    if (__builtin_amdgcn_readfirstlane(odd[i]) != 0)
+      redo_row<T>(a, t, t.row0 + i, hk, lo, hi, split);
+}
+
+// ---------------------------------------------------------------------------
+// Join of a split history: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.
+// A thread per four dims of a (token, head); a part without a seen key has
+// l = 0 and its O is not read. Bound by the read of the parts.
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void history_join(const float* __restrict__ ml,
+                                                    const float* __restrict__ po,
+                                                    T* __restrict__ out, int64_t rows, int D,
+                                                    int splits) {
+  const int quads = (D + 3) / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = i / quads;
+  const int d0 = 4 * (int)(i - row * quads);
+  if (row >= rows) return;
+  float m = -INFINITY;
+  for (int s = 0; s < splits; ++s)
+    if (ml[2 * (s * rows + row) + 1] != 0.f) m = fmaxf(m, ml[2 * (s * rows + row)]);
+  float l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) {
+    const int64_t at = s * rows + row;
+    const float ls = ml[2 * at + 1];
+    if (ls == 0.f) continue;
+    const float f = exp2f(ml[2 * at] - m);
+    l += f * ls;
+    for (int e = 0; e < 4; ++e)
+      if (d0 + e < D) y[e] += f * po[at * D + d0 + e];
+  }
+  for (int e = 0; e < 4; ++e)
+    if (d0 + e < D) out[row * D + d0 + e] = from_f32<T>(l == 0.f ? 0.f : y[e] / l);
+}
+
+template <typename T, int DP>
+hipError_t launch_general(const HistArgs& a, hipStream_t s) {
+  const int64_t slots = a.R + (a.N * a.G + kGenTile - 1) / kGenTile;
+  if (!grid_fits(slots, 256)) return hipErrorInvalidConfiguration;
+  const uintptr_t all = reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) |
+                        reinterpret_cast<uintptr_t>(a.v);
+  const bool vec = a.D % 4 == 0 && a.q_stride % 4 == 0 && a.kv_stride % 4 == 0 &&
+                   a.page_stride % 4 == 0 && all % (4 * sizeof(T)) == 0;
+  return launch_kernel(vec ? history_general<T, DP, true> : history_general<T, DP, false>,
+                       dim3((uint32_t)slots, (uint32_t)a.Hk, (uint32_t)a.splits), dim3(256), s, a);
+}
+
+template <typename T>
+hipError_t launch_general(const HistArgs& a, hipStream_t s) {
+  if (a.D <= 32) return launch_general<T, 32>(a, s);
+  if (a.D <= 64) return launch_general<T, 64>(a, s);
+  if (a.D <= 128) return launch_general<T, 128>(a, s);
+  return launch_general<T, 256>(a, s);
+}
+
+}  // namespace
+
+HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
+  HistPlan p{};
+  p.rows = kGenTile;
+  (void)bf16;
+  // Splits: a history is cut where the tiles alone leave the chip idle, into
+  // chunks of at least 256 keys, up to about two workgroups a CU.
+  const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
+  const int64_t tiles = R * ((each + p.rows - 1) / p.rows) * Hk;
+  int64_t splits = 512 / (tiles > 0 ? tiles : 1);
+  if (splits > (max_len + 255) / 256) splits = (max_len + 255) / 256;
+  if (splits < 1) splits = 1;
+  p.chunk = (int)(((max_len + splits - 1) / splits + 63) / 64 * 64);
+  p.splits = p.chunk > 0 ? (int)((max_len + p.chunk - 1) / p.chunk) : 1;
+  if (p.splits < 1) p.splits = 1;
+  if (p.splits > 1) {
+    p.ml_bytes = align256((size_t)p.splits * N * H * 2 * sizeof(float));
+    p.o_bytes = align256((size_t)p.splits * N * H * D * sizeof(float));
+  }
+  return p;
+}
+
+hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s) {
+  (void)rows;
+  (void)fast;
+  hipError_t e = bf16 ? launch_general<bf16_t>(a, s) : launch_general<float>(a, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t threads = a.N * a.H * ((a.D + 3) / 4);
+  const int64_t blocks = (threads + 255) / 256;
+  if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+  if (bf16)
+    return launch_kernel(history_join<bf16_t>, dim3((uint32_t)blocks), dim3(256), s, a.part_ml,
+                         a.part_o, static_cast<bf16_t*>(a.out), a.N * a.H, a.D, a.splits);
+  return launch_kernel(history_join<float>, dim3((uint32_t)blocks), dim3(256), s, a.part_ml,
+                       a.part_o, static_cast<float*>(a.out), a.N * a.H, a.D, a.splits);
+}
+
+}  // namespace rocs

@@ -28,6 +28,9 @@ __all__ = [
     "ikbo_lcb", "ikbo_lcb_mapped", "ikbo_mlp2", "mlp2_workspace_size", "glm_fm_linear",
     "fm_linear_workspace_size", "request_ids",
     "validate_offsets", "RocsError",
+    "history_attention", "paged_attention", "history_workspace_size", "cache_pool", "cache_reserve",
+    "cache_write", "cache_fork", "cache_free", "cache_compact", "cache_copy", "cache_check",
+    "cache_workspace_size",
 ]
 
 RocsError = _lib.RocsError
@@ -48,6 +51,7 @@ class _PythonPath:
         return None
 
     linear = glm_linear = mlp2 = fm_linear = lcb = plan = attention = _none
+    history = paged = cache_reserve = cache_write = cache_fork = cache_free = cache_compact = _none
 
 
 def _native():
@@ -762,3 +766,351 @@ def validate_offsets(offsets, total, *, stream=None):
     lib = _lib.load()
     _lib.check(lib.rocs_validate_offsets(_ptr(offsets), offsets.numel(), total,
                                          _stream(stream)), "rocs_validate_offsets")
+
+
+# ---------------------------------------------------------------------------
+# Attention of a request's own rows over its history, and the cache's pages
+# ---------------------------------------------------------------------------
+
+def _launch(device, stream, name, *args):
+    """The C entry point `name` on the tensors' device, on `stream` or that device's current
+    stream."""
+    fn = getattr(_lib.load(), name)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            s = torch.cuda.current_stream() if stream is None else stream
+            _lib.check(fn(*args, ctypes.c_void_p(s.cuda_stream)), name)
+        return
+    _lib.check(fn(*args, _stream(stream)), name)
+
+
+def history_workspace_size(num_requests, num_rows, heads, kv_heads, head_dim, max_kv_len, dtype):
+    code = _lib.DTYPE_BF16 if dtype == torch.bfloat16 else _lib.DTYPE_F32
+    return int(_lib.load().rocs_history_workspace_size(num_requests, num_rows, heads, kv_heads,
+                                                       head_dim, max_kv_len, code))
+
+
+def _rows_of(t, name):
+    """Row stride of [rows, heads, d] (or pages of such rows) whose rows are dense; 0: one row."""
+    h, d = t.shape[-2:]
+    _need((d == 1 or t.stride(-1) == 1) and (h == 1 or t.stride(-2) == d),
+          f"{name} rows must be dense [heads, d] blocks")
+    if t.shape[-3] <= 1:
+        return 0
+    _need(t.stride(-3) >= h * d, f"{name} rows must not overlap")
+    return t.stride(-3)
+
+
+def _int_vector(t, n, name):
+    _need(t is None or (t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()
+                        and t.numel() == n),
+          f"{name} must be a contiguous int32 tensor of {n} entries")
+
+
+def _score_rules(q, k, v, heads_of, prefix_lens, q_offsets, slopes, cap, causal, max_kv_len, out):
+    """The checks that both attentions share; returns (out's shape, cap, max_kv_len)."""
+    _need(q.dim() == 3, "q must be [N, heads, d]")
+    n, h, d = q.shape
+    hk = heads_of.shape[-2]
+    _need(heads_of.shape[-1] == d and hk >= 1 and h % hk == 0,
+          "k and v must have q's head_dim, and heads that divide q's")
+    _dtype_code(q)
+    _need(k.dtype == q.dtype and v.dtype == q.dtype, "q, k, v must share one dtype")
+    _need(q_offsets.numel() >= 1, "q_offsets needs R + 1 entries")
+    r = q_offsets.numel() - 1
+    _offsets(q_offsets, r)
+    _int_vector(prefix_lens, r, "prefix_lens")
+    _need(slopes is None or (slopes.dtype == torch.float32 and slopes.shape == (h,)
+                             and slopes.is_contiguous()),
+          "slopes must be contiguous float32 [heads]")
+    _need(causal in (True, False), "causal must be True or False")
+    cap = float(cap or 0.0)
+    _need(0.0 <= cap < 3.4e38, "cap must be finite and not negative")
+    _need(max_kv_len is None or max_kv_len >= 0, "max_kv_len must not be negative")
+    _need(out is None or (out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()),
+          "out must be a contiguous [N, heads, d] tensor of q's dtype")
+    return r, cap, int(max_kv_len or 0)
+
+
+def _history_scratch(workspace, need, device, stream):
+    if workspace is None and need > 0:
+        workspace = _new(need, torch.uint8, device, stream, scratch=True)
+    _on_gpu(workspace)
+    _need(workspace is None or workspace.is_contiguous(), "workspace must be contiguous")
+    return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def history_attention(q, k, v, q_offsets, kv_offsets, *, causal=True, prefix_lens=None,
+                      q_docs=None, kv_docs=None, slopes=None, cap=0.0, max_kv_len=None, scale=None,
+                      out=None, workspace=None, stream=None):
+    """rocs_history_attention: each request's query rows (the last rows of its history) attend
+    over the history's keys.
+
+    q [N, H, d], k and v [L_total, H_kv, d] with H_kv dividing H (rows may be strided: column
+    slices of one projection), q_offsets and kv_offsets int32 [R + 1]. `causal` hides the keys
+    after a row, but for the first prefix_lens[r] (int32 [R]); q_docs [N] and kv_docs [L_total]
+    (int32) keep a row to its own document; `cap` > 0 caps scores to cap * tanh(s / cap);
+    `slopes` (float32 [H]) takes slopes[h] * distance off them. A row that sees no key is zero.
+    max_kv_len: a bound on the histories' lengths, if the host knows one."""
+    done = (_binding or _native()).history(q, k, v, q_offsets, kv_offsets, causal, prefix_lens,
+                                           q_docs, kv_docs, slopes, cap, max_kv_len, scale, out,
+                                           workspace, stream)
+    if done is not None:
+        return done
+    _need(k.dim() == 3 and v.dim() == 3 and k.shape == v.shape, "k and v must be [L, kv_heads, d]")
+    r, cap, most = _score_rules(q, k, v, k, prefix_lens, q_offsets, slopes, cap, causal,
+                                max_kv_len, out)
+    n, h, d = q.shape
+    rows, hk = k.shape[0], k.shape[1]
+    _offsets(kv_offsets, r)
+    _need((q_docs is None) == (kv_docs is None), "q_docs and kv_docs go together")
+    _int_vector(q_docs, n, "q_docs")
+    _int_vector(kv_docs, rows, "kv_docs")
+    q_stride, k_stride = _rows_of(q, "q"), _rows_of(k, "k")
+    _need(_rows_of(v, "v") == k_stride, "k and v must share a row stride")
+    _on_gpu(q, k, v, q_offsets, kv_offsets, prefix_lens, q_docs, kv_docs, slopes, out)
+    if out is None:
+        out = _new(q.shape, q.dtype, q.device, stream)
+    need = history_workspace_size(r, n, h, hk, d, most or rows, q.dtype)
+    workspace, ws_bytes = _history_scratch(workspace, need, q.device, stream)
+    _on_gpu(q, workspace)
+    _launch(q.device, stream, "rocs_history_attention", _ptr(q), q_stride, _ptr(k), _ptr(v),
+            k_stride, _ptr(q_offsets), _ptr(kv_offsets), _ptr(prefix_lens), _ptr(q_docs),
+            _ptr(kv_docs), _ptr(slopes), r, n, rows, h, hk, d, float(scale or 0.0), cap,
+            int(causal), most, _dtype_code(q), _ptr(out), _ptr(workspace), ws_bytes)
+    return out
+
+
+def paged_attention(q, k_pages, v_pages, page_table, kv_lens, q_offsets, *, slots=None,
+                    causal=True, prefix_lens=None, slopes=None, cap=0.0, max_kv_len=None,
+                    scale=None, out=None, workspace=None, stream=None):
+    """rocs_paged_attention: history_attention over histories kept in pages.
+
+    k_pages, v_pages [P, page_size, H_kv, d] (views of one cache: pages and rows may be strided),
+    page_table int32 [S, W], kv_lens int32 [S], slots int32 [R] (None: request r is slot r),
+    q [N, H, d] with q_offsets int32 [R + 1]: the last rows of each history, whose K/V are in
+    the cache already, or with causal=False any rows (candidates) that attend over it."""
+    done = (_binding or _native()).paged(q, k_pages, v_pages, page_table, kv_lens, q_offsets,
+                                         slots, causal, prefix_lens, slopes, cap, max_kv_len,
+                                         scale, out, workspace, stream)
+    if done is not None:
+        return done
+    _need(k_pages.dim() == 4 and v_pages.dim() == 4 and k_pages.shape == v_pages.shape,
+          "k_pages and v_pages must be [pages, page_size, kv_heads, d]")
+    r, cap, most = _score_rules(q, k_pages, v_pages, k_pages, prefix_lens, q_offsets, slopes, cap,
+                                causal, max_kv_len, out)
+    n, h, d = q.shape
+    pages, page, hk = k_pages.shape[:3]
+    _need(pages >= 1 and page >= 1, "the cache needs at least one page and one row a page")
+    _need(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
+          and page_table.shape[1] >= 1, "page_table must be a contiguous int32 [slots, width]")
+    n_slots, width = page_table.shape
+    _int_vector(kv_lens, n_slots, "kv_lens")
+    _int_vector(slots, r, "slots")
+    _need(slots is not None or r <= n_slots, "without slots, request r is slot r: R <= slots")
+    q_stride, k_stride = _rows_of(q, "q"), _rows_of(k_pages, "k_pages")
+    _need(_rows_of(v_pages, "v_pages") == k_stride, "k_pages and v_pages must share strides")
+    page_stride = 0
+    if pages > 1:
+        page_stride = k_pages.stride(0)
+        _need(v_pages.stride(0) == page_stride, "k_pages and v_pages must share strides")
+        _need(page_stride >= (page - 1) * k_stride + hk * d, "pages must not overlap")
+    _on_gpu(q, k_pages, v_pages, page_table, kv_lens, q_offsets, slots, prefix_lens, slopes, out)
+    if out is None:
+        out = _new(q.shape, q.dtype, q.device, stream)
+    bound = min(most or width * page, width * page)
+    need = history_workspace_size(r, n, h, hk, d, bound, q.dtype)
+    workspace, ws_bytes = _history_scratch(workspace, need, q.device, stream)
+    _on_gpu(q, workspace)
+    _launch(q.device, stream, "rocs_paged_attention", _ptr(q), q_stride, _ptr(k_pages),
+            _ptr(v_pages), page_stride, k_stride, _ptr(page_table), width, _ptr(kv_lens),
+            _ptr(slots), n_slots, _ptr(q_offsets), _ptr(prefix_lens), _ptr(slopes), r, n, pages,
+            page, h, hk, d, float(scale or 0.0), cap, int(causal), most, _dtype_code(q), _ptr(out),
+            _ptr(workspace), ws_bytes)
+    return out
+
+
+def cache_workspace_size(entries, num_pages):
+    return int(_lib.load().rocs_cache_workspace_size(entries, num_pages))
+
+
+def cache_pool(layers, pages, page_size, kv_heads, head_dim, *, slots, table_width,
+               dtype=torch.bfloat16, device="cuda"):
+    """An empty cache: (pool [layers, pages, page_size, 2, kv_heads, head_dim], page_table
+    int32 [slots, table_width], lens int32 [slots], refs int32 [pages]). A row holds K, then V, as
+    a stacked K/V projection writes it; layer l's pages for paged_attention are
+    pool[l, :, :, 0] and pool[l, :, :, 1]."""
+    pool = torch.zeros((layers, pages, page_size, 2, kv_heads, head_dim), dtype=dtype,
+                       device=device)
+    table = torch.full((slots, table_width), -1, dtype=torch.int32, device=device)
+    return (pool, table, torch.zeros(slots, dtype=torch.int32, device=device),
+            torch.zeros(pages, dtype=torch.int32, device=device))
+
+
+def _cache_state(page_table, lens, refs):
+    _need(page_table.dtype == torch.int32 and page_table.dim() == 2
+          and page_table.is_contiguous() and page_table.shape[0] >= 1
+          and page_table.shape[1] >= 1, "page_table must be a contiguous int32 [slots, width]")
+    if lens is not None:
+        _int_vector(lens, page_table.shape[0], "lens")
+    _need(refs.dtype == torch.int32 and refs.dim() == 1 and refs.is_contiguous()
+          and refs.numel() >= 1, "refs must be a contiguous int32 [pages]")
+    return page_table.shape[0], page_table.shape[1], refs.numel()
+
+
+def _cache_layers(pool, pages):
+    """(layers, page_size, bytes of a row) of a pool [layers, pages, page_size, ...]."""
+    _need(pool.dim() >= 4 and pool.is_contiguous() and pool.shape[1] == pages
+          and pool.numel() > 0, "pool must be a contiguous [layers, pages, page_size, ...] tensor")
+    layers, _, page = pool.shape[:3]
+    return layers, page, pool.numel() // (layers * pages * page) * pool.element_size()
+
+
+def _cache_status(status, device, stream):
+    if status is None:
+        return _new(2, torch.int32, device, stream)
+    _int_vector(status, 2, "status")
+    return status
+
+
+def cache_reserve(slots, row_offsets, num_rows, page_table, lens, refs, page_size, *, rows=None,
+                  status=None, workspace=None, stream=None):
+    """rocs_cache_reserve: entry i adds row_offsets[i + 1] - row_offsets[i] rows to slot slots[i]
+    (int32 [n], [n + 1]; num_rows = row_offsets[n]); lens, page_table and refs follow in place.
+    Returns (rows int32 [num_rows]: the pool row of each new row, for cache_write; status int32
+    [2], see cache_check). All or nothing: otherwise rows are -1 and the cache is unchanged."""
+    done = (_binding or _native()).cache_reserve(slots, row_offsets, num_rows, page_table, lens,
+                                                 refs, page_size, rows, status, workspace, stream)
+    if done is not None:
+        return done
+    n_slots, width, pages = _cache_state(page_table, lens, refs)
+    n = slots.numel()
+    _int_vector(slots, n, "slots")
+    _offsets(row_offsets, n)
+    _need(num_rows >= 0 and (n > 0 or num_rows == 0) and page_size >= 1,
+          "num_rows must be row_offsets' last entry, page_size at least 1")
+    _on_gpu(slots, row_offsets, page_table, lens, refs, rows, status)
+    if rows is None:
+        rows = _new(num_rows, torch.int32, slots.device, stream)
+    _int_vector(rows, num_rows, "rows")
+    status = _cache_status(status, slots.device, stream)
+    workspace, ws_bytes = _history_scratch(workspace, cache_workspace_size(n, pages), slots.device,
+                                           stream)
+    _on_gpu(slots, workspace)
+    _launch(slots.device, stream, "rocs_cache_reserve", _ptr(slots), _ptr(row_offsets), n, num_rows,
+            _ptr(page_table), width, _ptr(lens), n_slots, _ptr(refs), pages, page_size, _ptr(rows),
+            _ptr(status), _ptr(workspace), ws_bytes)
+    return rows, status
+
+
+def cache_write(x, rows, pool, *, stream=None):
+    """rocs_cache_write: row m of x [M, ...] into pool row rows[m] (from cache_reserve) of one
+    layer's pool [pages, page_size, ...]. x's rows may be strided; rows that are -1 are passed
+    over."""
+    if (_binding or _native()).cache_write(x, rows, pool, stream) is not None:
+        return pool
+    _need(pool.dim() >= 3 and pool.is_contiguous() and pool.numel() > 0,
+          "pool must be a contiguous [pages, page_size, ...] tensor")
+    _need(x.dtype == pool.dtype, "x and pool must share one dtype")
+    pool_rows = pool.shape[0] * pool.shape[1]
+    width = pool.numel() // pool_rows
+    _need(x.dim() >= 2 and x.numel() == x.shape[0] * width, "x must hold rows of the pool's width")
+    _int_vector(rows, x.shape[0], "rows")
+    m = x.shape[0]
+    if m == 0:
+        return pool
+    _need(x[0].is_contiguous() and (m == 1 or x.stride(0) >= width), "x's rows must be dense")
+    _on_gpu(x, rows, pool)
+    size = x.element_size()
+    _launch(x.device, stream, "rocs_cache_write", _ptr(x), (x.stride(0) if m > 1 else width) * size,
+            _ptr(rows), m, _ptr(pool), pool_rows, width * size)
+    return pool
+
+
+def cache_fork(parents, children, page_table, lens, refs, pool, *, status=None, workspace=None,
+               stream=None):
+    """rocs_cache_fork: the empty slot children[i] becomes a copy of slot parents[i] (int32 [n]):
+    full pages are shared, the rows of a page that is not full are copied in every layer of pool
+    [layers, pages, page_size, ...]. Returns status (see cache_check)."""
+    done = (_binding or _native()).cache_fork(parents, children, page_table, lens, refs, pool,
+                                              status, workspace, stream)
+    if done is not None:
+        return done
+    n_slots, width, pages = _cache_state(page_table, lens, refs)
+    layers, page, row_bytes = _cache_layers(pool, pages)
+    n = parents.numel()
+    _int_vector(parents, n, "parents")
+    _int_vector(children, n, "children")
+    _on_gpu(parents, children, page_table, lens, refs, pool, status)
+    status = _cache_status(status, pool.device, stream)
+    workspace, ws_bytes = _history_scratch(workspace, cache_workspace_size(n, pages), pool.device,
+                                           stream)
+    _on_gpu(pool, workspace)
+    _launch(pool.device, stream, "rocs_cache_fork", _ptr(parents), _ptr(children), n,
+            _ptr(page_table), width, _ptr(lens), n_slots, _ptr(refs), pages, page, _ptr(pool),
+            layers, row_bytes, _ptr(status), _ptr(workspace), ws_bytes)
+    return status
+
+
+def cache_free(slots, page_table, lens, refs, page_size, *, stream=None):
+    """rocs_cache_free: the pages of these slots (int32 [n]) back to the cache; the slots are
+    empty then."""
+    if (_binding or _native()).cache_free(slots, page_table, lens, refs, page_size,
+                                          stream) is not None:
+        return
+    n_slots, width, pages = _cache_state(page_table, lens, refs)
+    _int_vector(slots, slots.numel(), "slots")
+    _need(page_size >= 1, "page_size must be at least 1")
+    _on_gpu(slots, page_table, lens, refs)
+    _launch(refs.device, stream, "rocs_cache_free", _ptr(slots), slots.numel(), _ptr(page_table),
+            width, _ptr(lens), n_slots, _ptr(refs), pages, page_size)
+
+
+def cache_compact(page_table, lens, refs, pool, *, status=None, workspace=None, stream=None):
+    """rocs_cache_compact: the live pages moved together to the cache's front, in every layer of
+    pool; page_table and refs follow. Returns status int32 [2]: {0, number of live pages}."""
+    done = (_binding or _native()).cache_compact(page_table, lens, refs, pool, status, workspace,
+                                                 stream)
+    if done is not None:
+        return done
+    n_slots, width, pages = _cache_state(page_table, lens, refs)
+    layers, page, row_bytes = _cache_layers(pool, pages)
+    _on_gpu(page_table, lens, refs, pool, status)
+    status = _cache_status(status, pool.device, stream)
+    workspace, ws_bytes = _history_scratch(workspace, cache_workspace_size(0, pages), pool.device,
+                                           stream)
+    _on_gpu(pool, workspace)
+    _launch(pool.device, stream, "rocs_cache_compact", _ptr(page_table), width, n_slots, _ptr(refs),
+            pages, page, _ptr(pool), layers, row_bytes, _ptr(status), _ptr(workspace), ws_bytes)
+    return status
+
+
+def cache_copy(src_pages, dst_pages, src_pool, dst_pool=None, *, stream=None):
+    """rocs_cache_copy: page src_pages[i] of src_pool into page dst_pages[i] of dst_pool (None: the
+    same pool), in every layer of [layers, pages, page_size, ...]."""
+    dst_pool = src_pool if dst_pool is None else dst_pool
+    layers, page, row_bytes = _cache_layers(src_pool, src_pool.shape[1])
+    _need(_cache_layers(dst_pool, dst_pool.shape[1]) == (layers, page, row_bytes),
+          "the pools must have the same layers and pages of the same size")
+    _need(src_pool.dtype == dst_pool.dtype, "the pools must share one dtype")
+    n = src_pages.numel()
+    _int_vector(src_pages, n, "src_pages")
+    _int_vector(dst_pages, n, "dst_pages")
+    _on_gpu(src_pages, dst_pages, src_pool, dst_pool)
+    _launch(src_pool.device, stream, "rocs_cache_copy", _ptr(src_pages), _ptr(dst_pages), n,
+            _ptr(src_pool), src_pool.shape[1], _ptr(dst_pool), dst_pool.shape[1], layers,
+            page * row_bytes)
+    return dst_pool
+
+
+def cache_check(status):
+    """Raises RocsError if a page operator could not be done. Reads status on the host (waits for
+    the current stream). Returns status[1]."""
+    code, detail = status.tolist()
+    if code != 0:
+        why = {_lib.CACHE_NO_PAGES: f"{detail} pages are missing",
+               _lib.CACHE_TABLE_FULL: "a slot would need more pages than its table row has",
+               _lib.CACHE_BAD_SLOT: "a slot is out of range, named twice or (a child) not empty"}
+        raise RocsError(_lib.INVALID_ARGUMENT,
+                        f"the cache is unchanged: {why.get(code, f'status {code}')}")
+    return detail
