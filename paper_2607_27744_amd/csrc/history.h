@@ -24,6 +24,7 @@ struct HistArgs {
   int64_t N, q_stride, kv_stride, page_stride;   // strides in elements
   int64_t width, pages;     // table columns, pages in the cache
   int R, S, H, Hk, G, D, page_size;              // G = H / Hk
+  uint32_t page_magic;      // 2^32 / (page_size / 16) + 1 (MFMA kernels)
   float scale, cap;
   int causal;
   int64_t max_len;          // bound on a history's length
@@ -42,6 +43,7 @@ struct HistPlan {
   size_t ml_bytes, o_bytes; // of the workspace, 256-byte aligned
 };
 HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16);
+hipError_t launch_history_tile(const HistArgs& a, hipStream_t s);
 hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s);
 
 hipError_t launch_reserve(const int32_t* slots, const int32_t* row_off, int64_t n, int64_t M,

@@ -235,8 +235,7 @@ hipError_t launch_general(const HistArgs& a, hipStream_t s) {
 
 HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
   HistPlan p{};
-  p.rows = kGenTile;
-  (void)bf16;
+  p.rows = bf16 && (D == 64 || D == 128) ? 128 : kGenTile;
   // Splits: a history is cut where the tiles alone leave the chip idle, into
   // chunks of at least 256 keys, up to about two workgroups a CU.
   const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
@@ -255,9 +254,9 @@ HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_le
 }
 
 hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s) {
-  (void)rows;
-  (void)fast;
-  hipError_t e = bf16 ? launch_general<bf16_t>(a, s) : launch_general<float>(a, s);
+  hipError_t e = fast && rows == 128 ? launch_history_tile(a, s)
+                 : bf16              ? launch_general<bf16_t>(a, s)
+                                     : launch_general<float>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t threads = a.N * a.H * ((a.D + 3) / 4);
   const int64_t blocks = (threads + 255) / 256;

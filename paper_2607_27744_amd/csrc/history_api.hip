@@ -216,6 +216,7 @@ int32_t rocs_paged_attention(const void* q, int64_t q_row_stride, const void* k_
   a.pages = num_pages; a.S = (int)num_slots; a.page_size = page_size;
   a.q_stride = q_row_stride != 0 ? q_row_stride : (int64_t)H * D;
   a.kv_stride = kv_stride;
+  a.page_magic = page_size >= 32 ? (uint32_t)((uint64_t(1) << 32) / (uint32_t)(page_size / 16)) + 1u : 0u;
   a.page_stride = page_stride != 0 ? page_stride : page_size * kv_stride;
   const int64_t k_bytes = ((num_pages - 1) * a.page_stride + extent) * (int64_t)esize(dtype);
   const int64_t bound = table_width * page_size;

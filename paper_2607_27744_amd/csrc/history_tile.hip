@@ -1,0 +1,423 @@
+// History attention, the tiled bf16 kernel: 128 rows (token, head) of one
+// request and K/V head a workgroup.
+//
+// Structure and reasons are those of the candidate attention's tiled kernel
+// (dca_attn_bf16): four waves of 32 rows share K/V stages of 64 keys that come
+// into two-slot LDS rings by DMA, K two stages and V one stage ahead; the
+// scores of the next stage run on the matrix cores while the VALU forms the
+// weights of this one; weights are taken against a running max that moves only
+// when a stage could pass 2^64. What differs:
+//
+// Masks. A row sees a leading run of keys (causal, prefix, the history's end)
+// and, with documents, part of it. A wave ends with the stage that its last
+// row sees, and stages that all its rows see whole run without a test: two
+// copies of the stage, the masked one with the general form of the bias.
+// The rows of a tile need not have seen a key yet when a stage starts
+// (documents), so a row's max may stay -inf; its weights are then 0.
+// Work order. Under the causal mask a request's last tiles are the longest:
+// they come first, so that the launch does not end with them.
+// Grouped heads. Rows are (token, head of the group), so the heads of a group
+// share the K/V stage.
+#include "history_mfma.h"
+#include "launch.h"
+
+namespace rocs {
+namespace {
+
+constexpr int kRows = 128;
+constexpr int kRing = 2;
+
+template <int D, int SCORE, bool DOCS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void
+history_tile(const HistArgs a, int64_t slots) {
+  constexpr int KB = 2, KS = D / 16, DB = D / 32, PS = 4;
+  constexpr int ROWB = 2 * D, CR = D / 8;
+  constexpr int STAGE = kStageKeys * ROWB;
+  constexpr int KPI = 1024 / ROWB;          // rows of a DMA load
+  constexpr int NI = 16 / KPI;              // loads a wave, operand and stage (its 16 rows)
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kRing * STAGE];
+  __shared__ __attribute__((aligned(16))) int32_t doc_ids[DOCS ? 2 * kStageKeys : 4];
+  __shared__ typename std::conditional<DOCS, DocList, int>::type doc_list;
+  ROCS_LDS char* const lds3 = (ROCS_LDS char*)lds;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, hh = lane >> 5;
+  const uint32_t work = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t per_head = (uint32_t)slots * (uint32_t)a.splits;
+  const int hk = (int)(work / per_head);
+  const uint32_t rest = work - (uint32_t)hk * per_head;
+  const int split = (int)(rest % (uint32_t)a.splits);
+  const HistTile t = hist_tile(a, slots - 1 - rest / (uint32_t)a.splits, kRows);
+  if (t.rows <= 0) return;
+
+  const int wrow0 = wave * 32;
+  const bool active = wrow0 < t.rows;
+  const int row = t.row0 + min(wrow0 + l32, t.rows - 1);      // clamped; extra rows never stored
+  const int token = row / a.G, head = hk * a.G + row % a.G;
+  RowRule rule;
+  rule.scale2 = a.scale * kLog2e;
+  rule.cap_in = a.cap > 0.f ? 2.0f * rule.scale2 / a.cap : 0.f;
+  rule.cap2 = a.cap * kLog2e;
+  rule.slope2 = (SCORE & kBias) != 0 ? a.slopes[head] * kLog2e : 0.f;
+  rule.pos = position_of(t, token);
+  rule.lim = limit_of(a, t, token);
+  rule.doc = DOCS ? a.q_docs[t.q0 + token] : 0;
+  // The wave's first and last rows bound what it sees.
+  const int first = (t.row0 + min(wrow0, t.rows - 1)) / a.G;
+  const int last = (t.row0 + min(wrow0 + 31, t.rows - 1)) / a.G;
+  const int lim_lo = limit_of(a, t, first);
+  const int lim_hi = active ? limit_of(a, t, last) : 0;
+  const int plain = (SCORE & kBias) != 0 ? min(lim_lo, position_of(t, first) + 1) : lim_lo;
+  const int most = limit_of(a, t, (t.row0 + t.rows - 1) / a.G);
+  const int lo = split * a.chunk, hi = split_end(a, split, most);
+
+  bf16x8 qf[KS];
+  {
+    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + 16 * ks + 8 * hh);
+  }
+
+  const KeyFeed feed(a, t);
+  const char* kbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + (int64_t)hk * D);
+  const char* vbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + (int64_t)hk * D);
+  // DMA lane map: load i of this wave's 16 rows of a stage fills rows KPI i +
+  // lane / CR, chunk position lane % CR, with chunk (lane % CR) ^ kv_swizzle.
+  int srow[NI];
+  uint32_t schunk[NI], soff[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    srow[i] = KPI * i + lane / CR;
+    schunk[i] = 16u * (uint32_t)((lane % CR) ^ kv_swizzle<D>(srow[i]));
+    soff[i] = (uint32_t)(srow[i] * feed.row_bytes) + schunk[i];
+  }
+  const uint32_t lds_base = lds_addr(lds);
+  // This wave's group of the stage at key `base`: past the end the group of
+  // the last key stands in.
+  auto group_of = [&](int base) __attribute__((always_inline)) {
+    return feed.group(min(base + 16 * wave, (hi - 1) & ~15));
+  };
+  auto issue = [&](const char* src, int base, int64_t off, uint32_t dst) __attribute__((always_inline)) {
+    const char* s = uniform_ptr(src + off);
+    dst += 16 * wave * ROWB;
+    if (base + 16 * wave + 16 <= hi) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) lds_dma16_sv(s, soff[i], dst + 1024u * i);
+    } else {
+      const int end = hi - 1 - min(base + 16 * wave, (hi - 1) & ~15);    // last row of the group
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        lds_dma16_sv(s, (uint32_t)(min(srow[i], end) * feed.row_bytes) + schunk[i], dst + 1024u * i);
+    }
+  };
+  auto issue_k = [&](int slot, int base, int64_t off) { issue(kbase, base, off, lds_base + slot * STAGE); };
+  auto issue_v = [&](int slot, int base, int64_t off) {
+    issue(vbase, base, off, lds_base + (kRing + slot) * STAGE);
+    if constexpr (DOCS) {
+      if (wave == 0)
+        lds_dma4(a.kv_docs + t.kv0 + min(base + lane, hi - 1), lds_addr(doc_ids) + 4u * kStageKeys * slot);
+    }
+  };
+
+  const uint32_t ka0 = (uint32_t)(l32 * ROWB + 16 * (hh ^ kv_swizzle<D>(l32)));
+  uint32_t va0[2];
+#pragma unroll
+  for (int rr = 0; rr < 2; ++rr) {
+    const int g = lane >> 4, jl = lane & 15;
+    const int key = 4 * (g >> 1) + 8 * rr + (jl >> 2);
+    const int chunk0 = 2 * (g & 1) + ((jl & 3) >> 1);
+    va0[rr] = (uint32_t)(kRing * STAGE + key * ROWB + 16 * (chunk0 ^ kv_swizzle<D>(key)) + 8 * (jl & 1));
+  }
+
+  int n = hi > lo ? (hi - lo + kStageKeys - 1) / kStageKeys : 0;
+  bool listed = false;
+  if constexpr (DOCS) {
+    if (n > 0) {
+      const int found = doc_stages(doc_list, a.kv_docs + t.kv0, rule.doc, lo, hi);
+      listed = found >= 0;
+      if (listed) n = found;
+    }
+  }
+  auto stage_at = [&](int i) __attribute__((always_inline)) -> int {   // its first key
+    if constexpr (DOCS) {
+      if (listed)
+        return lo + __builtin_amdgcn_readfirstlane(doc_list.entry[i] & (kMixed - 1)) * kStageKeys;
+    }
+    return lo + i * kStageKeys;
+  };
+
+  float m_run = -INFINITY, l_part = 0.f;
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+
+  auto qk_step = [&](int slot, int ks, f32x16 (&s)[KB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const bf16x8 f = *reinterpret_cast<const ROCS_LDS bf16x8*>(
+          lds3 + ((ka0 ^ (32u * ks)) + slot * STAGE + kb * 32 * ROWB));
+      s[kb] = mfma32(f, qf[ks], s[kb]);
+    }
+  };
+  // Weights of step ps as packed bf16 B fragments, against ms. Each pair is a
+  // scalar of its own (see dca_attn_bf16).
+  auto weights = [&](const f32x16 (&s)[KB], int ps, float ms, uint32_t (&pk)[4], float& sum)
+      __attribute__((always_inline)) {
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float s0 = s[ps / 2][8 * (ps % 2) + 2 * w], s1 = s[ps / 2][8 * (ps % 2) + 2 * w + 1];
+      float e0, e1;
+      if constexpr (SCORE == 0) {
+        e0 = fmaf(s0, rule.scale2, -ms);
+        e1 = fmaf(s1, rule.scale2, -ms);
+      } else {
+        e0 = s0 - ms;
+        e1 = s1 - ms;
+      }
+      pk[w] = pack_bf16x2(__builtin_amdgcn_exp2f(e0), __builtin_amdgcn_exp2f(e1));
+      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[w]), ones, sum, false);
+    }
+  };
+  // One stage: its weights and PV product, with the scores of the next one
+  // (NEXT) on the matrix cores meanwhile. GEN: masks and the general bias.
+  auto stage = [&](auto gen, auto next, int slot, int base, f32x16 (&s)[KB], f32x16 (&sn)[KB])
+      __attribute__((always_inline)) {
+    constexpr bool GEN = decltype(gen)::value, NEXT = decltype(next)::value;
+    if constexpr (NEXT) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) sn[kb] = f32x16{};
+    }
+    uint32_t pk[PS][4];
+    float sum = 0.f;
+    const ROCS_LDS int32_t* ids = (const ROCS_LDS int32_t*)doc_ids + (DOCS ? kStageKeys * slot : 0);
+#pragma unroll
+    for (int ps = 0; ps < PS; ++ps) {
+      if constexpr (NEXT) {
+#pragma unroll
+        for (int ks = KS / PS * ps; ks < KS / PS * (ps + 1); ++ks) qk_step(slot ^ 1, ks, sn);
+      }
+      score_step<SCORE, GEN>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
+      if constexpr (GEN) mask_step<DOCS>(s[ps / 2], ps / 2, ps % 2, rule, base, hh, ids);
+      weights(s, ps, m_run, pk[ps], sum);
+      if constexpr (D == 64 || GEN) __builtin_amdgcn_sched_barrier(0);
+    }
+    if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
+      float mx = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+      mx = max_across_halves(mx) * (SCORE == 0 ? rule.scale2 : 1.0f);
+      const bool need = mx > m_run + kLazyMove;
+      const float alpha = need ? exp2f(m_run - mx) : 1.0f;     // 0 for a row's first keys
+      if (need) m_run = mx;
+      l_part *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+      sum = 0.f;
+      const float ms = m_run == -INFINITY ? 0.f : m_run;       // no key seen yet: weights 0
+#pragma unroll
+      for (int ps = 0; ps < PS; ++ps) weights(s, ps, ms, pk[ps], sum);
+    }
+    l_part += sum;
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int ps = 0; ps < PS; ++ps) {
+      const bf16x8 pf = as_bf16x8(u32x4{pk[ps][0], pk[ps][1], pk[ps][2], pk[ps][3]});
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const uint32_t off = slot * STAGE + ps * 16 * ROWB;
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (ROCS_LDS i16x4*)(lds3 + ((va0[0] ^ (64u * db)) + off))));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (ROCS_LDS i16x4*)(lds3 + ((va0[1] ^ (64u * db)) + off))));
+        oacc[db] = mfma32(as_bf16x8(u32x4{x[0], x[1], y[0], y[1]}), pf, oacc[db]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  if (n > 0) {
+    using Yes = std::true_type;
+    using No = std::false_type;
+    // The wave's own stages, and how many of them (an even number, each with a
+    // stage after it) need no mask.
+    int nw = 0, free = 0;
+    if constexpr (DOCS) {
+      if (listed) {
+        for (int i = 0; i < n; i += 64)
+          nw += __builtin_popcountll(__ballot(
+              i + lane < n && lo + (doc_list.entry[i + lane] & (kMixed - 1)) * kStageKeys < lim_hi));
+      } else {
+        nw = max(min(n, (lim_hi - lo + kStageKeys - 1) / kStageKeys), 0);
+      }
+    } else {
+      nw = max(min(n, (lim_hi - lo + kStageKeys - 1) / kStageKeys), 0);
+      free = max(min((plain - lo) / kStageKeys, nw - 1), 0) & ~1;
+    }
+    nw = __builtin_amdgcn_readfirstlane(nw);
+    // The stages at kt, kt + 1 and kt + 2 (first keys), and the group offsets
+    // of the two that are still to be loaded; a stage's table entry is read a
+    // step before its first load.
+    int b0 = stage_at(0), b1 = stage_at(min(1, n - 1)), b2 = stage_at(min(2, n - 1));
+    const int64_t o0 = group_of(b0);
+    int64_t o1 = group_of(b1), o2 = group_of(b2);
+    issue_k(0, b0, o0);
+    issue_v(0, b0, o0);
+    if (n > 1) issue_k(1, b1, o1);
+    wait_vmcnt<0>();                                      // the query fragments included
+    ring_barrier();
+    f32x16 s_a[KB], s_b[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) s_a[kb] = f32x16{};
+    if (nw > 0) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        qk_step(0, ks, s_a);
+        if (ks % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    ring_barrier();                                       // K slot 0 has been read
+    // A step reads K of stage kt + 1 and V of stage kt; their other slots were
+    // released by the last barrier and take K of kt + 2 and V of kt + 1.
+    auto load = [&](int kt, int slot) __attribute__((always_inline)) {
+      if (kt + 2 < n) issue_k(slot, b2, o2);
+      if (kt + 1 < n) issue_v(slot ^ 1, b1, o1);
+    };
+    auto pass = [&](int kt) __attribute__((always_inline)) {
+      b0 = b1;
+      b1 = b2;
+      o1 = o2;
+      if (kt + 3 < n) {
+        b2 = stage_at(kt + 3);
+        o2 = group_of(b2);
+      }
+      wait_vmcnt<0>();
+      ring_barrier();
+    };
+    int kt = 0;
+    auto step = [&](auto gen, int slot, f32x16 (&cur)[KB], f32x16 (&nxt)[KB]) __attribute__((always_inline)) {
+      load(kt, slot);
+      stage(gen, Yes{}, slot, b0, cur, nxt);
+      pass(kt);
+      ++kt;
+    };
+    while (kt < free) {                                   // the score buffers swap roles
+      step(No{}, 0, s_a, s_b);
+      step(No{}, 1, s_b, s_a);
+    }
+    while (kt + 1 < nw) {
+      step(Yes{}, 0, s_a, s_b);
+      if (kt + 1 >= nw) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) s_a[kb] = s_b[kb];
+        break;
+      }
+      step(Yes{}, 1, s_b, s_a);
+    }
+    if (kt < nw) {
+      load(kt, kt & 1);
+      stage(Yes{}, No{}, kt & 1, b0, s_a, s_b);
+      pass(kt);
+      ++kt;
+    }
+    for (; kt < n; ++kt) {                                // the other waves' stages
+      load(kt, kt & 1);
+      pass(kt);
+    }
+  }
+
+  // Epilogue. The addresses come from a laundered lane index, so that they are
+  // not held through the main loop.
+  if (!active) return;
+  int lane_e = lane;
+  asm volatile("" : "+v"(lane_e));
+  const int l32e = lane_e & 31, hhe = lane_e >> 5;
+  const float l = sum_across_halves(l_part);
+  const uint64_t odd = __ballot(any_odd(oacc, l));
+  const int mine = min(t.rows - wrow0, 32);
+  uint32_t again = ((uint32_t)odd | (uint32_t)(odd >> 32)) & (mine == 32 ? ~0u : (1u << mine) - 1u);
+  auto out_row = [&](int i) -> int64_t {                  // row i of the wave
+    const int rw = t.row0 + wrow0 + i;
+    return (t.q0 + rw / a.G) * a.H + hk * a.G + rw % a.G;
+  };
+  if (a.splits > 1) {
+    if (l32e < mine) {
+      const int64_t to = (int64_t)split * a.N * a.H + out_row(l32e);
+      if (hhe == 0) {
+        a.part_ml[2 * to] = m_run;
+        a.part_ml[2 * to + 1] = l;
+      }
+      if (l != 0.f) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4*>(a.part_o + to * D + 32 * db + 8 * q + 4 * hhe) =
+                f32x4{oacc[db][4 * q], oacc[db][4 * q + 1], oacc[db][4 * q + 2], oacc[db][4 * q + 3]};
+      }
+    }
+  } else {
+    // Through this wave's share of the idle ring: row-contiguous stores.
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const uint32_t obase = (uint32_t)(wave * 32 * ROWB);
+    auto swz = [](int r) { return CR == 16 ? (r & 15) : ((r >> 1) & 7); };
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const f32x16& o = oacc[db];
+        const uint32_t e0 = pack_bf16x2(o[8 * j] * inv, o[8 * j + 1] * inv);
+        const uint32_t e1 = pack_bf16x2(o[8 * j + 2] * inv, o[8 * j + 3] * inv);
+        const uint32_t o0 = pack_bf16x2(o[8 * j + 4] * inv, o[8 * j + 5] * inv);
+        const uint32_t o1 = pack_bf16x2(o[8 * j + 6] * inv, o[8 * j + 7] * inv);
+        const auto x = __builtin_amdgcn_permlane32_swap(e0, o0, false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(e1, o1, false, false);
+        *reinterpret_cast<ROCS_LDS u32x4*>(lds3 + obase + l32e * ROWB +
+                                           16 * ((4 * db + 2 * j + hhe) ^ swz(l32e))) =
+            u32x4{x[0], y[0], x[1], y[1]};
+      }
+    constexpr int RPS = 1024 / ROWB, NST = 32 / RPS;
+#pragma unroll
+    for (int i = 0; i < NST; ++i) {
+      const int r = RPS * i + lane_e / CR;
+      const u32x4 v = *reinterpret_cast<const ROCS_LDS u32x4*>(
+          lds3 + obase + r * ROWB + 16 * ((lane_e % CR) ^ swz(r)));
+      if (r < mine)
+        *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.out) + out_row(r) * D + 8 * (lane_e % CR)) = v;
+    }
+  }
+  while (again != 0) {                                    // see lone_row
+    const int i = __builtin_ctz(again);
+    again &= again - 1;
+    redo_row<bf16_t>(a, t, t.row0 + wrow0 + i, hk, lo, hi, split);
+  }
+}
+
+template <int D, int SCORE>
+hipError_t launch_score(const HistArgs& a, int64_t slots, int64_t blocks, hipStream_t s) {
+  return launch_kernel(a.q_docs != nullptr ? history_tile<D, SCORE, true> : history_tile<D, SCORE, false>,
+                       dim3((uint32_t)blocks), dim3(256), s, a, slots);
+}
+
+template <int D>
+hipError_t launch_dim(const HistArgs& a, int64_t slots, int64_t blocks, hipStream_t s) {
+  const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
+  if (cap && bias) return launch_score<D, kCap | kBias>(a, slots, blocks, s);
+  if (cap) return launch_score<D, kCap>(a, slots, blocks, s);
+  if (bias) return launch_score<D, kBias>(a, slots, blocks, s);
+  return launch_score<D, 0>(a, slots, blocks, s);
+}
+
+}  // namespace
+
+hipError_t launch_history_tile(const HistArgs& a, hipStream_t s) {
+  const int64_t slots = a.R + (a.N * a.G + kRows - 1) / kRows;
+  const int64_t blocks = slots * a.Hk * a.splits;
+  if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+  return a.D == 128 ? launch_dim<128>(a, slots, blocks, s) : launch_dim<64>(a, slots, blocks, s);
+}
+
+}  // namespace rocs
