@@ -59,29 +59,36 @@ struct RowRule {
   int pos, lim, doc;
 };
 
-// Scores of one 16-key step (elements 8 half .. + 7 of the block at key
-// offset 32 kb) into exp2 units, keys from `base` (of the stage). GEN: any
-// stage; else one wholly before every row of the wave and unmasked.
-template <int SCORE, bool GEN, typename V>
+// One score in exp2 units for a stage that needs no mask and lies before the
+// row: key offset c in the stage, shift = plain_shift, less the running max.
+template <int SCORE>
+__device__ __forceinline__ float plain_shift(const RowRule& r, int base, int hh) {
+  float x = (SCORE & kCap) != 0 ? r.cap2 : 0.f;
+  if constexpr ((SCORE & kBias) != 0) x -= r.slope2 * (float)(r.pos - base - 4 * hh);
+  return x;
+}
+template <int SCORE>
+__device__ __forceinline__ float plain_score(float s, int c, const RowRule& r, float shift) {
+  if constexpr ((SCORE & kBias) != 0) shift = fmaf(r.slope2, (float)c, shift);
+  if constexpr ((SCORE & kCap) != 0)
+    return fmaf(-2.0f * r.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * r.cap_in)), shift);
+  return fmaf(s, r.scale2, shift);
+}
+
+// Scores of one 16-key step (elements 8 half .. + 7 of the block at key offset
+// 32 kb) in exp2 units, in place; keys from `base` (of the stage).
+template <int SCORE, typename V>
 __device__ __forceinline__ void score_step(V& s, int kb, int half, const RowRule& r, int base, int hh) {
-  if constexpr (SCORE == 0) return;
-  const int off = base + 4 * hh;
-  const float rel = (float)(r.pos - off);
-  const float lin = -r.slope2 * rel;
+  const float rel = (float)(r.pos - base - 4 * hh);
 #pragma unroll
   for (int e = 8 * half; e < 8 * half + 8; ++e) {
     const int c = 32 * kb + 8 * (e / 4) + e % 4;
     float y;
-    if constexpr ((SCORE & kCap) != 0) {
-      const float u = __builtin_amdgcn_exp2f(s[e] * r.cap_in);
-      y = fmaf(-2.0f * r.cap2, __builtin_amdgcn_rcpf(1.0f + u), r.cap2);
-    } else {
+    if constexpr ((SCORE & kCap) != 0)
+      y = fmaf(-2.0f * r.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[e] * r.cap_in)), r.cap2);
+    else
       y = s[e] * r.scale2;
-    }
-    if constexpr ((SCORE & kBias) != 0) {
-      if constexpr (GEN) y = fmaf(-r.slope2, fabsf(rel - (float)c), y);
-      else y += fmaf(r.slope2, (float)c, lin);
-    }
+    if constexpr ((SCORE & kBias) != 0) y = fmaf(-r.slope2, fabsf(rel - (float)c), y);
     s[e] = y;
   }
 }

@@ -159,23 +159,25 @@ history_tile(const HistArgs a, int64_t slots) {
       s[kb] = mfma32(f, qf[ks], s[kb]);
     }
   };
-  // Weights of step ps as packed bf16 B fragments, against ms. Each pair is a
-  // scalar of its own (see dca_attn_bf16).
-  auto weights = [&](const f32x16 (&s)[KB], int ps, float ms, uint32_t (&pk)[4], float& sum)
-      __attribute__((always_inline)) {
+  // Weights of step ps as packed bf16 B fragments, against ms. FINAL: the
+  // scores are in exp2 units already; else they are raw, of a stage without a
+  // mask, and the rules and the subtraction share their fused multiply-adds.
+  // Each pair is a scalar of its own (see dca_attn_bf16).
+  auto weights = [&](auto final, const f32x16 (&s)[KB], int ps, int base, float ms, uint32_t (&pk)[4],
+                     float& sum) __attribute__((always_inline)) {
     const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+    const float lin = plain_shift<SCORE>(rule, base, hh) - ms;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float s0 = s[ps / 2][8 * (ps % 2) + 2 * w], s1 = s[ps / 2][8 * (ps % 2) + 2 * w + 1];
-      float e0, e1;
-      if constexpr (SCORE == 0) {
-        e0 = fmaf(s0, rule.scale2, -ms);
-        e1 = fmaf(s1, rule.scale2, -ms);
-      } else {
-        e0 = s0 - ms;
-        e1 = s1 - ms;
+      float e[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int el = 8 * (ps % 2) + 2 * w + i;
+        const float x = s[ps / 2][el];
+        if constexpr (decltype(final)::value) e[i] = x - ms;
+        else e[i] = plain_score<SCORE>(x, 32 * (ps / 2) + 8 * (el / 4) + el % 4, rule, lin);
       }
-      pk[w] = pack_bf16x2(__builtin_amdgcn_exp2f(e0), __builtin_amdgcn_exp2f(e1));
+      pk[w] = pack_bf16x2(__builtin_amdgcn_exp2f(e[0]), __builtin_amdgcn_exp2f(e[1]));
       sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[w]), ones, sum, false);
     }
   };
@@ -197,18 +199,24 @@ history_tile(const HistArgs a, int64_t slots) {
 #pragma unroll
         for (int ks = KS / PS * ps; ks < KS / PS * (ps + 1); ++ks) qk_step(slot ^ 1, ks, sn);
       }
-      score_step<SCORE, GEN>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
-      if constexpr (GEN) mask_step<DOCS>(s[ps / 2], ps / 2, ps % 2, rule, base, hh, ids);
-      weights(s, ps, m_run, pk[ps], sum);
+      if constexpr (GEN) {
+        score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
+        mask_step<DOCS>(s[ps / 2], ps / 2, ps % 2, rule, base, hh, ids);
+      }
+      weights(gen, s, ps, base, m_run, pk[ps], sum);
       if constexpr (D == 64 || GEN) __builtin_amdgcn_sched_barrier(0);
     }
     if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
+      if constexpr (!GEN) {
+#pragma unroll
+        for (int ps = 0; ps < PS; ++ps) score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
+      }
       float mx = s[0][0];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
-      mx = max_across_halves(mx) * (SCORE == 0 ? rule.scale2 : 1.0f);
+      mx = max_across_halves(mx);
       const bool need = mx > m_run + kLazyMove;
       const float alpha = need ? exp2f(m_run - mx) : 1.0f;     // 0 for a row's first keys
       if (need) m_run = mx;
@@ -218,7 +226,7 @@ history_tile(const HistArgs a, int64_t slots) {
       sum = 0.f;
       const float ms = m_run == -INFINITY ? 0.f : m_run;       // no key seen yet: weights 0
 #pragma unroll
-      for (int ps = 0; ps < PS; ++ps) weights(s, ps, ms, pk[ps], sum);
+      for (int ps = 0; ps < PS; ++ps) weights(std::true_type{}, s, ps, base, ms, pk[ps], sum);
     }
     l_part += sum;
     __builtin_amdgcn_s_setprio(1);
@@ -308,18 +316,21 @@ history_tile(const HistArgs a, int64_t slots) {
       step(No{}, 0, s_a, s_b);
       step(No{}, 1, s_b, s_a);
     }
-    while (kt + 1 < nw) {
-      step(Yes{}, 0, s_a, s_b);
-      if (kt + 1 >= nw) {
+    // Stages with a mask, one after the other: in step with the next stage's
+    // scores they would need more registers than there are.
+    while (kt < nw) {
+      const int slot = kt & 1;
+      load(kt, slot);
+      stage(Yes{}, No{}, slot, b0, s_a, s_a);
+      if (kt + 1 < nw) {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s_a[kb] = s_b[kb];
-        break;
+        for (int kb = 0; kb < KB; ++kb) s_a[kb] = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          qk_step(slot ^ 1, ks, s_a);
+          if (ks % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      step(Yes{}, 1, s_b, s_a);
-    }
-    if (kt < nw) {
-      load(kt, kt & 1);
-      stage(Yes{}, No{}, kt & 1, b0, s_a, s_b);
       pass(kt);
       ++kt;
     }
