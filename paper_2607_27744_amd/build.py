@@ -19,7 +19,8 @@ BUILD_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "librocs.so")
 BINDING_PATH = os.path.join(PKG, "_binding.so")
 SOURCES = ["api.hip", "linear.hip", "attention.hip", "interaction.hip", "lcb.hip", "mlp.hip",
-           "fmlinear.hip", "history_api.hip", "history.hip", "history_tile.hip", "cache.hip"]
+           "fmlinear.hip", "history_api.hip", "history.hip", "history_tile.hip", "history_split.hip",
+           "cache.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")
 ARCH = "gfx950"

@@ -44,6 +44,7 @@ struct HistPlan {
 };
 HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16);
 hipError_t launch_history_tile(const HistArgs& a, hipStream_t s);
+hipError_t launch_history_split(const HistArgs& a, hipStream_t s);
 hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s);
 
 hipError_t launch_reserve(const int32_t* slots, const int32_t* row_off, int64_t n, int64_t M,

@@ -181,34 +181,62 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
 
 // ---------------------------------------------------------------------------
 // Join of a split history: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.
-// A thread per four dims of a (token, head); a part without a seen key has
-// l = 0 and its O is not read. Bound by the read of the parts.
+// A wave a row: lanes hold the parts' weights, then each lane adds four dims
+// (a lane group a part where a row has fewer than 256) of four parts at a time.
+// A part without a seen key has l = 0 and its O is not read. Bound by latency
+// for few rows, else by the read of the parts.
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void history_join(const float* __restrict__ ml,
                                                     const float* __restrict__ po,
                                                     T* __restrict__ out, int64_t rows, int D,
                                                     int splits) {
-  const int quads = (D + 3) / 4;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = i / quads;
-  const int d0 = 4 * (int)(i - row * quads);
-  if (row >= rows) return;
-  float m = -INFINITY;
-  for (int s = 0; s < splits; ++s)
-    if (ml[2 * (s * rows + row) + 1] != 0.f) m = fmaxf(m, ml[2 * (s * rows + row)]);
-  float l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const int64_t at = s * rows + row;
-    const float ls = ml[2 * at + 1];
-    if (ls == 0.f) continue;
-    const float f = exp2f(ml[2 * at] - m);
-    l += f * ls;
-    for (int e = 0; e < 4; ++e)
-      if (d0 + e < D) y[e] += f * po[at * D + d0 + e];
+  __shared__ float part[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+  const bool live = row < rows;
+  float m = -INFINITY, l = 0.f;
+  float y[4] = {0.f, 0.f, 0.f, 0.f};
+  const int d0 = lane;                                    // dims lane, + 64, ..
+  for (int s0 = 0; live && s0 < splits; s0 += 64) {
+    const int s = s0 + lane;
+    float ms = -INFINITY, ls = 0.f;
+    if (s < splits) {
+      const float* p = ml + 2 * ((int64_t)s * rows + row);
+      ms = p[0];
+      ls = p[1];
+    }
+    const bool use = ls != 0.f;
+    const float mn = fmaxf(m, wave_max(use ? ms : -INFINITY));
+    const float old = m == mn ? 1.f : exp2f(m - mn);
+    const float f = use ? exp2f(ms - mn) : 0.f;
+    l = l * old + wave_sum(use ? f * ls : 0.f);
+    m = mn;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) y[c] *= old;
+    part[wave][lane] = use ? f : 0.f;
+    const uint64_t on = __ballot(use);
+    const int top = on == 0 ? 0 : 64 - __builtin_clzll(on);
+    const float* o = po + ((int64_t)s0 * rows + row) * D;
+    for (int i = 0; i < top; i += 8) {
+      float x[8][4];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          x[j][c] = i + j < top && ((on >> (i + j)) & 1) && d0 + 64 * c < D
+                        ? o[(int64_t)(i + j) * rows * D + d0 + 64 * c] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (i + j < 64) y[c] += x[j][c] * part[wave][i + j];
+    }
   }
-  for (int e = 0; e < 4; ++e)
-    if (d0 + e < D) out[row * D + d0 + e] = from_f32<T>(l == 0.f ? 0.f : y[e] / l);
+  if (!live) return;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    if (d0 + 64 * c < D) out[row * D + d0 + 64 * c] = from_f32<T>(l == 0.f ? 0.f : y[c] / l);
 }
 
 template <typename T, int DP>
@@ -235,10 +263,10 @@ hipError_t launch_general(const HistArgs& a, hipStream_t s) {
 
 HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
   HistPlan p{};
-  p.rows = bf16 && (D == 64 || D == 128) ? 128 : kGenTile;
+  const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
+  p.rows = !(bf16 && (D == 64 || D == 128)) ? kGenTile : each <= 32 ? 32 : 128;
   // Splits: a history is cut where the tiles alone leave the chip idle, into
   // chunks of at least 256 keys, up to about two workgroups a CU.
-  const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
   const int64_t tiles = R * ((each + p.rows - 1) / p.rows) * Hk;
   int64_t splits = 512 / (tiles > 0 ? tiles : 1);
   if (splits > (max_len + 255) / 256) splits = (max_len + 255) / 256;
@@ -254,12 +282,12 @@ HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_le
 }
 
 hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s) {
-  hipError_t e = fast && rows == 128 ? launch_history_tile(a, s)
+  hipError_t e = fast && rows == 128  ? launch_history_tile(a, s)
+                 : fast && rows == 32 ? launch_history_split(a, s)
                  : bf16              ? launch_general<bf16_t>(a, s)
                                      : launch_general<float>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t threads = a.N * a.H * ((a.D + 3) / 4);
-  const int64_t blocks = (threads + 255) / 256;
+  const int64_t blocks = (a.N * a.H + 3) / 4;
   if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
   if (bf16)
     return launch_kernel(history_join<bf16_t>, dim3((uint32_t)blocks), dim3(256), s, a.part_ml,
