@@ -31,6 +31,7 @@ struct HistArgs {
   // History split over workgroups: `splits` chunks of `chunk` keys; partial
   // results per (split, row, head): {max (log2 units), sum} and the sums.
   int splits, chunk;
+  int heads;                // K/V heads a workgroup of the 32-row kernel: 1, 2 or 4
   float* part_ml;           // [splits][N * H][2]
   float* part_o;            // [splits][N * H][D]
 };
@@ -39,7 +40,7 @@ struct HistArgs {
 // follows from them.
 struct HistPlan {
   int rows;                 // query rows a workgroup: 128, 32 (MFMA) or 16 (general)
-  int splits, chunk;
+  int splits, chunk, heads;
   size_t ml_bytes, o_bytes; // of the workspace, 256-byte aligned
 };
 HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16);

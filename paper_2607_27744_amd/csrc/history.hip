@@ -181,62 +181,65 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
 
 // ---------------------------------------------------------------------------
 // Join of a split history: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.
-// A wave a row: lanes hold the parts' weights, then each lane adds four dims
-// (a lane group a part where a row has fewer than 256) of four parts at a time.
-// A part without a seen key has l = 0 and its O is not read. Bound by latency
-// for few rows, else by the read of the parts.
+// A workgroup a row: each wave forms all weights (a lane a part), then the
+// waves share the parts, eight in flight. A part without a seen key has l = 0
+// and no O; its loads are not skipped (a branch would put one latency after the
+// other) but dropped. Bound by latency for few rows, else by the read of the
+// parts.
 // ---------------------------------------------------------------------------
-template <typename T>
+constexpr int kMaxSplits = 256;
+
+template <typename T, int NC>              // NC: head_dim / 64, rounded up
 __global__ __launch_bounds__(256) void history_join(const float* __restrict__ ml,
                                                     const float* __restrict__ po,
                                                     T* __restrict__ out, int64_t rows, int D,
                                                     int splits) {
-  __shared__ float part[4][64];
+  constexpr int NS = kMaxSplits / 64;
+  __shared__ float weight[kMaxSplits], ysum[4][64 * NC];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
-  const bool live = row < rows;
-  float m = -INFINITY, l = 0.f;
-  float y[4] = {0.f, 0.f, 0.f, 0.f};
-  const int d0 = lane;                                    // dims lane, + 64, ..
-  for (int s0 = 0; live && s0 < splits; s0 += 64) {
-    const int s = s0 + lane;
-    float ms = -INFINITY, ls = 0.f;
-    if (s < splits) {
-      const float* p = ml + 2 * ((int64_t)s * rows + row);
-      ms = p[0];
-      ls = p[1];
-    }
-    const bool use = ls != 0.f;
-    const float mn = fmaxf(m, wave_max(use ? ms : -INFINITY));
-    const float old = m == mn ? 1.f : exp2f(m - mn);
-    const float f = use ? exp2f(ms - mn) : 0.f;
-    l = l * old + wave_sum(use ? f * ls : 0.f);
-    m = mn;
+  const int64_t row = blockIdx.x;
+  float ms[NS], ls[NS], m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) y[c] *= old;
-    part[wave][lane] = use ? f : 0.f;
-    const uint64_t on = __ballot(use);
-    const int top = on == 0 ? 0 : 64 - __builtin_clzll(on);
-    const float* o = po + ((int64_t)s0 * rows + row) * D;
-    for (int i = 0; i < top; i += 8) {
-      float x[8][4];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          x[j][c] = i + j < top && ((on >> (i + j)) & 1) && d0 + 64 * c < D
-                        ? o[(int64_t)(i + j) * rows * D + d0 + 64 * c] : 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (i + j < 64) y[c] += x[j][c] * part[wave][i + j];
-    }
+  for (int i = 0; i < NS; ++i) {
+    const int s = 64 * i + lane;
+    const float* p = ml + 2 * ((int64_t)min(s, splits - 1) * rows + row);
+    ms[i] = p[0];
+    ls[i] = s < splits ? p[1] : 0.f;
+    if (ls[i] != 0.f) m = fmaxf(m, ms[i]);
   }
-  if (!live) return;
+  m = wave_max(m);
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
-    if (d0 + 64 * c < D) out[row * D + d0 + 64 * c] = from_f32<T>(l == 0.f ? 0.f : y[c] / l);
+  for (int i = 0; i < NS; ++i) {
+    const float f = ls[i] != 0.f ? exp2f(ms[i] - m) : 0.f;
+    if (ls[i] != 0.f) l += f * ls[i];
+    if (wave == 0) weight[64 * i + lane] = ls[i] != 0.f ? f : -1.f;   // -1: no O
+  }
+  l = wave_sum(l);
+  __syncthreads();
+  float y[NC] = {};
+  for (int i = wave; i < splits; i += 32) {
+    float x[8][NC], f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int s = min(i + 4 * j, splits - 1);
+      f[j] = i + 4 * j < splits ? weight[s] : -1.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        x[j][c] = po[((int64_t)s * rows + row) * D + min(lane + 64 * c, D - 1)];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (!(f[j] < 0.f)) y[c] += x[j][c] * f[j];
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) ysum[wave][lane + 64 * c] = y[c];
+  __syncthreads();
+  for (int d = threadIdx.x; d < D; d += 256) {
+    const float t = (ysum[0][d] + ysum[1][d]) + (ysum[2][d] + ysum[3][d]);
+    out[row * D + d] = from_f32<T>(l == 0.f ? 0.f : t / l);
+  }
 }
 
 template <typename T, int DP>
@@ -259,17 +262,50 @@ hipError_t launch_general(const HistArgs& a, hipStream_t s) {
   return launch_general<T, 256>(a, s);
 }
 
+template <typename T>
+hipError_t launch_join(const HistArgs& a, hipStream_t s) {
+  const int64_t rows = a.N * a.H;
+  if (!grid_fits(rows, 256)) return hipErrorInvalidConfiguration;
+  return launch_kernel(a.D <= 64    ? history_join<T, 1>
+                       : a.D <= 128 ? history_join<T, 2>
+                                    : history_join<T, 4>,
+                       dim3((uint32_t)rows), dim3(256), s, a.part_ml, a.part_o,
+                       static_cast<T*>(a.out), rows, a.D, a.splits);
+}
+
 }  // namespace
 
 HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
   HistPlan p{};
   const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
   p.rows = !(bf16 && (D == 64 || D == 128)) ? kGenTile : each <= 32 ? 32 : 128;
-  // Splits: a history is cut where the tiles alone leave the chip idle, into
-  // chunks of at least 256 keys, up to about two workgroups a CU.
+  p.heads = 1;
   const int64_t tiles = R * ((each + p.rows - 1) / p.rows) * Hk;
-  int64_t splits = 512 / (tiles > 0 ? tiles : 1);
-  if (splits > (max_len + 255) / 256) splits = (max_len + 255) / 256;
+  const auto parts = [max_len](int64_t most, int64_t least_keys) {
+    const int64_t n = (max_len + least_keys - 1) / least_keys;
+    return n < most ? n : most;
+  };
+  // A history is cut where the tiles alone leave the chip idle: two workgroups a
+  // CU, chunks of at least 256 keys.
+  int64_t splits = parts(512 / tiles, 256);
+  if (p.rows == 32) {
+    // Few rows: a read of K and V. With two rounds of the chip in chunks of 512
+    // keys, a workgroup takes up to four heads and chunks are many, so that ragged
+    // histories end together (128 histories of 3,125 rows on average, 8 heads x
+    // 128: 301 us; a head a workgroup: 326; 40 of them: 95 and 126). With less,
+    // the waves of a head share its keys, which is fewer steps one after the
+    // other (one history of 16,384 rows: 18 us, by four heads 34).
+    const int hw = Hk % 4 == 0 ? 4 : Hk % 2 == 0 ? 2 : 1;
+    const int64_t wide = R * (Hk / hw);
+    if (wide * ((max_len + 511) / 512) >= 1024) {
+      p.heads = hw;
+      splits = parts(4096 / wide, 512);
+    } else {
+      const int64_t more = parts(2048 / tiles, 1024);
+      if (more > splits) splits = more;
+    }
+  }
+  if (splits > kMaxSplits) splits = kMaxSplits;
   if (splits < 1) splits = 1;
   p.chunk = (int)(((max_len + splits - 1) / splits + 63) / 64 * 64);
   p.splits = p.chunk > 0 ? (int)((max_len + p.chunk - 1) / p.chunk) : 1;
@@ -287,13 +323,7 @@ hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hip
                  : bf16              ? launch_general<bf16_t>(a, s)
                                      : launch_general<float>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t blocks = (a.N * a.H + 3) / 4;
-  if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-  if (bf16)
-    return launch_kernel(history_join<bf16_t>, dim3((uint32_t)blocks), dim3(256), s, a.part_ml,
-                         a.part_o, static_cast<bf16_t*>(a.out), a.N * a.H, a.D, a.splits);
-  return launch_kernel(history_join<float>, dim3((uint32_t)blocks), dim3(256), s, a.part_ml,
-                       a.part_o, static_cast<float*>(a.out), a.N * a.H, a.D, a.splits);
+  return bf16 ? launch_join<bf16_t>(a, s) : launch_join<float>(a, s);
 }
 
 }  // namespace rocs

@@ -49,6 +49,7 @@ int32_t attend(const char* name, HistArgs a, int64_t R, int64_t k_bytes, float s
   a.max_len = max_len;
   a.splits = p.splits;
   a.chunk = p.chunk;
+  a.heads = p.heads;
   a.part_ml = static_cast<float*>(workspace);
   a.part_o = need > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.ml_bytes)
                       : nullptr;

@@ -1,14 +1,19 @@
-// History attention, the bf16 kernel for few rows: 32 rows (token, head) of one
-// request and K/V head a workgroup, its four waves walking the keys in turn.
+// History attention, the bf16 kernel for few rows: 32 rows (token, head of the
+// group) of one request a wave.
 //
 // A single new event has as many rows as a K/V head has query heads, so one
-// tile holds them all and the call is a read of K and V. Each wave stages 32
-// keys of K and of V in LDS of its own by DMA (the next K under the softmax, the
-// next V under the next scores), so the waves run freely and two workgroups
-// share a CU (64 KiB of LDS at head_dim 128): up to 128 KiB a CU in flight. Long
+// tile holds them all and the call is a read of K and V. A workgroup's four
+// waves take up to four K/V heads of the same keys, which lie next to each
+// other in memory (with a head a workgroup, each 256 bytes of a row are read
+// from another XCD at another time: 128 ragged histories of 3,125 rows, 8
+// heads x 128, at 5.0 TB/s instead of MEASURED); what is left of the four shares
+// the keys in turn (HW heads x 4 / HW key ways). Each wave stages 32 keys of K
+// and of V in LDS of its own by DMA (the next K under the softmax, the next V
+// under the next scores), so the waves run freely and two workgroups share a
+// CU (64 KiB of LDS at head_dim 128): up to 128 KiB a CU in flight. Long
 // histories are cut over workgroups as well (HistArgs::splits). Scores, masks
-// and the running max are those of history_tile; the waves' partial softmaxes
-// meet in LDS at the end.
+// and the running max are those of history_tile; the partial softmaxes of one
+// head's waves meet in LDS at the end.
 // What bounds it: HBM with many or long histories, otherwise the latency of a
 // wave's chain of stages.
 #include "history_mfma.h"
@@ -34,19 +39,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   __shared__ __attribute__((aligned(1024))) char lds[kWaves * 2 * STAGE];
   __shared__ __attribute__((aligned(16))) int32_t doc_ids[DOCS ? kWaves * 2 * 64 : 4];
   __shared__ float pm[kWaves][kRows], pl[kWaves][kRows];
-  __shared__ int odd[kRows];
+  __shared__ int odd[kWaves][kRows];       // by head and row: to form again
   ROCS_LDS char* const lds3 = (ROCS_LDS char*)lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hh = lane >> 5;
-  const uint32_t work = xcd_remap(blockIdx.x, gridDim.x);
-  const uint32_t per_head = (uint32_t)slots * (uint32_t)a.splits;
-  const int hk = (int)(work / per_head);
-  const uint32_t rest = work - (uint32_t)hk * per_head;
+  // Neighbours in the work order, which run at the same time on different XCDs, are the
+  // head groups and parts of one history: they read neighbouring memory. Each
+  // eight are rotated against the eight before, so that no XCD gets only the
+  // last parts, which most histories do not reach.
+  const uint32_t b8 = blockIdx.x & ~7u;
+  const uint32_t work = b8 + 8 > gridDim.x ? blockIdx.x : b8 + ((blockIdx.x + (blockIdx.x >> 3)) & 7u);
+  const int HW = a.heads, KW = kWaves / HW;
+  const uint32_t groups_n = (uint32_t)(a.Hk / HW);
+  const int hk0 = (int)(work % groups_n) * HW, hk = hk0 + wave % HW;
+  const uint32_t rest = work / groups_n;
   const int split = (int)(rest % (uint32_t)a.splits);
   const HistTile t = hist_tile(a, slots - 1 - rest / (uint32_t)a.splits, kRows);
   if (t.rows <= 0) return;
-  if (tid < kRows) odd[tid] = 0;
+  if (tid < kWaves * kRows) odd[0][tid] = 0;
 
   const int row = t.row0 + min(l32, t.rows - 1);              // clamped; extra rows never stored
   const int token = row / a.G, head = hk * a.G + row % a.G;
@@ -63,12 +74,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   const int plain = DOCS ? 0 : (SCORE & kBias) != 0 ? min(lim_lo, position_of(t, first) + 1) : lim_lo;
   const int lo = split * a.chunk, hi = split_end(a, split, limit_of(a, t, last));
 
-  bf16x8 qf[KS];
-  {
-    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * D;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + 16 * ks + 8 * hh);
-  }
   const KeyFeed feed(a, t);
   const char* kbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + (int64_t)hk * D);
   const char* vbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + (int64_t)hk * D);
@@ -97,8 +102,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     if constexpr (DOCS) lds_dma4(a.kv_docs + t.kv0 + min(base + lane, hi - 1), ids0 + 256u * slot);
     issue(kbase, base, off, kdst);
   };
-  // The query rows resident before the first DMA load: from here on only those
-  // are in flight, which the waits below count.
+  int base = lo + kKeys * (wave / HW);
+  int64_t off[2];
+  if (base < hi) {
+    groups(base, off);
+    issue_k(base, off, 0);
+    issue(vbase, base, off, kdst + STAGE);
+  }
+  // The query rows, with the first stage in flight; resident before the loop,
+  // in which only DMA loads are in flight, which its waits count.
+  bf16x8 qf[KS];
+  {
+    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + 16 * ks + 8 * hh);
+  }
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) asm volatile("" :: "v"(as_u32x4(qf[ks])));
 
@@ -117,15 +135,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
 #pragma unroll
   for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
 
-  int base = lo + kKeys * wave;
-  int64_t off[2];
-  if (base < hi) {
-    groups(base, off);
-    issue_k(base, off, 0);
-    issue(vbase, base, off, kdst + STAGE);
-  }
-  for (int slot = 0; base < hi; base += kWaves * kKeys, slot ^= 1) {
-    const int next = base + kWaves * kKeys;
+  for (int slot = 0; base < hi; base += KW * kKeys, slot ^= 1) {
+    const int next = base + KW * kKeys;
     const bool more = next < hi;
     if (more) groups(next, off);
     wait_vmcnt<NI>();                                     // K of this stage (V may be in flight)
@@ -223,24 +234,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       *reinterpret_cast<ROCS_LDS f32x4*>(lds3 + kb0 + l32 * D * 4 + 16 * ((8 * db + 2 * q + hh) ^ (l32 & 15))) =
           f32x4{oacc[db][4 * q], oacc[db][4 * q + 1], oacc[db][4 * q + 2], oacc[db][4 * q + 3]};
   __syncthreads();
-  auto out_row = [&](int i) -> int64_t {
-    const int rw = t.row0 + i;
-    return (t.q0 + rw / a.G) * a.H + hk * a.G + rw % a.G;
-  };
-  for (int c = tid; c < t.rows * CF; c += 256) {
-    const int i = c / CF, piece = c % CF;
-    const float mx = fmaxf(fmaxf(pm[0][i], pm[1][i]), fmaxf(pm[2][i], pm[3][i]));
+  // Pieces of (head, row); the head's waves are hs, hs + HW, ..
+  for (int c = tid; c < HW * t.rows * CF; c += 256) {
+    const int piece = c % CF, i = c / CF % t.rows, hs = c / CF / t.rows;
+    float mx = pm[hs][i];
+    for (int w = hs + HW; w < kWaves; w += HW) mx = fmaxf(mx, pm[w][i]);
     const float ms = mx == -INFINITY ? 0.f : mx;
     float l = 0.f;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = hs; w < kWaves; w += HW) {
       const float f = exp2f(pm[w][i] - ms);
       l += pl[w][i] * f;
       y += *reinterpret_cast<const ROCS_LDS f32x4*>(lds3 + w * 2 * STAGE + i * D * 4 + 16 * (piece ^ (i & 15))) * f;
     }
-    if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3]))) odd[i] = 1;
-    const int64_t at = out_row(i);
+    if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3]))) odd[hs][i] = 1;
+    const int rw = t.row0 + i;
+    const int64_t at = (t.q0 + rw / a.G) * a.H + (hk0 + hs) * a.G + rw % a.G;
     if (a.splits > 1) {
       const int64_t to = (int64_t)split * a.N * a.H + at;
       if (piece == 0) {
@@ -255,9 +264,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     }
   }
   __syncthreads();
-  for (int i = wave; i < t.rows; i += kWaves)             // see lone_row
-    if (__builtin_amdgcn_readfirstlane(odd[i]) != 0)
-      redo_row<bf16_t>(a, t, t.row0 + i, hk, lo, hi, split);
+  for (int i = wave; i < HW * t.rows; i += kWaves)        // see lone_row
+    if (__builtin_amdgcn_readfirstlane(odd[i / t.rows][i % t.rows]) != 0)
+      redo_row<bf16_t>(a, t, t.row0 + i % t.rows, hk0 + i / t.rows, lo, hi, split);
 }
 
 template <int D, int SCORE>
@@ -279,7 +288,7 @@ hipError_t launch_dim(const HistArgs& a, int64_t slots, int64_t blocks, hipStrea
 
 hipError_t launch_history_split(const HistArgs& a, hipStream_t s) {
   const int64_t slots = a.R + (a.N * a.G + kRows - 1) / kRows;
-  const int64_t blocks = slots * a.Hk * a.splits;
+  const int64_t blocks = slots * (a.Hk / a.heads) * a.splits;
   if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
   return a.D == 128 ? launch_dim<128>(a, slots, blocks, s) : launch_dim<64>(a, slots, blocks, s);
 }
