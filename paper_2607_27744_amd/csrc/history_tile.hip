@@ -138,11 +138,15 @@ history_tile(const HistArgs a, int64_t slots) {
       if (listed) n = found;
     }
   }
-  auto stage_at = [&](int i) __attribute__((always_inline)) -> int {   // its first key
+  // First key of the i-th stage; mixed: keys of it may be of another document
+  // than rows of the tile.
+  auto stage_at = [&](int i, bool& mixed) __attribute__((always_inline)) -> int {
     if constexpr (DOCS) {
-      if (listed)
-        return lo + __builtin_amdgcn_readfirstlane(doc_list.entry[i] & (kMixed - 1)) * kStageKeys;
+      const int e = listed ? __builtin_amdgcn_readfirstlane((int)doc_list.entry[i]) : i;
+      mixed = !listed || (e & kMixed) != 0;
+      return lo + (listed ? e & (kMixed - 1) : i) * kStageKeys;
     }
+    mixed = false;
     return lo + i * kStageKeys;
   };
 
@@ -269,7 +273,8 @@ history_tile(const HistArgs a, int64_t slots) {
     // The stages at kt, kt + 1 and kt + 2 (first keys), and the group offsets
     // of the two that are still to be loaded; a stage's table entry is read a
     // step before its first load.
-    int b0 = stage_at(0), b1 = stage_at(min(1, n - 1)), b2 = stage_at(min(2, n - 1));
+    bool x0, x1, x2;
+    int b0 = stage_at(0, x0), b1 = stage_at(min(1, n - 1), x1), b2 = stage_at(min(2, n - 1), x2);
     const int64_t o0 = group_of(b0);
     int64_t o1 = group_of(b1), o2 = group_of(b2);
     issue_k(0, b0, o0);
@@ -297,9 +302,11 @@ history_tile(const HistArgs a, int64_t slots) {
     auto pass = [&](int kt) __attribute__((always_inline)) {
       b0 = b1;
       b1 = b2;
+      x0 = x1;
+      x1 = x2;
       o1 = o2;
       if (kt + 3 < n) {
-        b2 = stage_at(kt + 3);
+        b2 = stage_at(kt + 3, x2);
         o2 = group_of(b2);
       }
       wait_vmcnt<0>();
@@ -312,13 +319,9 @@ history_tile(const HistArgs a, int64_t slots) {
       pass(kt);
       ++kt;
     };
-    while (kt < free) {                                   // the score buffers swap roles
-      step(No{}, 0, s_a, s_b);
-      step(No{}, 1, s_b, s_a);
-    }
-    // Stages with a mask, one after the other: in step with the next stage's
-    // scores they would need more registers than there are.
-    while (kt < nw) {
+    // A stage with a mask, then the next scores: in step with them it would need
+    // more registers than there are.
+    auto masked = [&]() __attribute__((always_inline)) {
       const int slot = kt & 1;
       load(kt, slot);
       stage(Yes{}, No{}, slot, b0, s_a, s_a);
@@ -333,7 +336,28 @@ history_tile(const HistArgs a, int64_t slots) {
       }
       pass(kt);
       ++kt;
+    };
+    if constexpr (DOCS) {
+      // Packed documents: a document's first stages, its whole ones, the last.
+      auto whole = [&]() __attribute__((always_inline)) {
+        return kt + 2 < nw && !x0 && !x1 && b1 + kStageKeys <= plain;
+      };
+      // (With a bias at head_dim 128 both forms do not fit the registers.)
+      if constexpr (D == 64 || (SCORE & kBias) == 0) {
+        while (kt < nw && !whole()) masked();
+        while (whole()) {
+          const int slot = kt & 1;
+          step(No{}, slot, s_a, s_b);
+          step(No{}, slot ^ 1, s_b, s_a);
+        }
+      }
+    } else {
+      while (kt < free) {                                 // the score buffers swap roles
+        step(No{}, 0, s_a, s_b);
+        step(No{}, 1, s_b, s_a);
+      }
     }
+    while (kt < nw) masked();
     for (; kt < n; ++kt) {                                // the other waves' stages
       load(kt, kt & 1);
       pass(kt);
