@@ -47,11 +47,12 @@ __device__ __forceinline__ int block_scan(int v, int* part, int* total) {
   return before + incl - v;
 }
 
-// The first `want` pages with refs 0, in ascending order, into list; returns
-// how many there are (at most want). All threads call it.
-__device__ int free_pages(const int32_t* refs, int64_t P, int want, int32_t* list, int* part) {
+// The first `want` pages from page `from` on with refs 0, in ascending order,
+// into list; returns how many there are (at most want). All threads call it.
+__device__ int free_pages(const int32_t* refs, int64_t from, int64_t P, int want, int32_t* list,
+                          int* part) {
   int found = 0;
-  for (int64_t base = 0; base < P && found < want; base += 4 * kPlanThreads) {
+  for (int64_t base = from; base < P && found < want; base += 4 * kPlanThreads) {
     const int64_t p = base + 4 * threadIdx.x;
     bool free[4];
     int n = 0;
@@ -82,8 +83,9 @@ __device__ __forceinline__ int owner_in(const int* start, int n, int v) {
   return lo;
 }
 
-__device__ __forceinline__ int pages_of(int rows, int page) {
-  return (int)(((int64_t)rows + page - 1) / page);
+// rows and page below 2^31.
+__device__ __forceinline__ int pages_of(uint32_t rows, int page) {
+  return (int)((rows + (uint32_t)page - 1u) / (uint32_t)page);
 }
 
 // Sets slot s's bit; whether it was set before.
@@ -92,23 +94,43 @@ __device__ __forceinline__ bool take_bit(uint32_t* bits, int s) {
 }
 
 // ---------------------------------------------------------------------------
-// reserve, one workgroup. First a pass that checks every entry and adds up the
-// pages, then, if all is well, the free pages are listed and each handed to
-// its owner (found by binary search in the prefix sums in LDS). A page search
-// ends with the last page needed.
+// reserve, one workgroup. A pass over the entries checks them and adds up the
+// pages; if all is well the free pages are listed and each handed to its owner
+// (found by binary search in the prefix sums). A page search ends with the
+// last page needed. Bound by the chain of memory latencies: what the first
+// round needs (a thread's entry, the first 4096 reference counts) is in flight
+// from the start and stays in registers, what was found is in LDS.
 // ---------------------------------------------------------------------------
+constexpr int kPagesHere = 4 * kPlanThreads;     // pages of the first round
+
 __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
     const int32_t* __restrict__ slots, const int32_t* __restrict__ row_off, int n, int64_t M,
     int32_t* __restrict__ table, int64_t width, int32_t* __restrict__ lens, int S,
     int32_t* __restrict__ refs, int64_t P, int page, int32_t* __restrict__ rows,
     int32_t* __restrict__ status, int32_t* __restrict__ ws, int rows_here) {
   __shared__ uint32_t bits[kSlotWords];
-  __shared__ int upto[kSegment], old_len[kSegment], slot[kSegment];
+  __shared__ int upto[kSegment], start[kSegment + 1], old_len[kSegment], slot[kSegment];
+  __shared__ int found[kPagesHere];              // free pages of the first round
   __shared__ int part[kPlanThreads / 64];
   __shared__ int bad, wide;
   __shared__ unsigned long long wanted;
   const int tid = threadIdx.x;
-  int32_t* list = ws + kWsHead;
+  int32_t* list = ws + kWsHead;                  // free pages of later rounds
+  int first_free = 0;
+  bool open[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    open[i] = 4 * tid + i < P && refs[min((int64_t)(4 * tid + i), P - 1)] == 0;
+    first_free += open[i];
+  }
+  // The thread's first entry: slot, first row, rows, length.
+  int s0 = -1, r0 = 0, add0 = 0, l0 = 0;
+  if (tid < n) {
+    s0 = slots[tid];
+    r0 = row_off[tid];
+    add0 = max(row_off[tid + 1] - r0, 0);
+    if (s0 >= 0 && s0 < S) l0 = lens[s0];
+  }
   const int words = (S + 31) / 32;
   for (int i = tid; i < words; i += kPlanThreads) bits[i] = 0;
   if (tid == 0) {
@@ -119,19 +141,32 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
   // Pages wanted, and what is wrong.
   int64_t want = 0;
   for (int i = tid; i < n; i += kPlanThreads) {
-    const int s = slots[i], add = max(row_off[i + 1] - row_off[i], 0);
+    const int s = i == tid ? s0 : slots[i];
     if (s < 0 || s >= S || take_bit(bits, s)) {
       bad = 1;
       continue;
     }
-    const int64_t now = (int64_t)lens[s] + add;
-    if ((now + page - 1) / page > width) wide = 1;
-    want += (now + page - 1) / page - pages_of(lens[s], page);
+    const int l = i == tid ? l0 : lens[s], add = i == tid ? add0 : max(row_off[i + 1] - row_off[i], 0);
+    const int64_t now = pages_of((uint32_t)l + (uint32_t)add, page);
+    if (now > width) wide = 1;
+    want += now - pages_of(l, page);
   }
   if (want > 0) atomicAdd(&wanted, (unsigned long long)want);
   __syncthreads();
   const int total = (int)(wanted < 0x7fffffffull ? wanted : 0x7fffffffull);
-  const int have = bad || wide ? 0 : free_pages(refs, P, total, list, part);
+  int here = 0, have = 0;
+  if (!bad && !wide && total > 0) {
+    int sum;
+    int at = block_scan(first_free, part, &sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (open[i]) found[at] = 4 * tid + i;
+      at += open[i];
+    }
+    here = min(sum, total);
+    have = here;
+    if (here < total) have += free_pages(refs, kPagesHere, P, total - here, list, part);
+  }
   const bool good = !bad && !wide && have == total;
   if (tid == 0) {
     status[0] = bad ? 3 : wide ? 2 : good ? 0 : 1;
@@ -144,45 +179,50 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
     return;
   }
   int taken = 0;
+  auto page_at = [&](int k) { return taken + k < here ? found[taken + k] : list[taken + k - here]; };
   for (int i0 = 0; i0 < n; i0 += kSegment) {
     const int cnt = min(kSegment, n - i0);
     int run = 0;
     for (int i = tid; i < (cnt + kPlanThreads - 1) / kPlanThreads * kPlanThreads; i += kPlanThreads) {
-      int need = 0, s = 0, l = 0;
+      const bool one = i0 + i == tid;
+      int need = 0, s = 0, l = 0, r = 0;
       if (i < cnt) {
-        s = slots[i0 + i];
-        l = lens[s];
-        const int add = max(row_off[i0 + i + 1] - row_off[i0 + i], 0);
+        s = one ? s0 : slots[i0 + i];
+        r = one ? r0 : row_off[i0 + i];
+        const int add = one ? add0 : max(row_off[i0 + i + 1] - r, 0);
+        l = one ? l0 : lens[s];
         need = pages_of(l + add, page) - pages_of(l, page);
-        lens[s] = l + add;
+        if (add > 0) lens[s] = l + add;
+        if (i == cnt - 1) start[cnt] = r + add;
       }
       int sum;
       const int before = block_scan(need, part, &sum);
       if (i < cnt) {
         upto[i] = run + before;
+        start[i] = r;
         old_len[i] = l;
         slot[i] = s;
       }
       run += sum;
     }
-    __syncthreads();                                   // the list and the segment are complete
+    __syncthreads();                                   // the lists and the segment are complete
     for (int k = tid; k < run; k += kPlanThreads) {
       const int i = owner_in(upto, cnt, k);
-      const int p = list[taken + k];
+      const int p = page_at(k);
       table[(int64_t)slot[i] * width + pages_of(old_len[i], page) + (k - upto[i])] = p;
       refs[p] = 1;
     }
-    taken += run;
-    __syncthreads();                                   // the table's entries are visible
     if (rows_here) {
-      const int m0 = max(row_off[i0], 0), m1 = (int)min((int64_t)row_off[i0 + cnt], M);
-      for (int m = m0 + tid; m < m1; m += kPlanThreads) {
-        const int i = owner_in(row_off + i0, cnt, m);
-        const int at = old_len[i] + (m - row_off[i0 + i]);
-        rows[m] = table[(int64_t)slot[i] * width + at / page] * page + at % page;
+      const int m1 = (int)min((int64_t)start[cnt], M);
+      for (int m = max(start[0], 0) + tid; m < m1; m += kPlanThreads) {
+        const int i = owner_in(start, cnt, m);
+        const int at = old_len[i] + (m - start[i]), col = at / page, had = pages_of(old_len[i], page);
+        const int p = col < had ? table[(int64_t)slot[i] * width + col] : page_at(upto[i] + col - had);
+        rows[m] = p * page + at % page;
       }
     }
-    __syncthreads();
+    taken += run;
+    __syncthreads();                                   // the segment's arrays are free
   }
 }
 
@@ -325,7 +365,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(
     if (a >= 0 && a < S && ((bits[a >> 5] >> (a & 31)) & 1)) bad = 1;
   }
   __syncthreads();
-  const int have = bad ? 0 : free_pages(refs, P, total, list, part);
+  const int have = bad ? 0 : free_pages(refs, 0, P, total, list, part);
   const bool good = !bad && have == total;
   if (tid == 0) {
     status[0] = bad ? 3 : good ? 0 : 1;
