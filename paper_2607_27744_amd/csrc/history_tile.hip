@@ -185,77 +185,101 @@ history_tile(const HistArgs a, int64_t slots) {
       sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[w]), ones, sum, false);
     }
   };
-  // One stage: its weights and PV product, with the scores of the next one
-  // (NEXT) on the matrix cores meanwhile. GEN: masks and the general bias.
-  auto stage = [&](auto gen, auto next, int slot, int base, f32x16 (&s)[KB], f32x16 (&sn)[KB])
-      __attribute__((always_inline)) {
-    constexpr bool GEN = decltype(gen)::value, NEXT = decltype(next)::value;
-    if constexpr (NEXT) {
+  auto row_max = [&](const f32x16& s) __attribute__((always_inline)) {
+    float mx = s[0];
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) sn[kb] = f32x16{};
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    return mx;
+  };
+  // The stage's weights could pass 2^64 (or are not finite): the running max of the
+  // rows that need it moves to mx, and what has been summed is rescaled.
+  auto move_max = [&](float mx) __attribute__((always_inline)) {
+    const bool need = mx > m_run + kLazyMove;
+    const float alpha = need ? exp2f(m_run - mx) : 1.0f;       // 0 for a row's first keys
+    if (need) m_run = mx;
+    l_part *= alpha;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+    return m_run == -INFINITY ? 0.f : m_run;                   // no key seen yet: weights 0
+  };
+  auto pv_step = [&](int slot, int ps, const uint32_t (&pk)[4]) __attribute__((always_inline)) {
+    const bf16x8 pf = as_bf16x8(u32x4{pk[0], pk[1], pk[2], pk[3]});
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const uint32_t off = slot * STAGE + ps * 16 * ROWB;
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (ROCS_LDS i16x4*)(lds3 + ((va0[0] ^ (64u * db)) + off))));
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (ROCS_LDS i16x4*)(lds3 + ((va0[1] ^ (64u * db)) + off))));
+      oacc[db] = mfma32(as_bf16x8(u32x4{x[0], x[1], y[0], y[1]}), pf, oacc[db]);
     }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // A stage that every row of the wave sees whole: its weights and PV product,
+  // with the scores of the next stage on the matrix cores meanwhile.
+  auto stage = [&](int slot, int base, f32x16 (&s)[KB], f32x16 (&sn)[KB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) sn[kb] = f32x16{};
     uint32_t pk[PS][4];
     float sum = 0.f;
-    const ROCS_LDS int32_t* ids = (const ROCS_LDS int32_t*)doc_ids + (DOCS ? kStageKeys * slot : 0);
 #pragma unroll
     for (int ps = 0; ps < PS; ++ps) {
-      if constexpr (NEXT) {
 #pragma unroll
-        for (int ks = KS / PS * ps; ks < KS / PS * (ps + 1); ++ks) qk_step(slot ^ 1, ks, sn);
-      }
-      if constexpr (GEN) {
-        score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
-        mask_step<DOCS>(s[ps / 2], ps / 2, ps % 2, rule, base, hh, ids);
-      }
-      weights(gen, s, ps, base, m_run, pk[ps], sum);
-      if constexpr (D == 64 || GEN) __builtin_amdgcn_sched_barrier(0);
+      for (int ks = KS / PS * ps; ks < KS / PS * (ps + 1); ++ks) qk_step(slot ^ 1, ks, sn);
+      weights(std::false_type{}, s, ps, base, m_run, pk[ps], sum);
+      if constexpr (D == 64) __builtin_amdgcn_sched_barrier(0);
     }
     if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
-      if constexpr (!GEN) {
 #pragma unroll
-        for (int ps = 0; ps < PS; ++ps) score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
-      mx = max_across_halves(mx);
-      const bool need = mx > m_run + kLazyMove;
-      const float alpha = need ? exp2f(m_run - mx) : 1.0f;     // 0 for a row's first keys
-      if (need) m_run = mx;
-      l_part *= alpha;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+      for (int ps = 0; ps < PS; ++ps) score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
+      const float ms = move_max(max_across_halves(fmaxf(row_max(s[0]), row_max(s[1]))));
       sum = 0.f;
-      const float ms = m_run == -INFINITY ? 0.f : m_run;       // no key seen yet: weights 0
 #pragma unroll
       for (int ps = 0; ps < PS; ++ps) weights(std::true_type{}, s, ps, base, ms, pk[ps], sum);
     }
     l_part += sum;
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int ps = 0; ps < PS; ++ps) {
-      const bf16x8 pf = as_bf16x8(u32x4{pk[ps][0], pk[ps][1], pk[ps][2], pk[ps][3]});
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const uint32_t off = slot * STAGE + ps * 16 * ROWB;
-        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (ROCS_LDS i16x4*)(lds3 + ((va0[0] ^ (64u * db)) + off))));
-        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (ROCS_LDS i16x4*)(lds3 + ((va0[1] ^ (64u * db)) + off))));
-        oacc[db] = mfma32(as_bf16x8(u32x4{x[0], x[1], y[0], y[1]}), pf, oacc[db]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int ps = 0; ps < PS; ++ps) pv_step(slot, ps, pk[ps]);
     __builtin_amdgcn_s_setprio(0);
+  };
+  // Half a stage (32 keys) of any other kind: the mask, where rows without a max
+  // so far take theirs before the weights, and no work for keys that no row sees.
+  auto half = [&](int slot, int base, int kb, f32x16 (&s)[KB]) __attribute__((always_inline)) {
+    const int key = base + 32 * kb;
+    if (key >= lim_hi) return;
+    const ROCS_LDS int32_t* ids = (const ROCS_LDS int32_t*)doc_ids + (DOCS ? kStageKeys * slot : 0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) score_step<SCORE>(s[kb], kb, h, rule, base, hh);
+    if (DOCS || key + 32 > lim_lo) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) mask_step<DOCS>(s[kb], kb, h, rule, base, hh, ids);
+    }
+    float ms = m_run;
+    if (__ballot(m_run == -INFINITY) != 0) {
+      const float mx = max_across_halves(row_max(s[kb]));
+      if (m_run == -INFINITY) m_run = mx;                      // nothing summed yet
+      ms = m_run == -INFINITY ? 0.f : m_run;
+    }
+    uint32_t pk[2][4];
+    float sum = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) weights(std::true_type{}, s, 2 * kb + h, base, ms, pk[h], sum);
+    if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
+      ms = move_max(max_across_halves(row_max(s[kb])));
+      sum = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) weights(std::true_type{}, s, 2 * kb + h, base, ms, pk[h], sum);
+    }
+    if (DOCS && __ballot(sum != 0.f) == 0) return;
+    l_part += sum;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) pv_step(slot, 2 * kb + h, pk[h]);
   };
 
   if (n > 0) {
-    using Yes = std::true_type;
-    using No = std::false_type;
-    // The wave's own stages, and how many of them (an even number, each with a
-    // stage after it) need no mask.
+    // The wave's own stages, and how many of them (each with a stage after it)
+    // need no mask.
     int nw = 0, free = 0;
     if constexpr (DOCS) {
       if (listed) {
@@ -267,7 +291,7 @@ history_tile(const HistArgs a, int64_t slots) {
       }
     } else {
       nw = max(min(n, (lim_hi - lo + kStageKeys - 1) / kStageKeys), 0);
-      free = max(min((plain - lo) / kStageKeys, nw - 1), 0) & ~1;
+      free = max(min((plain - lo) / kStageKeys, nw - 1), 0);
     }
     nw = __builtin_amdgcn_readfirstlane(nw);
     // The stages at kt, kt + 1 and kt + 2 (first keys), and the group offsets
@@ -313,9 +337,9 @@ history_tile(const HistArgs a, int64_t slots) {
       ring_barrier();
     };
     int kt = 0;
-    auto step = [&](auto gen, int slot, f32x16 (&cur)[KB], f32x16 (&nxt)[KB]) __attribute__((always_inline)) {
+    auto step = [&](int slot, f32x16 (&cur)[KB], f32x16 (&nxt)[KB]) __attribute__((always_inline)) {
       load(kt, slot);
-      stage(gen, Yes{}, slot, b0, cur, nxt);
+      stage(slot, b0, cur, nxt);
       pass(kt);
       ++kt;
     };
@@ -324,7 +348,8 @@ history_tile(const HistArgs a, int64_t slots) {
     auto masked = [&]() __attribute__((always_inline)) {
       const int slot = kt & 1;
       load(kt, slot);
-      stage(Yes{}, No{}, slot, b0, s_a, s_a);
+      half(slot, b0, 0, s_a);
+      half(slot, b0, 1, s_a);
       if (kt + 1 < nw) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) s_a[kb] = f32x16{};
@@ -339,22 +364,24 @@ history_tile(const HistArgs a, int64_t slots) {
     };
     if constexpr (DOCS) {
       // Packed documents: a document's first stages, its whole ones, the last.
-      auto whole = [&]() __attribute__((always_inline)) {
-        return kt + 2 < nw && !x0 && !x1 && b1 + kStageKeys <= plain;
-      };
       // (With a bias at head_dim 128 both forms do not fit the registers.)
       if constexpr (D == 64 || (SCORE & kBias) == 0) {
+        auto whole = [&]() __attribute__((always_inline)) {
+          return kt + 2 < nw && !x0 && !x1 && b1 + kStageKeys <= plain;
+        };
         while (kt < nw && !whole()) masked();
         while (whole()) {
           const int slot = kt & 1;
-          step(No{}, slot, s_a, s_b);
-          step(No{}, slot ^ 1, s_b, s_a);
+          step(slot, s_a, s_b);
+          step(slot ^ 1, s_b, s_a);
         }
       }
     } else {
-      while (kt < free) {                                 // the score buffers swap roles
-        step(No{}, 0, s_a, s_b);
-        step(No{}, 1, s_b, s_a);
+      // The first stage finds the rows' max before its weights, as masked ones do.
+      if (nw > 0) masked();
+      while (kt + 1 < free) {                             // the score buffers swap roles
+        step(1, s_a, s_b);
+        step(0, s_b, s_a);
       }
     }
     while (kt < nw) masked();
