@@ -67,6 +67,8 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
   const int lo = split * a.chunk;
   const int most = limit_of(a, t, (t.row0 + t.rows - 1) / a.G);    // the tile's last row sees most
   const int hi = split_end(a, split, most);
+  const bool alone = tile_alone(a, most), direct = a.splits == 1 || alone;
+  if (alone && split > 0) return;
   const T* q = static_cast<const T*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)h * D;
   const T* k = static_cast<const T*>(a.k) + (int64_t)hk * D;
   const T* v = static_cast<const T*>(a.v) + (int64_t)hk * D;
@@ -158,11 +160,11 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
     if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3]))) odd[i] = 1;
     const int rw = t.row0 + i;
     const int64_t at = (t.q0 + rw / a.G) * a.H + hk * a.G + rw % a.G;
-    if (a.splits > 1) {
-      if (d0 == 0) {
-        a.part_ml[2 * (part0 + at)] = mx * kLog2e;
-        a.part_ml[2 * (part0 + at) + 1] = l;
-      }
+    if (a.splits > 1 && d0 == 0) {
+      a.part_ml[2 * (part0 + at)] = mx * kLog2e;
+      a.part_ml[2 * (part0 + at) + 1] = alone ? kDone : l;
+    }
+    if (!direct) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (d0 + e < D && l != 0.f) a.part_o[(part0 + at) * D + d0 + e] = y[e];
@@ -176,28 +178,33 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
   __syncthreads();
   for (int i = wave; i < t.rows; i += 4)
     if (__builtin_amdgcn_readfirstlane(odd[i]) != 0)
-      redo_row<T>(a, t, t.row0 + i, hk, lo, hi, split);
+      redo_row<T>(a, t, t.row0 + i, hk, lo, hi, split, direct);
 }
 
 // ---------------------------------------------------------------------------
 // Join of a split history: out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.
-// A workgroup a row: each wave forms all weights (a lane a part), then the
-// waves share the parts, eight in flight. A part without a seen key has l = 0
-// and no O; its loads are not skipped (a branch would put one latency after the
-// other) but dropped. Bound by latency for few rows, else by the read of the
-// parts.
+// W waves a row (four for few rows, else one): each forms all weights (a lane a
+// part), then they share the parts, eight in flight. A part without a seen key
+// has l = 0 and no O; its loads are not skipped (a branch would put one latency
+// after the other) but dropped. Rows that are done already (kDone) are left.
+// Bound by latency for few rows, else by the read of the parts.
 // ---------------------------------------------------------------------------
 constexpr int kMaxSplits = 256;
 
-template <typename T, int NC>              // NC: head_dim / 64, rounded up
+template <typename T, int NC, int W>       // NC: head_dim / 64, rounded up
 __global__ __launch_bounds__(256) void history_join(const float* __restrict__ ml,
                                                     const float* __restrict__ po,
-                                                    T* __restrict__ out, int64_t rows, int D,
+                                                    const int32_t* __restrict__ q_end,
+                                                    T* __restrict__ out, int64_t rows, int H, int D,
                                                     int splits) {
   constexpr int NS = kMaxSplits / 64;
-  __shared__ float weight[kMaxSplits], ysum[4][64 * NC];
+  __shared__ float weight[4][kMaxSplits], ysum[4][64 * NC];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = blockIdx.x;
+  const int64_t row = W == 4 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
+  // Rows behind the last request have no parts and stay as they are. (Uniform
+  // over the row's waves.)
+  if (row >= rows || row >= (int64_t)*q_end * H || ml[2 * row + 1] == kDone) return;
+  const int first = W == 4 ? wave : 0;
   float ms[NS], ls[NS], m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int i = 0; i < NS; ++i) {
@@ -212,17 +219,16 @@ __global__ __launch_bounds__(256) void history_join(const float* __restrict__ ml
   for (int i = 0; i < NS; ++i) {
     const float f = ls[i] != 0.f ? exp2f(ms[i] - m) : 0.f;
     if (ls[i] != 0.f) l += f * ls[i];
-    if (wave == 0) weight[64 * i + lane] = ls[i] != 0.f ? f : -1.f;   // -1: no O
+    weight[wave][64 * i + lane] = ls[i] != 0.f ? f : -1.f;     // -1: no O
   }
   l = wave_sum(l);
-  __syncthreads();
   float y[NC] = {};
-  for (int i = wave; i < splits; i += 32) {
+  for (int i = first; i < splits; i += 8 * W) {
     float x[8][NC], f[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int s = min(i + 4 * j, splits - 1);
-      f[j] = i + 4 * j < splits ? weight[s] : -1.f;
+      const int s = min(i + W * j, splits - 1);
+      f[j] = i + W * j < splits ? weight[wave][s] : -1.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         x[j][c] = po[((int64_t)s * rows + row) * D + min(lane + 64 * c, D - 1)];
@@ -233,12 +239,18 @@ __global__ __launch_bounds__(256) void history_join(const float* __restrict__ ml
       for (int c = 0; c < NC; ++c)
         if (!(f[j] < 0.f)) y[c] += x[j][c] * f[j];
   }
+  if constexpr (W == 4) {
 #pragma unroll
-  for (int c = 0; c < NC; ++c) ysum[wave][lane + 64 * c] = y[c];
-  __syncthreads();
-  for (int d = threadIdx.x; d < D; d += 256) {
-    const float t = (ysum[0][d] + ysum[1][d]) + (ysum[2][d] + ysum[3][d]);
-    out[row * D + d] = from_f32<T>(l == 0.f ? 0.f : t / l);
+    for (int c = 0; c < NC; ++c) ysum[wave][lane + 64 * c] = y[c];
+    __syncthreads();
+    for (int d = threadIdx.x; d < D; d += 256) {
+      const float t = (ysum[0][d] + ysum[1][d]) + (ysum[2][d] + ysum[3][d]);
+      out[row * D + d] = from_f32<T>(l == 0.f ? 0.f : t / l);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      if (lane + 64 * c < D) out[row * D + lane + 64 * c] = from_f32<T>(l == 0.f ? 0.f : y[c] / l);
   }
 }
 
@@ -262,15 +274,21 @@ hipError_t launch_general(const HistArgs& a, hipStream_t s) {
   return launch_general<T, 256>(a, s);
 }
 
-template <typename T>
+template <typename T, int NC>
 hipError_t launch_join(const HistArgs& a, hipStream_t s) {
   const int64_t rows = a.N * a.H;
-  if (!grid_fits(rows, 256)) return hipErrorInvalidConfiguration;
-  return launch_kernel(a.D <= 64    ? history_join<T, 1>
-                       : a.D <= 128 ? history_join<T, 2>
-                                    : history_join<T, 4>,
-                       dim3((uint32_t)rows), dim3(256), s, a.part_ml, a.part_o,
-                       static_cast<T*>(a.out), rows, a.D, a.splits);
+  const bool few = rows <= 2048;
+  const int64_t blocks = few ? rows : (rows + 3) / 4;
+  if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+  return launch_kernel(few ? history_join<T, NC, 4> : history_join<T, NC, 1>, dim3((uint32_t)blocks),
+                       dim3(256), s, a.part_ml, a.part_o, a.q_off + a.R, static_cast<T*>(a.out), rows,
+                       a.H, a.D, a.splits);
+}
+template <typename T>
+hipError_t launch_join(const HistArgs& a, hipStream_t s) {
+  return a.D <= 64    ? launch_join<T, 1>(a, s)
+         : a.D <= 128 ? launch_join<T, 2>(a, s)
+                      : launch_join<T, 4>(a, s);
 }
 
 }  // namespace
@@ -286,7 +304,9 @@ HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_le
     return n < most ? n : most;
   };
   // A history is cut where the tiles alone leave the chip idle: two workgroups a
-  // CU, chunks of at least 256 keys.
+  // CU, chunks of at least 256 keys. (More parts than that do not pay at 128 rows:
+  // chunks over six cached histories of 2,400 to 12,800 rows take 435 us in 504
+  // whole tiles, 520 in four parts.)
   int64_t splits = parts(512 / tiles, 256);
   if (p.rows == 32) {
     // Few rows: a read of K and V. With two rounds of the chip in chunks of 512

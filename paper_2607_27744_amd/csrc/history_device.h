@@ -57,6 +57,14 @@ __device__ __forceinline__ int split_end(const HistArgs& a, int split, int most)
   return (int)min((int64_t)(split + 1) * a.chunk, (int64_t)most);
 }
 
+// A tile of a split call whose rows see no key past the first part: that part's
+// workgroup writes the result itself and marks it (a sum of -1) for the join;
+// the others leave. So histories shorter than a part cost no partial results.
+__device__ __forceinline__ bool tile_alone(const HistArgs& a, int most) {
+  return a.splits > 1 && most <= a.chunk;
+}
+constexpr float kDone = -1.f;
+
 // Element offset of K/V row j (of all heads).
 __device__ __forceinline__ int64_t key_row(const HistArgs& a, const HistTile& t, int j) {
   if (t.pages == nullptr) return (t.kv0 + j) * a.kv_stride;
@@ -138,12 +146,12 @@ __device__ __forceinline__ void lone_row(const HistArgs& a, const HistTile& t, i
 // The lone row's result where the kernel's own would have gone.
 template <typename T>
 __device__ __forceinline__ void redo_row(const HistArgs& a, const HistTile& t, int row, int hk,
-                                         int lo, int hi, int split) {
+                                         int lo, int hi, int split, bool direct) {
   float m, l, acc[4];
   lone_row<T>(a, t, row, hk, lo, hi, m, l, acc);
   const int lane = (int)(threadIdx.x & 63);
   const int64_t at = (t.q0 + row / a.G) * a.H + hk * a.G + row % a.G;
-  if (a.splits > 1) {
+  if (!direct) {
     const int64_t to = (int64_t)split * a.N * a.H + at;
     if (lane == 0) {
       a.part_ml[2 * to] = m;

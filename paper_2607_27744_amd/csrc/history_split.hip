@@ -72,7 +72,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   const int first = t.row0 / a.G, last = (t.row0 + t.rows - 1) / a.G;
   const int lim_lo = limit_of(a, t, first);
   const int plain = DOCS ? 0 : (SCORE & kBias) != 0 ? min(lim_lo, position_of(t, first) + 1) : lim_lo;
-  const int lo = split * a.chunk, hi = split_end(a, split, limit_of(a, t, last));
+  const int most = limit_of(a, t, last);
+  const int lo = split * a.chunk, hi = split_end(a, split, most);
+  const bool alone = tile_alone(a, most), direct = a.splits == 1 || alone;
+  if (alone && split > 0) return;
 
   const KeyFeed feed(a, t);
   const char* kbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + (int64_t)hk * D);
@@ -250,12 +253,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3]))) odd[hs][i] = 1;
     const int rw = t.row0 + i;
     const int64_t at = (t.q0 + rw / a.G) * a.H + (hk0 + hs) * a.G + rw % a.G;
-    if (a.splits > 1) {
-      const int64_t to = (int64_t)split * a.N * a.H + at;
-      if (piece == 0) {
-        a.part_ml[2 * to] = mx;
-        a.part_ml[2 * to + 1] = l;
-      }
+    const int64_t to = (int64_t)split * a.N * a.H + at;
+    if (a.splits > 1 && piece == 0) {
+      a.part_ml[2 * to] = mx;
+      a.part_ml[2 * to + 1] = alone ? kDone : l;
+    }
+    if (!direct) {
       if (l != 0.f) *reinterpret_cast<f32x4*>(a.part_o + to * D + 4 * piece) = y;
     } else {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -266,7 +269,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   __syncthreads();
   for (int i = wave; i < HW * t.rows; i += kWaves)        // see lone_row
     if (__builtin_amdgcn_readfirstlane(odd[i / t.rows][i % t.rows]) != 0)
-      redo_row<bf16_t>(a, t, t.row0 + i % t.rows, hk0 + i / t.rows, lo, hi, split);
+      redo_row<bf16_t>(a, t, t.row0 + i % t.rows, hk0 + i / t.rows, lo, hi, split, direct);
 }
 
 template <int D, int SCORE>

@@ -70,6 +70,8 @@ history_tile(const HistArgs a, int64_t slots) {
   const int plain = (SCORE & kBias) != 0 ? min(lim_lo, position_of(t, first) + 1) : lim_lo;
   const int most = limit_of(a, t, (t.row0 + t.rows - 1) / a.G);
   const int lo = split * a.chunk, hi = split_end(a, split, most);
+  const bool alone = tile_alone(a, most), direct = a.splits == 1 || alone;
+  if (alone && split > 0) return;
 
   bf16x8 qf[KS];
   {
@@ -405,23 +407,22 @@ history_tile(const HistArgs a, int64_t slots) {
     const int rw = t.row0 + wrow0 + i;
     return (t.q0 + rw / a.G) * a.H + hk * a.G + rw % a.G;
   };
-  if (a.splits > 1) {
-    if (l32e < mine) {
-      const int64_t to = (int64_t)split * a.N * a.H + out_row(l32e);
-      if (hhe == 0) {
-        a.part_ml[2 * to] = m_run;
-        a.part_ml[2 * to + 1] = l;
-      }
-      if (l != 0.f) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<f32x4*>(a.part_o + to * D + 32 * db + 8 * q + 4 * hhe) =
-                f32x4{oacc[db][4 * q], oacc[db][4 * q + 1], oacc[db][4 * q + 2], oacc[db][4 * q + 3]};
-      }
+  if (a.splits > 1 && l32e < mine) {
+    const int64_t to = (int64_t)split * a.N * a.H + out_row(l32e);
+    if (hhe == 0) {
+      a.part_ml[2 * to] = m_run;
+      a.part_ml[2 * to + 1] = alone ? kDone : l;
     }
-  } else {
+    if (!direct && l != 0.f) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4*>(a.part_o + to * D + 32 * db + 8 * q + 4 * hhe) =
+              f32x4{oacc[db][4 * q], oacc[db][4 * q + 1], oacc[db][4 * q + 2], oacc[db][4 * q + 3]};
+    }
+  }
+  if (direct) {
     // Through this wave's share of the idle ring: row-contiguous stores.
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     const uint32_t obase = (uint32_t)(wave * 32 * ROWB);
@@ -454,7 +455,7 @@ history_tile(const HistArgs a, int64_t slots) {
   while (again != 0) {                                    // see lone_row
     const int i = __builtin_ctz(again);
     again &= again - 1;
-    redo_row<bf16_t>(a, t, t.row0 + wrow0 + i, hk, lo, hi, split);
+    redo_row<bf16_t>(a, t, t.row0 + wrow0 + i, hk, lo, hi, split, direct);
   }
 }
 

@@ -257,6 +257,21 @@ def test_rows_past_the_last_request_stay(gpu_lib):
         check(out[:80], *ref, 50, "bf16" if dtype == BF else "fp32")
 
 
+@pytest.mark.parametrize("dtype, d, rows", [(BF, 64, 1), (BF, 128, 90), (F32, 16, 3)])
+def test_rows_past_the_last_request_of_a_split_history(gpu_lib, dtype, d, rows):
+    # Long and short histories in one split call: partial results for some rows, the result at
+    # once for others, nothing for the rows of no request.
+    lens, new = [6000, 200, 9000], [rows, 1, rows]
+    q, k, v = _case(dtype, 4, 2, d, [sum(new) + 5], [sum(lens)], seed=6)
+    assert ops.history_workspace_size(3, sum(new) + 5, 4, 2, d, 9000, dtype) > 0
+    out = torch.full_like(q, 5.0)
+    ops.history_attention(q, k, v, _off(new), _off(lens), max_kv_len=9000, out=out)
+    n = sum(new)
+    assert bool((out[n:] == 5).all())
+    ref = oracle.attention(_np(q[:n]), _np(k), _np(v), new, lens)
+    check(out[:n], *ref, 9000, "bf16" if dtype == BF else "fp32")
+
+
 def test_bad_pages_and_slots_stay_inside(gpu_lib):
     # Ids out of range act as the last page or slot, lengths as the nearest possible one.
     q, k, v = _case(BF, 2, 2, 64, [1, 1], [40, 33])
