@@ -51,7 +51,7 @@ extern "C" {
  *                keys of its own document. Documents may come in any order;
  *                stretches of 64 keys without a document of the tile's rows
  *                are passed over, which is fast where documents are contiguous.
- *   slopes       [num_heads] fp32 or NULL;  cap >= 0 (0: none)
+ *   slopes       [num_heads] fp32 or NULL;  cap 0 (none) or at least 1e-30
  *   causal       0 or 1
  *   max_kv_len   an upper bound on every L_r, known on the host, or 0 for
  *                num_kv_rows: it only decides how a long history is split over
@@ -64,7 +64,7 @@ extern "C" {
  * Fast path (bf16 MFMA kernels): bf16, head_dim 64 or 128, strides multiples
  * of 8 elements, pointers 16-byte aligned (kv_docs 4). Other cases run a
  * general kernel (fp32 matrix instructions), head_dim up to 256.
- * Limits: N * num_heads < 2^31, num_heads < 2^16, num_kv_rows < 2^31.
+ * Limits: N * num_heads <= 2^30, num_heads < 2^16, num_kv_rows < 2^31.
  * ---------------------------------------------------------------------------
  */
 size_t rocs_history_workspace_size(int64_t num_requests, int64_t num_rows, int32_t num_heads,
@@ -156,7 +156,8 @@ size_t rocs_cache_workspace_size(int64_t entries, int64_t num_pages);
 /* Room for new rows: entry i adds row_offsets[i+1] - row_offsets[i] rows to
  * slot slots[i]. lens, page_table and refs follow; rows[m] (int32 [num_rows])
  * becomes the pool row (page * page_size + row in the page) of new row m, or
- * -1 where the call could not be done. workspace:
+ * -1 where the call could not be done and for rows past row_offsets[entries]
+ * (a batch padded to a fixed num_rows). workspace:
  * rocs_cache_workspace_size(entries, num_pages) bytes, 256-byte aligned. */
 int32_t rocs_cache_reserve(const int32_t* slots, const int32_t* row_offsets, int64_t entries,
                            int64_t num_rows, int32_t* page_table, int64_t table_width,

@@ -578,7 +578,7 @@ Rules rules(const Ten& q, const Ten& k, const Ten& v, const Ten& off, const Ten&
   need(!slopes || (slopes->scalar_type() == c10::kFloat && slopes->dim() == 1 &&
                    slopes->size(0) == h && slopes->is_contiguous()));
   x.cap = scale_of(cap);
-  need(x.cap >= 0.f && x.cap < 3.4e38f);
+  need(x.cap == 0.f || (x.cap >= 1e-30f && x.cap < 3.4e38f));
   x.causal = truth(causal);
   x.most = count_of(most);
   x.scale = scale_of(scale);

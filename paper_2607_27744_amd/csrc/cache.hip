@@ -221,6 +221,8 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
         rows[m] = p * page + at % page;
       }
     }
+    if (rows_here && i0 + cnt == n)                    // rows of no entry (a padded batch)
+      for (int64_t m = max(start[cnt], 0) + tid; m < M; m += kPlanThreads) rows[m] = -1;
     taken += run;
     __syncthreads();                                   // the segment's arrays are free
   }
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(256) void reserve_rows(
     int32_t* __restrict__ rows, const int32_t* __restrict__ ws) {
   const int64_t m = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (m >= M) return;
-  if (ws[0] == 0) {
+  if (ws[0] == 0 || m < row_off[0] || m >= row_off[n]) {
     rows[m] = -1;
     return;
   }

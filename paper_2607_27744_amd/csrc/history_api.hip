@@ -11,6 +11,9 @@ using namespace rocs;
 
 namespace {
 
+// Rows (token, head) of a call: their numbers, rounded up to a tile, stay in 32 bits.
+constexpr int64_t kMaxRows = int64_t(1) << 30;
+
 // The checks that both attentions share, and the launch.
 int32_t attend(const char* name, HistArgs a, int64_t R, int64_t k_bytes, float scale,
                int64_t max_len, int32_t dtype, void* workspace, size_t workspace_bytes,
@@ -74,10 +77,10 @@ int32_t check_call(const char* name, int64_t R, int64_t N, int32_t H, int32_t Hk
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: num_heads %d is no multiple of kv_heads %d", name, H, Hk);
   if (causal != 0 && causal != 1)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: causal must be 0 or 1", name);
-  if (!(cap >= 0.f) || cap > 3.4e38f)
-    return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: cap must be finite and not negative", name);
+  if (!(cap == 0.f || cap >= 1e-30f) || cap > 3.4e38f)
+    return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: cap must be 0, or finite and at least 1e-30", name);
   if (D > 256) return fail(ROCS_ERR_UNSUPPORTED, "%s: head_dim %d > 256", name, D);
-  if (R > kMaxI32 || N > kMaxI32 || H > 65535 || N * H > kMaxI32 || max_len > kMaxI32)
+  if (R > kMaxI32 || N > kMaxI32 || H > 65535 || N * H > kMaxRows || max_len > kMaxI32)
     return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
   if (q_stride != 0 && q_stride < (int64_t)H * D)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: q_row_stride < num_heads * head_dim", name);
@@ -138,7 +141,7 @@ extern "C" {
 size_t rocs_history_workspace_size(int64_t R, int64_t N, int32_t H, int32_t Hk, int32_t D,
                                    int64_t max_len, int32_t dtype) {
   if (R <= 0 || N <= 0 || H < 1 || Hk < 1 || H % Hk != 0 || D < 1 || D > 256 || max_len <= 0 ||
-      R > kMaxI32 || N > kMaxI32 || H > 65535 || N * H > kMaxI32 || max_len > kMaxI32 ||
+      R > kMaxI32 || N > kMaxI32 || H > 65535 || N * H > kMaxRows || max_len > kMaxI32 ||
       !valid_dtype(dtype))
     return 0;
   const HistPlan p = history_plan(R, N, H, Hk, D, max_len, dtype == ROCS_DTYPE_BF16);

@@ -5,9 +5,9 @@
 // tile holds them all and the call is a read of K and V. A workgroup's four
 // waves take up to four K/V heads of the same keys, which lie next to each
 // other in memory (with a head a workgroup, each 256 bytes of a row are read
-// from another XCD at another time: 128 ragged histories of 3,125 rows, 8
-// heads x 128, at 5.0 TB/s instead of MEASURED); what is left of the four shares
-// the keys in turn (HW heads x 4 / HW key ways). Each wave stages 32 keys of K
+// from another XCD at another time: 128 ragged histories of 3,125 rows on
+// average, 8 heads x 128, at 5.0 TB/s instead of 5.7); what is left of the four
+// shares the keys in turn (HW heads x 4 / HW key ways). Each wave stages 32 keys of K
 // and of V in LDS of its own by DMA (the next K under the softmax, the next V
 // under the next scores), so the waves run freely and two workgroups share a
 // CU (64 KiB of LDS at head_dim 128): up to 128 KiB a CU in flight. Long

@@ -825,7 +825,7 @@ def _score_rules(q, k, v, heads_of, prefix_lens, q_offsets, slopes, cap, causal,
           "slopes must be contiguous float32 [heads]")
     _need(causal in (True, False), "causal must be True or False")
     cap = float(cap or 0.0)
-    _need(0.0 <= cap < 3.4e38, "cap must be finite and not negative")
+    _need(cap == 0.0 or 1e-30 <= cap < 3.4e38, "cap must be 0, or finite and at least 1e-30")
     _need(max_kv_len is None or max_kv_len >= 0, "max_kv_len must not be negative")
     _need(out is None or (out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()),
           "out must be a contiguous [N, heads, d] tensor of q's dtype")
@@ -976,9 +976,9 @@ def _cache_status(status, device, stream):
 def cache_reserve(slots, row_offsets, num_rows, page_table, lens, refs, page_size, *, rows=None,
                   status=None, workspace=None, stream=None):
     """rocs_cache_reserve: entry i adds row_offsets[i + 1] - row_offsets[i] rows to slot slots[i]
-    (int32 [n], [n + 1]; num_rows = row_offsets[n]); lens, page_table and refs follow in place.
-    Returns (rows int32 [num_rows]: the pool row of each new row, for cache_write; status int32
-    [2], see cache_check). All or nothing: otherwise rows are -1 and the cache is unchanged."""
+    (int32 [n], [n + 1]; num_rows >= row_offsets[n]); lens, page_table and refs follow in place.
+    Returns (rows int32 [num_rows]: the pool row of each new row, for cache_write, -1 past
+    row_offsets[n]; status int32 [2], see cache_check). All or nothing: otherwise rows are -1 and the cache is unchanged."""
     done = (_binding or _native()).cache_reserve(slots, row_offsets, num_rows, page_table, lens,
                                                  refs, page_size, rows, status, workspace, stream)
     if done is not None:
@@ -988,7 +988,7 @@ def cache_reserve(slots, row_offsets, num_rows, page_table, lens, refs, page_siz
     _int_vector(slots, n, "slots")
     _offsets(row_offsets, n)
     _need(num_rows >= 0 and (n > 0 or num_rows == 0) and page_size >= 1,
-          "num_rows must be row_offsets' last entry, page_size at least 1")
+          "num_rows must not be negative (or without entries), page_size at least 1")
     _on_gpu(slots, row_offsets, page_table, lens, refs, rows, status)
     if rows is None:
         rows = _new(num_rows, torch.int32, slots.device, stream)

@@ -6,6 +6,9 @@ orientation; K and V projection weights of one layer stacked so both come out
 of one GEMM), and every output and workspace buffer preallocated. `step(p)`
 then enqueues one pass of the hot path on the current stream and allocates
 nothing. Host work here is argument marshalling only.
+
+`history_step` is a batch of ranking over histories that are kept, projected,
+in a paged cache between batches (`prepare_history_cache`).
 """
 
 from types import SimpleNamespace
@@ -215,3 +218,37 @@ def dca_layer_step(p):
 def dca_layer(w, device="cuda"):
     """prepare_dca_layer then one dca_layer_step."""
     return dca_layer_step(prepare_dca_layer(w, device))
+
+
+def prepare_history_cache(w, *, pages, page_size=64, table_width=64, slots=None, device="cuda"):
+    """Upload the weights of a `history_case` and make an empty cache for its histories: one
+    layer, `slots` histories (default: one per request) of up to table_width pages."""
+    dev = torch.device(device)
+    p = SimpleNamespace(h=w.heads, hk=w.kv_heads, d=w.head_dim, page=page_size,
+                        wkv=_bf16(w.wkv, dev), wq_s=_bf16(w.wq_s, dev), wq_c=_bf16(w.wq_c, dev),
+                        slopes=_f32(w.slopes, dev))
+    p.pool, p.table, p.lens, p.refs = ops.cache_pool(
+        1, pages, page_size, w.kv_heads, w.head_dim, slots=slots or w.n_req,
+        table_width=table_width, device=dev)
+    return p
+
+
+def history_step(p, slots, s_new, offsets, e_c, cand_offsets, max_kv_len=None):
+    """One batch of ranking over cached histories: request r is cache slot slots[r]. Its new
+    events s_new[offsets[r] ..] are projected to K/V once and appended to the slot's pages, attend
+    over the whole history (the request-side encoder: causal, weighted towards recent events),
+    and its candidates e_c[cand_offsets[r] ..] attend over all of it (DCA on the pages). Nothing
+    of the history is projected or copied again. Returns {"events", "candidates", "status"}; see
+    ops.cache_check for the status."""
+    m, n = s_new.shape[0], e_c.shape[0]
+    kv = ops.ikbo_linear(s_new, p.wkv)                      # [K | V], a cache row each
+    rows, status = ops.cache_reserve(slots, offsets, m, p.table, p.lens, p.refs, p.page)
+    ops.cache_write(kv, rows, p.pool[0])
+    k, v = p.pool[0, :, :, 0], p.pool[0, :, :, 1]
+    q_s = ops.ikbo_linear(s_new, p.wq_s).view(m, p.h, p.d)
+    q_c = ops.ikbo_linear(e_c, p.wq_c).view(n, p.h, p.d)
+    events = ops.paged_attention(q_s, k, v, p.table, p.lens, offsets, slots=slots,
+                                 slopes=p.slopes, max_kv_len=max_kv_len)
+    cands = ops.paged_attention(q_c, k, v, p.table, p.lens, cand_offsets, slots=slots,
+                                causal=False, max_kv_len=max_kv_len)
+    return {"events": events, "candidates": cands, "status": status}

@@ -36,6 +36,14 @@ line with the call's algorithmic FLOPs and bytes against the MI355X peaks.
   fm_linear         the interaction workload (128 requests x 512 candidates,
                     32 + 8 fields of width 128, FM then 1024 + 320 -> 512
                     ReLU) as one fused call, timed beside the two operators
+  history_attention causal attention of whole histories over themselves: 16
+                    requests x 2048 rows, 8 heads x 128, timed with capped
+                    scores too
+  paged_step        one new event of each of 128 users over paged histories of
+                    2048 rows, 8 heads x 128, pages of 64 rows
+  history_step      a batch of ranking over cached histories: append 4 events of
+                    each of 64 users, encode them, 200 candidates each over
+                    the pages (4 heads x 64, history 1024)
 """
 
 
@@ -50,7 +58,8 @@ PEAK_HBM_GBS = 8000.0
 
 NAMES = ("lcb", "dca_tq32", "dca_tq64", "dca_mapped", "dca_request", "linear_mapped",
          "linear_combined",
-         "glm_linear", "dca_layer", "mlp2", "fm_linear")
+         "glm_linear", "dca_layer", "mlp2", "fm_linear", "history_attention", "paged_step",
+         "history_step")
 
 
 def _bf16(a):
@@ -308,6 +317,74 @@ def _fm_linear(steps, warmup):
                  ms, flops, byts, "hbm", n, "candidates", {"two_operator_ms": round(ms_two, 4)})
 
 
+def _history_attention(steps, warmup):
+    r, length, h, d = 16, 2048, 8, 128
+    c = wl.attention_case([length] * r, [length] * r, h, d, seed=7)
+    q, k, v = _bf16(c.q).view(-1, h, d), _bf16(c.k), _bf16(c.v)
+    off = _i32(c.kv_offsets)
+    out = torch.empty_like(q)
+    ms = _time(lambda: ops.history_attention(q, k, v, off, off, max_kv_len=length, out=out),
+               steps, warmup)
+    ms_cap = _time(lambda: ops.history_attention(q, k, v, off, off, cap=30.0, max_kv_len=length,
+                                                 out=out), steps, warmup)
+    n = r * length
+    flops = 4.0 * h * d * r * length * (length + 1) / 2
+    return _line("history_attention", {"requests": r, "history": length, "heads": h,
+                                       "head_dim": d, "mask": "causal"},
+                 ms, flops, 2.0 * 4 * n * h * d, "mfma", n, "events",
+                 {"capped_ms": round(ms_cap, 4)})
+
+
+def _history_cache(r, length, new, steps_ahead, h, hk, d, page):
+    """A cache of r histories of `length` events, with room for the timed steps' events."""
+    from . import pipelines
+    w = wl.history_case([200] * r, [[length] * r, [new] * r], heads=h, kv_heads=hk, head_dim=d,
+                        seed=8)
+    width = -(-(length + new * steps_ahead) // page)
+    p = pipelines.prepare_history_cache(w, pages=r * width, page_size=page, table_width=width)
+    slots = _i32(np.random.default_rng(8).permutation(r))
+    first, b = w.batches
+    fill = pipelines.history_step(p, slots, _bf16(first.s), _i32(first.offsets), _bf16(first.e_c),
+                                  _i32(first.cand_offsets))
+    ops.cache_check(fill["status"])
+    return p, slots, (_bf16(b.s), _i32(b.offsets), _bf16(b.e_c), _i32(b.cand_offsets))
+
+
+def _paged_step(steps, warmup):
+    r, length, h, hk, d, page = 128, 2048, 8, 8, 128, 64
+    p, slots, (_, offsets, _, _) = _history_cache(r, length, 1, 1, h, hk, d, page)
+    q = torch.randn((r, h, d), device="cuda").to(torch.bfloat16)
+    out = torch.empty_like(q)
+    k, v = p.pool[0, :, :, 0], p.pool[0, :, :, 1]
+    ms = _time(lambda: ops.paged_attention(q, k, v, p.table, p.lens, offsets, slots=slots,
+                                           max_kv_len=length, out=out), steps, warmup)
+    return _line("paged_step", {"requests": r, "history": length, "heads": h, "kv_heads": hk,
+                                "head_dim": d, "page_size": page, "rows_per_request": 1},
+                 ms, 4.0 * r * length * h * d, 2.0 * (2 * r * length * hk * d + 2 * r * h * d),
+                 "hbm", r, "events")
+
+
+def _history_step(steps, warmup):
+    from . import pipelines
+    r, length, new, h, hk, d, page = 64, 1024, 4, 4, 4, 64, 64
+    p, slots, b = _history_cache(r, length, new, steps + warmup, h, hk, d, page)
+    last = {}
+
+    def step():
+        last.update(pipelines.history_step(p, slots, *b,
+                                           max_kv_len=length + new * (steps + warmup)))
+    ms = _time(step, steps, warmup)
+    ops.cache_check(last["status"])
+    n, d_seq = r * 200, 256
+    flops = (4.0 * (r * 200 + r * new) * length * h * d + 2.0 * n * d_seq * h * d
+             + 2.0 * r * new * d_seq * (h + 2 * hk) * d)
+    byts = 2.0 * (4 * r * length * hk * d + n * (d_seq + h * d))
+    return _line("history_step", {"requests": r, "candidates_per_request": 200,
+                                  "history": length, "new_events_per_request": new, "heads": h,
+                                  "head_dim": d, "page_size": page},
+                 ms, flops, byts, "mfma", n, "candidates")
+
+
 def run(name, steps=20, warmup=3):
     """Time one variant; returns its JSON-ready record."""
     ops.load_library()
@@ -333,4 +410,10 @@ def run(name, steps=20, warmup=3):
         return _mlp2(steps, warmup)
     if name == "fm_linear":
         return _fm_linear(steps, warmup)
+    if name == "history_attention":
+        return _history_attention(steps, warmup)
+    if name == "paged_step":
+        return _paged_step(steps, warmup)
+    if name == "history_step":
+        return _history_step(steps, warmup)
     raise ValueError(f"variant must be one of {NAMES}")

@@ -243,6 +243,29 @@ def dca_layer_case(counts, kv_lens, *, f_req=32, f_cand=16, o_req=32, o_cand=32,
 # The five benchmark workloads.
 # ---------------------------------------------------------------------------
 
+def history_case(counts, events, *, heads=4, kv_heads=2, head_dim=64, d_seq=256, seed=0,
+                 config_id=800):
+    """Ranking over cached histories: `events` is a list of batches, each the number of new events
+    per request (the histories grow by them), `counts` the candidates per request of every batch.
+    A list of batches of event features s [M, d_seq] and candidate features e_c [N, d_seq] with
+    their offsets, and the projections wkv [2 H_kv d, d_seq] (K rows, then V), wq_s and wq_c
+    [H d, d_seq]."""
+    rng = lambda t: tensor_rng(seed, config_id, t)   # noqa: E731
+    std = 1.0 / np.sqrt(d_seq)
+    batches = []
+    for b, new in enumerate(events):
+        off, co = offsets_from_counts(new), offsets_from_counts(counts)
+        batches.append(SimpleNamespace(
+            s=normal(rng(10 + 2 * b), (int(off[-1]), d_seq)), offsets=off,
+            e_c=normal(rng(11 + 2 * b), (int(co[-1]), d_seq)), cand_offsets=co))
+    return SimpleNamespace(
+        n_req=len(counts), heads=heads, kv_heads=kv_heads, head_dim=head_dim, batches=batches,
+        wkv=normal(rng(1), (2 * kv_heads * head_dim, d_seq), std),
+        wq_s=normal(rng(2), (heads * head_dim, d_seq), std),
+        wq_c=normal(rng(3), (heads * head_dim, d_seq), std),
+        slopes=np.float32(2.0) ** -np.arange(2, 2 + heads, dtype=np.float32))
+
+
 def _weights(seed, cid, tid, d_out, fan_in, bf16=True):
     return normal(tensor_rng(seed, cid, tid), (d_out, fan_in),
                   std=1.0 / np.sqrt(fan_in), bf16=bf16)

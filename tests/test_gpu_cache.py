@@ -159,6 +159,21 @@ def test_many_entries(gpu_lib):
     c.check()
 
 
+@pytest.mark.parametrize("entries, padded", [(3, 10), (5, 9000)])
+def test_a_padded_batch(gpu_lib, entries, padded):
+    # A fixed number of rows of which the last belong to no entry: they go nowhere.
+    pool, table, lens, refs = ops.cache_pool(1, 40, 4, 1, 8, slots=entries, table_width=8)
+    off = dev_i32(np.arange(entries + 1) + (np.arange(entries + 1) > 1))      # one has two rows
+    rows = torch.full((padded,), 7, dtype=torch.int32, device="cuda")
+    got, status = ops.cache_reserve(dev_i32(np.arange(entries)), off, padded, table, lens, refs, 4,
+                                    rows=rows)
+    assert got is rows and status.tolist() == [0, 0]
+    n = entries + 1
+    assert rows[:n].min() >= 0 and bool((rows[n:] == -1).all()) and int(lens.sum()) == n
+    ops.cache_write(torch.ones((padded, 16), dtype=torch.bfloat16, device="cuda"), rows, pool[0])
+    assert float(pool.float().sum()) == 16 * n
+
+
 def test_write_strided_and_missing_rows(gpu_lib):
     pool = torch.zeros((4, 8, 2, 1, 8), dtype=torch.bfloat16, device="cuda")
     for at, width in ((0, 40), (1, 19), (8, 24)):

@@ -55,6 +55,7 @@ def _packed(lib, **kw):
 @pytest.mark.parametrize("bad, status", [
     (dict(dtype=7), _lib.INVALID_ARGUMENT), (dict(Hk=3), _lib.INVALID_ARGUMENT),
     (dict(causal=2), _lib.INVALID_ARGUMENT), (dict(cap=-1.0), _lib.INVALID_ARGUMENT),
+    (dict(cap=1e-38), _lib.INVALID_ARGUMENT),
     (dict(cap=float("nan")), _lib.INVALID_ARGUMENT), (dict(cap=float("inf")), _lib.INVALID_ARGUMENT),
     (dict(D=257), _lib.UNSUPPORTED), (dict(N=1 << 30), _lib.UNSUPPORTED),
     (dict(qs=64), _lib.INVALID_ARGUMENT), (dict(ks=64), _lib.INVALID_ARGUMENT),
