@@ -61,9 +61,10 @@ extern "C" {
  *                kv_heads, head_dim, max_kv_len or num_kv_rows, dtype) bytes,
  *                256-byte aligned; may be NULL when that is 0. Scratch.
  *
- * Fast path (bf16 MFMA kernels): bf16, head_dim 64 or 128, strides multiples
- * of 8 elements, pointers 16-byte aligned (kv_docs 4). Other cases run a
- * general kernel (fp32 matrix instructions), head_dim up to 256.
+ * Fast path (bf16 MFMA kernels): bf16, head_dim a multiple of 8 up to 128
+ * (fastest at 64 and 128), strides multiples of 8 elements, pointers 16-byte
+ * aligned. Other cases run a general kernel (fp32 matrix instructions),
+ * head_dim up to 256.
  * Limits: N * num_heads <= 2^30, num_heads < 2^16, num_kv_rows < 2^31.
  * ---------------------------------------------------------------------------
  */

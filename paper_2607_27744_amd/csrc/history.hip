@@ -296,7 +296,7 @@ hipError_t launch_join(const HistArgs& a, hipStream_t s) {
 HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
   HistPlan p{};
   const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
-  p.rows = !(bf16 && (D == 64 || D == 128)) ? kGenTile : each <= 32 ? 32 : 128;
+  p.rows = !(bf16 && D % 8 == 0 && D <= 128) ? kGenTile : each <= 32 ? 32 : 128;
   p.heads = 1;
   const int64_t tiles = R * ((each + p.rows - 1) / p.rows) * Hk;
   const auto parts = [max_len](int64_t most, int64_t least_keys) {

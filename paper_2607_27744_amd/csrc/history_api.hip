@@ -56,7 +56,7 @@ int32_t attend(const char* name, HistArgs a, int64_t R, int64_t k_bytes, float s
   a.part_ml = static_cast<float*>(workspace);
   a.part_o = need > 0 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.ml_bytes)
                       : nullptr;
-  const bool fast = dtype == ROCS_DTYPE_BF16 && (a.D == 64 || a.D == 128) && a.q_stride % 8 == 0 &&
+  const bool fast = dtype == ROCS_DTYPE_BF16 && a.D % 8 == 0 && a.D <= 128 && a.q_stride % 8 == 0 &&
                     a.kv_stride % 8 == 0 && a.page_stride % 8 == 0 && aligned(a.q, 16) &&
                     aligned(a.k, 16) && aligned(a.v, 16) && aligned(a.out, 16) &&
                     (a.table == nullptr || a.page_size % 16 == 0) && a.kv_stride < (1 << 24);

@@ -34,7 +34,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   constexpr int STAGE = kKeys * ROWB;
   constexpr int KPI = 1024 / ROWB;        // rows of a DMA load
   constexpr int NI = kKeys / KPI;         // loads of a stage and operand
-  constexpr int CF = D / 4;               // 16-byte pieces of a partial output row
   static_assert(kRows * D * 4 <= 2 * STAGE, "a wave's partial output takes its staging");
   __shared__ __attribute__((aligned(1024))) char lds[kWaves * 2 * STAGE];
   __shared__ __attribute__((aligned(16))) int32_t doc_ids[DOCS ? kWaves * 2 * 64 : 4];
@@ -78,12 +77,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   if (alone && split > 0) return;
 
   const KeyFeed feed(a, t);
-  const char* kbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + (int64_t)hk * D);
-  const char* vbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + (int64_t)hk * D);
+  const char* kbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + (int64_t)hk * a.D);
+  const char* vbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + (int64_t)hk * a.D);
   const uint32_t kdst = lds_addr(lds) + (uint32_t)(wave * 2 * STAGE);
   const uint32_t ids0 = DOCS ? lds_addr(doc_ids) + (uint32_t)(wave * 2 * 64 * 4) : 0;
   // Load i of a stage fills rows KPI i + lane / CR (of group KPI i / 16), chunk
   // position lane % CR, with chunk (lane % CR) ^ kv_swizzle.
+  const int top = a.D / 8 - 1;            // the head's last chunk stands in past its end
   auto issue = [&](const char* src, int base, const int64_t (&off)[2], uint32_t dst) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
 #pragma unroll
       for (int i = 0; i < NI / 2; ++i) {
         const int r = KPI * i + lane / CR;
-        lds_dma16_sv(s, (uint32_t)(min(r, end) * feed.row_bytes) + 16u * (uint32_t)((lane % CR) ^ kv_swizzle<D>(r)),
+        lds_dma16_sv(s, (uint32_t)(min(r, end) * feed.row_bytes) + 16u * (uint32_t)min((lane % CR) ^ kv_swizzle<D>(r), top),
                      dst + 1024u * (NI / 2 * g + i));
       }
     }
@@ -116,9 +116,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   // in which only DMA loads are in flight, which its waits count.
   bf16x8 qf[KS];
   {
-    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * D;
+    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * a.D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + 16 * ks + 8 * hh);
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = as_bf16x8(load16(q + 16 * ks + 8 * hh, 16 * ks + 8 * hh < a.D));
   }
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) asm volatile("" :: "v"(as_u32x4(qf[ks])));
@@ -237,7 +237,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       *reinterpret_cast<ROCS_LDS f32x4*>(lds3 + kb0 + l32 * D * 4 + 16 * ((8 * db + 2 * q + hh) ^ (l32 & 15))) =
           f32x4{oacc[db][4 * q], oacc[db][4 * q + 1], oacc[db][4 * q + 2], oacc[db][4 * q + 3]};
   __syncthreads();
-  // Pieces of (head, row); the head's waves are hs, hs + HW, ..
+  // 16-byte pieces of (head, row); the head's waves are hs, hs + HW, ..
+  const int CF = a.D / 4;
   for (int c = tid; c < HW * t.rows * CF; c += 256) {
     const int piece = c % CF, i = c / CF % t.rows, hs = c / CF / t.rows;
     float mx = pm[hs][i];
@@ -259,10 +260,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       a.part_ml[2 * to + 1] = alone ? kDone : l;
     }
     if (!direct) {
-      if (l != 0.f) *reinterpret_cast<f32x4*>(a.part_o + to * D + 4 * piece) = y;
+      if (l != 0.f) *reinterpret_cast<f32x4*>(a.part_o + to * a.D + 4 * piece) = y;
     } else {
       const float inv = l == 0.f ? 0.f : 1.0f / l;
-      *reinterpret_cast<u32x2*>(static_cast<bf16_t*>(a.out) + at * D + 4 * piece) =
+      *reinterpret_cast<u32x2*>(static_cast<bf16_t*>(a.out) + at * a.D + 4 * piece) =
           u32x2{pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv)};
     }
   }
@@ -293,7 +294,7 @@ hipError_t launch_history_split(const HistArgs& a, hipStream_t s) {
   const int64_t slots = a.R + (a.N * a.G + kRows - 1) / kRows;
   const int64_t blocks = slots * (a.Hk / a.heads) * a.splits;
   if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-  return a.D == 128 ? launch_dim<128>(a, slots, blocks, s) : launch_dim<64>(a, slots, blocks, s);
+  return a.D > 64 ? launch_dim<128>(a, slots, blocks, s) : launch_dim<64>(a, slots, blocks, s);
 }
 
 }  // namespace rocs

@@ -16,6 +16,9 @@
 // (documents), so a row's max may stay -inf; its weights are then 0.
 // Work order. Under the causal mask a request's last tiles are the longest:
 // they come first, so that the launch does not end with them.
+// Head dims. D is 64 or 128; a head_dim below it (a multiple of 8) has zeros in
+// the query fragments' places past its end, its last 16 bytes once more in the
+// K/V stage's, and those columns of the result are not stored.
 // Grouped heads. Rows are (token, head of the group), so the heads of a group
 // share the K/V stage.
 #include "history_mfma.h"
@@ -75,14 +78,14 @@ history_tile(const HistArgs a, int64_t slots) {
 
   bf16x8 qf[KS];
   {
-    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * D;
+    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * a.D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + 16 * ks + 8 * hh);
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = as_bf16x8(load16(q + 16 * ks + 8 * hh, 16 * ks + 8 * hh < a.D));
   }
 
   const KeyFeed feed(a, t);
-  const char* kbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + (int64_t)hk * D);
-  const char* vbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + (int64_t)hk * D);
+  const char* kbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + (int64_t)hk * a.D);
+  const char* vbase = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + (int64_t)hk * a.D);
   // DMA lane map: load i of this wave's 16 rows of a stage fills rows KPI i +
   // lane / CR, chunk position lane % CR, with chunk (lane % CR) ^ kv_swizzle.
   int srow[NI];
@@ -90,7 +93,7 @@ history_tile(const HistArgs a, int64_t slots) {
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     srow[i] = KPI * i + lane / CR;
-    schunk[i] = 16u * (uint32_t)((lane % CR) ^ kv_swizzle<D>(srow[i]));
+    schunk[i] = 16u * (uint32_t)min((lane % CR) ^ kv_swizzle<D>(srow[i]), a.D / 8 - 1);
     soff[i] = (uint32_t)(srow[i] * feed.row_bytes) + schunk[i];
   }
   const uint32_t lds_base = lds_addr(lds);
@@ -418,8 +421,9 @@ history_tile(const HistArgs a, int64_t slots) {
       for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<f32x4*>(a.part_o + to * D + 32 * db + 8 * q + 4 * hhe) =
-              f32x4{oacc[db][4 * q], oacc[db][4 * q + 1], oacc[db][4 * q + 2], oacc[db][4 * q + 3]};
+          if (32 * db + 8 * q < a.D)
+            *reinterpret_cast<f32x4*>(a.part_o + to * a.D + 32 * db + 8 * q + 4 * hhe) =
+                f32x4{oacc[db][4 * q], oacc[db][4 * q + 1], oacc[db][4 * q + 2], oacc[db][4 * q + 3]};
     }
   }
   if (direct) {
@@ -448,8 +452,8 @@ history_tile(const HistArgs a, int64_t slots) {
       const int r = RPS * i + lane_e / CR;
       const u32x4 v = *reinterpret_cast<const ROCS_LDS u32x4*>(
           lds3 + obase + r * ROWB + 16 * ((lane_e % CR) ^ swz(r)));
-      if (r < mine)
-        *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.out) + out_row(r) * D + 8 * (lane_e % CR)) = v;
+      if (r < mine && lane_e % CR < a.D / 8)
+        *reinterpret_cast<u32x4*>(static_cast<bf16_t*>(a.out) + out_row(r) * a.D + 8 * (lane_e % CR)) = v;
     }
   }
   while (again != 0) {                                    // see lone_row
@@ -480,7 +484,7 @@ hipError_t launch_history_tile(const HistArgs& a, hipStream_t s) {
   const int64_t slots = a.R + (a.N * a.G + kRows - 1) / kRows;
   const int64_t blocks = slots * a.Hk * a.splits;
   if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-  return a.D == 128 ? launch_dim<128>(a, slots, blocks, s) : launch_dim<64>(a, slots, blocks, s);
+  return a.D > 64 ? launch_dim<128>(a, slots, blocks, s) : launch_dim<64>(a, slots, blocks, s);
 }
 
 }  // namespace rocs
