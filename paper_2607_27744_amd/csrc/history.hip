@@ -15,11 +15,16 @@ namespace {
 // through LDS. Scores and outputs run on the fp32 matrix instructions
 // (16x16x4; bf16 converts exactly): S^T = K Q^T leaves lane (l16, g) keys
 // 4 g .. + 3 of row l16, the B operand of O^T = V^T P^T as it stands. A score
-// is summed in 4 accumulators a 64 dims, added pairwise: shorter chains.
-// Loads are clamped into the history, never skipped, so they are in flight
-// together; a key that a row does not see gets the weight 0.
-// What bounds it: the latency of a wave's loads, and the fp32 matrix rate (an
-// eighth of bf16's) at long histories.
+// is summed in four chains, one for each of four neighbouring dims.
+// Rows of four aligned elements and head_dim up to 128 (PIPE): lane l16 takes
+// the NB dims from NB l16 of V^T, so that V comes in 16-byte loads as K does; a
+// block's V and the next one's K are in flight over its scores and weights, and
+// the next block's page numbers before them. Loads are clamped into the
+// history and the head, never skipped; what stands in past an end meets a
+// weight or a query of 0, or a column that is not stored.
+// What bounds it: HBM where rows are few (fp32, 64 rows over 2,048 keys each, 8
+// heads x 128: 277 us, 3.9 TB/s; 952 us with 4-byte V loads, one block at a time),
+// else the fp32 matrix rate, an eighth of bf16's.
 // ---------------------------------------------------------------------------
 constexpr int kGenTile = 16;
 
@@ -46,7 +51,7 @@ __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void history_general(
     const HistArgs a) {
   constexpr int NB = DP / 16;              // 16-dim blocks
-  constexpr int CB = sizeof(T) == 2 || DP == 32 ? 1 : DP == 64 ? 4 : 8;
+  constexpr bool PIPE = VEC && DP <= 128;
   constexpr int LP = DP + 4;               // LDS row (floats), padded against bank conflicts
   __shared__ __attribute__((aligned(16))) float po[4][kGenTile][LP];
   __shared__ float pm[4][kGenTile], pl[4][kGenTile];
@@ -79,27 +84,9 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
   f32x4 o[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int kb = lo + 16 * wave; kb < hi; kb += 64) {
-    const T* kr = k + key_row(a, t, min(kb + l16, hi - 1));
-    const T* vr[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) vr[i] = v + key_row(a, t, min(kb + 4 * g + i, hi - 1));
-    f32x4 part[CB][4] = {};
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const f32x4 kf = row4<T, VEC>(kr, 16 * b + 4 * g, D);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        part[b % CB][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i], qf[b][i], part[b % CB][i],
-                                                               0, 0, 0);
-    }
-#pragma unroll
-    for (int c = 1; c < CB; c *= 2)
-#pragma unroll
-      for (int b = 0; b + c < CB; b += 2 * c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) part[b][i] += part[b + c][i];
-    f32x4 s4 = (part[0][0] + part[0][1]) + (part[0][2] + part[0][3]);
+  // Scores of the block at kb in s4 -> weights in p, and the running max.
+  auto softmax = [&](int kb, const f32x4& dot, f32x4& p) __attribute__((always_inline)) {
+    f32x4 s4;
     bool seen[4];
     float mx = -INFINITY;
 #pragma unroll
@@ -107,7 +94,7 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
       const int j = kb + 4 * g + i;
       seen[i] = j < lim && j < hi;
       if (a.q_docs != nullptr) seen[i] = seen[i] && a.kv_docs[t.kv0 + min(j, hi - 1)] == doc;
-      float s = s4[i] * a.scale;
+      float s = dot[i] * a.scale;
       if (a.cap > 0.f) s = a.cap * tanhf(s / a.cap);
       if (a.slopes != nullptr) s -= slope * fabsf((float)(pos - j));
       s4[i] = seen[i] ? s : -INFINITY;
@@ -116,21 +103,86 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
     const float mn = fmaxf(m, max_across_rows(mx));
     const float ms = mn == -INFINITY ? 0.f : mn;         // no finite score yet: weights 0
     const float alpha = expf(m - ms);
-    f32x4 p;
 #pragma unroll
     for (int i = 0; i < 4; ++i) p[i] = seen[i] ? expf(s4[i] - ms) : 0.f;
     lsum = lsum * alpha + ((p[0] + p[1]) + (p[2] + p[3]));
     m = mn;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int dim = 16 * b + l16;
-      o[b] *= alpha;
+    for (int b = 0; b < NB; ++b) o[b] *= alpha;
+  };
+  if constexpr (PIPE) {
+    constexpr int NV = NB < 4 ? NB : 4;    // dims of one V load
+    auto key_at = [&](int j) __attribute__((always_inline)) { return key_row(a, t, min(j, hi - 1)); };
+    int64_t kr = 0, vr[4] = {};
+    f32x4 kf[NB];
+    auto load_k = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float vf = load_f32(vr[i] + min(dim, D - 1));
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(kb + 4 * g + i < hi && dim < D ? vf : 0.f,
-                                                    p[i], o[b], 0, 0, 0);
+      for (int b = 0; b < NB; ++b) kf[b] = load4_f32<T, true>(k + kr + min(16 * b + 4 * g, D - 4), 4);
+    };
+    const int first = lo + 16 * wave;
+    if (first < hi) {
+      kr = key_at(first + l16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vr[i] = key_at(first + 4 * g + i);
+      load_k();
+    }
+    for (int kb = first; kb < hi; kb += 64) {
+      float vv[4][NB];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < NB / NV; ++c) {
+          const T* src = v + vr[i] + min(NB * l16 + NV * c, D - NV);
+          if constexpr (NV == 4) {
+            const f32x4 x = load4_f32<T, true>(src, 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vv[i][4 * c + e] = x[e];
+          } else {
+#pragma unroll
+            for (int e = 0; e < NV; ++e) vv[i][NV * c + e] = load_f32(src + e);
+          }
+        }
+      kr = key_at(kb + 64 + l16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vr[i] = key_at(kb + 64 + 4 * g + i);
+      f32x4 part[4] = {};
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          part[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][i], qf[b][i], part[i], 0, 0, 0);
+      load_k();
+      f32x4 p;
+      softmax(kb, (part[0] + part[1]) + (part[2] + part[3]), p);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[i][b], p[i], o[b], 0, 0, 0);
+    }
+  } else {
+    for (int kb = lo + 16 * wave; kb < hi; kb += 64) {
+      const T* kr = k + key_row(a, t, min(kb + l16, hi - 1));
+      const T* vr[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vr[i] = v + key_row(a, t, min(kb + 4 * g + i, hi - 1));
+      f32x4 part[4] = {};
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const f32x4 kf = row4<T, VEC>(kr, 16 * b + 4 * g, D);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          part[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i], qf[b][i], part[i], 0, 0, 0);
       }
+      f32x4 p;
+      softmax(kb, (part[0] + part[1]) + (part[2] + part[3]), p);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float vf = load_f32(vr[i] + min(16 * b + l16, D - 1));
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(kb + 4 * g + i < hi ? vf : 0.f, p[i], o[b], 0, 0, 0);
+        }
     }
   }
   lsum = sum_across_rows(lsum);
@@ -138,9 +190,12 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
     pm[wave][l16] = m;
     pl[wave][l16] = lsum;
   }
+  // Element i of o[b] is dim 16 b + 4 g + i of row l16, or (PIPE) NB (4 g + i) + b.
 #pragma unroll
   for (int b = 0; b < NB; ++b)
-    *reinterpret_cast<f32x4*>(&po[wave][l16][16 * b + 4 * g]) = o[b];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      po[wave][l16][PIPE ? NB * (4 * g + i) + b : 16 * b + 4 * g + i] = o[b][i];
   __syncthreads();
   // Merge the four partial softmaxes, four dims a step.
   const int64_t part0 = (int64_t)split * a.N * a.H;
