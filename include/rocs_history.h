@@ -56,7 +56,8 @@ extern "C" {
  *   max_kv_len   an upper bound on every L_r, known on the host, or 0 for
  *                num_kv_rows: it only decides how a long history is split over
  *                workgroups (the results' fp32 sums follow that split)
- *   out          [N, num_heads, head_dim], dense, not overlapping an input
+ *   out          [N, num_heads, head_dim], dense, not overlapping an input;
+ *                rows past q_offsets[R] (a padded batch) stay as they are
  *   workspace    at least rocs_history_workspace_size(R, N, num_heads,
  *                kv_heads, head_dim, max_kv_len or num_kv_rows, dtype) bytes,
  *                256-byte aligned; may be NULL when that is 0. Scratch.
@@ -142,10 +143,13 @@ int32_t rocs_paged_attention(const void* q, int64_t q_row_stride, const void* k_
  *   ROCS_CACHE_TABLE_FULL  a slot would need more than table_width pages
  *   ROCS_CACHE_BAD_SLOT    a slot outside [0, num_slots), one named twice (as
  *                          an entry of reserve, or a child of fork), a child
- *                          that is not empty or that is a parent as well
+ *                          that is not empty or that is a parent as well, a
+ *                          slot whose length cannot be one
  * (the last cause in this list that holds). Nothing else is changed then.
  *
- * Limits: num_slots <= 2^18, num_pages * page_size < 2^31, table_width < 2^31.
+ * The lists of a call do not overlap the cache's arrays or its outputs.
+ * Limits: num_slots <= 2^18, entries <= 2^30 (free: < 2^24); num_pages *
+ * page_size and table_width * page_size < 2^31.
  * ---------------------------------------------------------------------------
  */
 #define ROCS_CACHE_NO_PAGES 1

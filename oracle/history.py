@@ -76,7 +76,8 @@ class Cache:
     def reserve(self, slots, counts):
         """(rows, status): the pool row of every new row."""
         total = sum(counts)
-        if any(not 0 <= s < len(self.lens) for s in slots) or len(set(slots)) < len(slots):
+        if (any(not 0 <= s < len(self.lens) or self.lens[s] < 0 for s in slots)
+                or len(set(slots)) < len(slots)):
             return [-1] * total, (3, 0)
         want = [-(-(self.lens[s] + c) // self.page) for s, c in zip(slots, counts)]
         if any(w > self.width for w in want):
@@ -104,7 +105,8 @@ class Cache:
         n = len(self.lens)
         if (any(not 0 <= s < n for s in list(parents) + list(children))
                 or len(set(children)) < len(children) or set(children) & set(parents)
-                or any(self.lens[c] for c in children)):
+                or any(self.lens[c] for c in children)
+                or any(not 0 <= self.lens[a] <= self.width * self.page for a in parents)):
             return 3, 0
         need = sum(self.lens[a] % self.page != 0 for a in parents)
         free = self._free()

@@ -146,7 +146,12 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
       bad = 1;
       continue;
     }
-    const int l = i == tid ? l0 : lens[s], add = i == tid ? add0 : max(row_off[i + 1] - row_off[i], 0);
+    const int l = i == tid ? l0 : lens[s];
+    if (l < 0) {                                       // no length: nothing to append to
+      bad = 1;
+      continue;
+    }
+    const int add = i == tid ? add0 : max(row_off[i + 1] - row_off[i], 0);
     const int64_t now = pages_of((uint32_t)l + (uint32_t)add, page);
     if (now > width) wide = 1;
     want += now - pages_of(l, page);
@@ -355,7 +360,8 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan(
   int mine = 0;
   for (int i = tid; i < n; i += kPlanThreads) {
     const int a = parents[i], c = children[i];
-    if (a < 0 || a >= S || c < 0 || c >= S || take_bit(bits, c) || lens[c] != 0)
+    if (a < 0 || a >= S || c < 0 || c >= S || take_bit(bits, c) || lens[c] != 0 ||
+        lens[a] < 0 || lens[a] > width * page)         // (no length: its pages are not in the table)
       bad = 1;
     else
       mine += lens[a] % page != 0;

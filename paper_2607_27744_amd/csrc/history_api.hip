@@ -4,6 +4,8 @@
 
 #include <math.h>
 
+#include <initializer_list>
+
 #include "history.h"
 #include "status.h"
 
@@ -15,8 +17,8 @@ namespace {
 constexpr int64_t kMaxRows = int64_t(1) << 30;
 
 // The checks that both attentions share, and the launch.
-int32_t attend(const char* name, HistArgs a, int64_t R, int64_t k_bytes, float scale,
-               int64_t max_len, int32_t dtype, void* workspace, size_t workspace_bytes,
+int32_t attend(const char* name, HistArgs a, int64_t R, int64_t kv_rows, int64_t k_bytes,
+               float scale, int64_t max_len, int32_t dtype, void* workspace, size_t workspace_bytes,
                void* stream) {
   const size_t es = esize(dtype);
   a.R = (int)R;
@@ -30,7 +32,7 @@ int32_t attend(const char* name, HistArgs a, int64_t R, int64_t k_bytes, float s
       {a.q_off, (size_t)(R + 1) * 4, "q_offsets"}, {a.kv_off, (size_t)(R + 1) * 4, "kv_offsets"},
       {a.table, (size_t)a.S * a.width * 4, "page_table"}, {a.lens, (size_t)a.S * 4, "kv_lens"},
       {a.slots, (size_t)R * 4, "slots"}, {a.prefix, (size_t)R * 4, "prefix_lens"},
-      {a.q_docs, (size_t)a.N * 4, "q_docs"}, {a.kv_docs, 4, "kv_docs"},
+      {a.q_docs, (size_t)a.N * 4, "q_docs"}, {a.kv_docs, (size_t)kv_rows * 4, "kv_docs"},
       {a.slopes, (size_t)a.H * 4, "slopes"}};
   const HistPlan p = history_plan(R, a.N, a.H, a.Hk, a.D, max_len, dtype == ROCS_DTYPE_BF16);
   const size_t need = p.ml_bytes + p.o_bytes;
@@ -93,14 +95,24 @@ int32_t check_call(const char* name, int64_t R, int64_t N, int32_t H, int32_t Hk
 const int32_t none_ = 0;
 const void* const kNone = &none_;
 
+// Entries of a call: the loops over them step by 4096 in 32 bits.
+constexpr int64_t kMaxEntries = int64_t(1) << 30;
+
 struct Cache {
   const void *table, *lens, *refs, *pool, *status, *ws;
   int64_t width, S, P, layers, row_bytes;
   int32_t page;
 };
 
-// Sizes and pointers of a page operator; `need` bytes of workspace.
-int32_t check_cache(const char* name, const Cache& c, size_t need, size_t have) {
+struct List {
+  const void* p;
+  int64_t n;               // int32 entries
+};
+
+// Sizes and pointers of a page operator; `need` bytes of workspace. lists: the
+// caller's other arrays.
+int32_t check_cache(const char* name, const Cache& c, std::initializer_list<List> lists,
+                    size_t need, size_t have) {
   if (c.width < 1 || c.S < 1 || c.P < 1 || c.page < 1)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: table_width, num_slots, num_pages and page_size "
                 "must be at least 1", name);
@@ -131,6 +143,11 @@ int32_t check_cache(const char* name, const Cache& c, size_t need, size_t have) 
       if (overlap(parts[i].p, parts[i].n, parts[j].p, parts[j].n))
         return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: the cache's arrays, status and workspace "
                     "must not overlap", name);
+  for (const List& l : lists)
+    for (const auto& part : parts)
+      if (overlap(l.p, (size_t)l.n * 4, part.p, part.n))
+        return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: a list of the call overlaps the cache's arrays, "
+                    "status or workspace", name);
   return ROCS_OK;
 }
 
@@ -177,8 +194,8 @@ int32_t rocs_history_attention(const void* q, int64_t q_row_stride, const void* 
   a.kv_stride = kv_row_stride != 0 ? kv_row_stride : (int64_t)Hk * D;
   const int64_t k_bytes =
       num_kv_rows > 0 ? ((num_kv_rows - 1) * a.kv_stride + (int64_t)Hk * D) * (int64_t)esize(dtype) : 0;
-  return attend(name, a, R, k_bytes, softmax_scale, max_kv_len > 0 ? max_kv_len : num_kv_rows,
-                dtype, workspace, workspace_bytes, stream);
+  return attend(name, a, R, num_kv_rows, k_bytes, softmax_scale,
+                max_kv_len > 0 ? max_kv_len : num_kv_rows, dtype, workspace, workspace_bytes, stream);
 }
 
 int32_t rocs_paged_attention(const void* q, int64_t q_row_stride, const void* k_pages,
@@ -224,13 +241,13 @@ int32_t rocs_paged_attention(const void* q, int64_t q_row_stride, const void* k_
   a.page_stride = page_stride != 0 ? page_stride : page_size * kv_stride;
   const int64_t k_bytes = ((num_pages - 1) * a.page_stride + extent) * (int64_t)esize(dtype);
   const int64_t bound = table_width * page_size;
-  return attend(name, a, R, k_bytes, softmax_scale,
+  return attend(name, a, R, 0, k_bytes, softmax_scale,
                 max_kv_len > 0 && max_kv_len < bound ? max_kv_len : bound, dtype, workspace,
                 workspace_bytes, stream);
 }
 
 size_t rocs_cache_workspace_size(int64_t entries, int64_t num_pages) {
-  if (entries < 0 || num_pages < 1 || entries > kMaxI32 || num_pages > kMaxI32) return 0;
+  if (entries < 0 || num_pages < 1 || entries > kMaxEntries || num_pages > kMaxI32) return 0;
   // A head, then: the free pages found (reserve); three lists and the pages of
   // fork's entries; compact's counts per 4096 pages and three lists.
   const size_t n = (size_t)entries, p = (size_t)num_pages;
@@ -248,14 +265,18 @@ int32_t rocs_cache_reserve(const int32_t* slots, const int32_t* row_offsets, int
                 0, 0, page_size};
   if (entries < 0 || num_rows < 0)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: a size is negative", name);
-  const int32_t st = check_cache(name, c, rocs_cache_workspace_size(entries, num_pages),
-                                 workspace_bytes);
-  if (st != ROCS_OK) return st;
-  if (entries > kMaxI32 || num_rows > kMaxI32)
+  if (entries > kMaxEntries || num_rows > kMaxI32)
     return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
+  const List from{slots, entries}, at{row_offsets, entries + 1}, to{rows, num_rows};
+  const int32_t st = check_cache(name, c, {from, at, to},
+                                 rocs_cache_workspace_size(entries, num_pages), workspace_bytes);
+  if (st != ROCS_OK) return st;
   if ((entries > 0 && (slots == nullptr || row_offsets == nullptr)) ||
       (num_rows > 0 && (rows == nullptr || entries == 0)))
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: null pointer argument", name);
+  for (const List& l : {from, at})
+    if (overlap(rows, (size_t)num_rows * 4, l.p, (size_t)l.n * 4))
+      return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: rows overlaps an input", name);
   const hipError_t e = launch_reserve(slots, row_offsets, entries, num_rows, page_table,
                                       table_width, lens, num_slots, refs, num_pages, page_size,
                                       rows, status, static_cast<int32_t*>(workspace),
@@ -297,10 +318,10 @@ int32_t rocs_cache_fork(const int32_t* parents, const int32_t* children, int64_t
   if (entries < 0 || num_layers < 1 || row_bytes < 1)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: need entries >= 0, num_layers >= 1 and "
                 "row_bytes >= 1", name);
-  const int32_t st = check_cache(name, c, rocs_cache_workspace_size(entries, num_pages),
-                                 workspace_bytes);
+  if (entries > kMaxEntries) return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
+  const int32_t st = check_cache(name, c, {{parents, entries}, {children, entries}},
+                                 rocs_cache_workspace_size(entries, num_pages), workspace_bytes);
   if (st != ROCS_OK) return st;
-  if (entries > kMaxI32) return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
   if (entries > 0 && (parents == nullptr || children == nullptr))
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: null pointer argument", name);
   const hipError_t e = launch_fork(parents, children, entries, page_table, table_width, lens,
@@ -318,10 +339,10 @@ int32_t rocs_cache_free(const int32_t* slots, int64_t entries, int32_t* page_tab
   const Cache c{page_table, lens, refs, kNone, kNone, nullptr, table_width, num_slots, num_pages,
                 0, 0, page_size};
   if (entries < 0) return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: a size is negative", name);
-  const int32_t st = check_cache(name, c, 0, 0);
-  if (st != ROCS_OK) return st;
-  if (entries * 256 >= (int64_t(1) << 32))
+  if (entries >= (int64_t(1) << 24))                   // a workgroup of 256 each
     return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
+  const int32_t st = check_cache(name, c, {{slots, entries}}, 0, 0);
+  if (st != ROCS_OK) return st;
   if (entries == 0) return ok();
   if (slots == nullptr) return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: null pointer argument", name);
   const hipError_t e = launch_free(slots, entries, page_table, table_width, lens, num_slots, refs,
@@ -339,7 +360,7 @@ int32_t rocs_cache_compact(int32_t* page_table, int64_t table_width, int64_t num
                 num_layers, row_bytes, page_size};
   if (num_layers < 1 || row_bytes < 1)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: need num_layers >= 1 and row_bytes >= 1", name);
-  const int32_t st = check_cache(name, c, rocs_cache_workspace_size(0, num_pages),
+  const int32_t st = check_cache(name, c, {}, rocs_cache_workspace_size(0, num_pages),
                                  workspace_bytes);
   if (st != ROCS_OK) return st;
   const hipError_t e = launch_compact(page_table, table_width, num_slots, refs, num_pages, pool,

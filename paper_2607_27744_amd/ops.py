@@ -978,7 +978,8 @@ def cache_reserve(slots, row_offsets, num_rows, page_table, lens, refs, page_siz
     """rocs_cache_reserve: entry i adds row_offsets[i + 1] - row_offsets[i] rows to slot slots[i]
     (int32 [n], [n + 1]; num_rows >= row_offsets[n]); lens, page_table and refs follow in place.
     Returns (rows int32 [num_rows]: the pool row of each new row, for cache_write, -1 past
-    row_offsets[n]; status int32 [2], see cache_check). All or nothing: otherwise rows are -1 and the cache is unchanged."""
+    row_offsets[n]; status int32 [2], see cache_check). All or nothing: a call that cannot be done
+    leaves the cache unchanged, and its rows are -1."""
     done = (_binding or _native()).cache_reserve(slots, row_offsets, num_rows, page_table, lens,
                                                  refs, page_size, rows, status, workspace, stream)
     if done is not None:

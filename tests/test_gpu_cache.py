@@ -111,6 +111,21 @@ def test_all_or_nothing(gpu_lib):
     c.check()
 
 
+def test_lengths_that_cannot_be(gpu_lib):
+    # Device data that the operators did not write: refused, with nothing read or changed.
+    c = Pair(1, 6, 4, 4, 2)
+    assert c.append([0, 3], [7, 6]) == 0
+    for length, code in ((-1, 3), (-100, 3), (9, 2), (2 ** 31 - 1, 2)):
+        c.ref.lens[3] = length
+        c.dev[2][3] = length
+        assert c.append([3], [1]) == code and c.fork([3], [1]) == 3
+        c.check()
+    c.ref.lens[3] = 6
+    c.dev[2][3] = 6
+    assert c.fork([3], [1]) == 0
+    c.check()
+
+
 def test_empty_calls(gpu_lib):
     c = Pair(2, 4, 4, 3, 2)
     assert c.append([], []) == 0 and c.append([1], [0]) == 0 and c.fork([], []) == 0

@@ -63,6 +63,7 @@ def _packed(lib, **kw):
     (dict(k=None), _lib.INVALID_ARGUMENT), (dict(qd=FAKE[6]), _lib.INVALID_ARGUMENT),
     (dict(out=FAKE[0]), _lib.INVALID_ARGUMENT), (dict(out=FAKE[2]), _lib.INVALID_ARGUMENT),
     (dict(out=FAKE[3]), _lib.INVALID_ARGUMENT), (dict(L=-1), _lib.INVALID_ARGUMENT),
+    (dict(qd=FAKE[6], kd=FAKE[7], out=P(FAKE[7].value + 128)), _lib.INVALID_ARGUMENT),
     (dict(most=-1), _lib.INVALID_ARGUMENT),
     (dict(most=100000), _lib.WORKSPACE_TOO_SMALL),
     (dict(most=100000, ws=P(0x90000010), ws_bytes=1 << 30), _lib.INVALID_ARGUMENT),
@@ -123,12 +124,18 @@ def test_cache_refusals(lib):
         assert call(ws=None) == call(ws_bytes=16) == _lib.WORKSPACE_TOO_SMALL
         assert call(ws=P(0xa0000010)) == _lib.INVALID_ARGUMENT
         assert call(refs=FAKE[2]) == call(status=FAKE[4]) == _lib.INVALID_ARGUMENT
+    assert reserve(n=(1 << 30) + 1) == fork(n=(1 << 30) + 1) == _lib.UNSUPPORTED
+    for out in (FAKE[0], FAKE[1], FAKE[2], FAKE[3], FAKE[4], FAKE[6], FAKE[9]):
+        assert reserve(rows=out) == _lib.INVALID_ARGUMENT       # rows over another array
+    assert reserve(slots=FAKE[3]) == reserve(off=FAKE[4]) == _lib.INVALID_ARGUMENT
+    assert fork(par=FAKE[2]) == fork(kid=FAKE[6]) == fork(kid=FAKE[7]) == _lib.INVALID_ARGUMENT
     assert reserve(n=-1) == reserve(m=-1) == reserve(n=0) == reserve(rows=None) == _lib.INVALID_ARGUMENT
     assert fork(layers=0) == fork(row=0) == fork(pool=None) == fork(par=None) == _lib.INVALID_ARGUMENT
     assert compact(layers=0) == compact(pool=FAKE[4]) == _lib.INVALID_ARGUMENT
     free = lambda n=2, slots=FAKE[0], table=FAKE[2]: lib.rocs_cache_free(   # noqa: E731
         slots, n, table, 4, FAKE[3], 8, FAKE[4], 8, 16, None)
     assert free(n=-1) == free(slots=None) == free(table=None) == _lib.INVALID_ARGUMENT
+    assert free(slots=FAKE[3]) == free(slots=FAKE[4]) == _lib.INVALID_ARGUMENT
     assert free(n=1 << 24) == _lib.UNSUPPORTED and free(n=0) == _lib.OK
     write = lambda x=FAKE[0], xs=64, m=4, n=8, row=64, pool=FAKE[2]: lib.rocs_cache_write(  # noqa: E731
         x, xs, FAKE[1], m, pool, n, row, None)
