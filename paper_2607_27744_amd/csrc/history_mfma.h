@@ -114,6 +114,20 @@ __device__ __forceinline__ void mask_step(V& s, int kb, int half, const RowRule&
   }
 }
 
+// The order of a run of PRODUCTS matrix instructions, each with READS LDS reads
+// for it AHEAD products earlier. (Left alone, the compiler puts a product's
+// reads right before it and waits for their latency each time.)
+template <int AHEAD, int READS, int PRODUCTS>
+__device__ __forceinline__ void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);        // LDS reads
+#pragma unroll
+  for (int i = 0; i < PRODUCTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);                    // a matrix instruction
+    if (i + AHEAD < PRODUCTS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // 4 bytes per lane from global memory into LDS, lane i at dst + 4 i.
 __device__ __forceinline__ void lds_dma4(const void* src, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" :: "v"(src), "s"(dst) : "m0");

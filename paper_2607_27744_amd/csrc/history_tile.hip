@@ -160,13 +160,27 @@ history_tile(const HistArgs a, int64_t slots) {
 #pragma unroll
   for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
 
-  auto qk_step = [&](int slot, int ks, f32x16 (&s)[KB]) __attribute__((always_inline)) {
+  // Products run with their K or V fragments read kAhead ahead of them (left alone, the
+  // compiler waits for the latency of each).
+  constexpr int kAhead = D == 64 ? 2 : 3, NM = KS * KB;
+  auto k_frag = [&](int slot, int i) __attribute__((always_inline)) {
+    return *reinterpret_cast<const ROCS_LDS bf16x8*>(
+        lds3 + ((ka0 ^ (32u * (i / KB))) + slot * STAGE + (i % KB) * 32 * ROWB));
+  };
+  // Scores of the stage in K's slot.
+  auto qk = [&](int slot, f32x16 (&s)[KB]) __attribute__((always_inline)) {
+    bf16x8 kf[kAhead];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const bf16x8 f = *reinterpret_cast<const ROCS_LDS bf16x8*>(
-          lds3 + ((ka0 ^ (32u * ks)) + slot * STAGE + kb * 32 * ROWB));
-      s[kb] = mfma32(f, qf[ks], s[kb]);
+    for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) kf[i] = k_frag(slot, i);
+#pragma unroll
+    for (int i = 0; i < NM; ++i) {
+      s[i % KB] = mfma32(kf[i % kAhead], qf[i / KB], s[i % KB]);
+      if (i + kAhead < NM) kf[i % kAhead] = k_frag(slot, i + kAhead);
     }
+    reads_ahead<kAhead, 1, NM>();
   };
   // Weights of step ps as packed bf16 B fragments, against ms. FINAL: the
   // scores are in exp2 units already; else they are raw, of a stage without a
@@ -207,18 +221,30 @@ history_tile(const HistArgs a, int64_t slots) {
     for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
     return m_run == -INFINITY ? 0.f : m_run;                   // no key seen yet: weights 0
   };
-  auto pv_step = [&](int slot, int ps, const uint32_t (&pk)[4]) __attribute__((always_inline)) {
-    const bf16x8 pf = as_bf16x8(u32x4{pk[0], pk[1], pk[2], pk[3]});
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      const uint32_t off = slot * STAGE + ps * 16 * ROWB;
+  // V times the weights of `count` 16-key steps from ps0.
+  auto pv = [&](int slot, int ps0, auto count, const uint32_t (&pk)[decltype(count)::value][4])
+      __attribute__((always_inline)) {
+    constexpr int NF = decltype(count)::value * DB;
+    auto frag = [&](int i) __attribute__((always_inline)) {
+      const int db = i % DB;
+      const uint32_t off = slot * STAGE + (ps0 + i / DB) * 16 * ROWB;
       const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (ROCS_LDS i16x4*)(lds3 + ((va0[0] ^ (64u * db)) + off))));
       const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (ROCS_LDS i16x4*)(lds3 + ((va0[1] ^ (64u * db)) + off))));
-      oacc[db] = mfma32(as_bf16x8(u32x4{x[0], x[1], y[0], y[1]}), pf, oacc[db]);
-    }
+      return as_bf16x8(u32x4{x[0], x[1], y[0], y[1]});
+    };
     __builtin_amdgcn_sched_barrier(0);
+    bf16x8 vf[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) vf[i] = frag(i);
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const uint32_t (&w)[4] = pk[i / DB];
+      oacc[i % DB] = mfma32(vf[i % kAhead], as_bf16x8(u32x4{w[0], w[1], w[2], w[3]}), oacc[i % DB]);
+      if (i + kAhead < NF) vf[i % kAhead] = frag(i + kAhead);
+    }
+    reads_ahead<kAhead, 2, NF>();
   };
   // A stage that every row of the wave sees whole: its weights and PV product,
   // with the scores of the next stage on the matrix cores meanwhile.
@@ -227,13 +253,44 @@ history_tile(const HistArgs a, int64_t slots) {
     for (int kb = 0; kb < KB; ++kb) sn[kb] = f32x16{};
     uint32_t pk[PS][4];
     float sum = 0.f;
+    constexpr int NP = 4 * PS, LAG = (SCORE & kCap) != 0 ? 2 : 0;
+    bf16x8 kf[kAhead];
 #pragma unroll
-    for (int ps = 0; ps < PS; ++ps) {
+    for (int i = 0; i < kAhead; ++i) kf[i] = k_frag(slot ^ 1, i);
+    const float lin = plain_shift<SCORE>(rule, base, hh) - m_run;
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+    float x[NP][2];
 #pragma unroll
-      for (int ks = KS / PS * ps; ks < KS / PS * (ps + 1); ++ks) qk_step(slot ^ 1, ks, sn);
-      weights(std::false_type{}, s, ps, base, m_run, pk[ps], sum);
-      if constexpr (D == 64) __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < NP + LAG + 1; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (i < NP && i % (NP / NM) == 0) {
+        const int j = i / (NP / NM);
+        sn[j % KB] = mfma32(kf[j % kAhead], qf[j / KB], sn[j % KB]);
+        if (j + kAhead < NM) kf[j % kAhead] = k_frag(slot ^ 1, j + kAhead);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        auto raw = [&](int at) __attribute__((always_inline)) { return s[at / 8][2 * (at % 8) + h]; };
+        auto key = [&](int at) { return 32 * (at / 8) + 8 * ((2 * (at % 8)) / 4) + (2 * (at % 8)) % 4 + h; };
+        if constexpr ((SCORE & kCap) != 0) {
+          if (i < NP) x[i][h] = __builtin_amdgcn_exp2f(raw(i) * rule.cap_in);
+          if (i >= 1 && i - 1 < NP) x[i - 1][h] = __builtin_amdgcn_rcpf(1.0f + x[i - 1][h]);
+          if (i >= 2 && i - 2 < NP) {
+            float shift = lin;
+            if constexpr ((SCORE & kBias) != 0) shift = fmaf(rule.slope2, (float)key(i - 2), shift);
+            x[i - 2][h] = __builtin_amdgcn_exp2f(fmaf(-2.0f * rule.cap2, x[i - 2][h], shift));
+          }
+        } else {
+          if (i < NP) x[i][h] = __builtin_amdgcn_exp2f(plain_score<SCORE>(raw(i), key(i), rule, lin));
+        }
+      }
+      const int d = i - LAG - 1;
+      if (d >= 0 && d < NP) {
+        pk[d / 4][d % 4] = pack_bf16x2(x[d][0], x[d][1]);
+        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[d / 4][d % 4]), ones, sum, false);
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
     if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
 #pragma unroll
       for (int ps = 0; ps < PS; ++ps) score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
@@ -244,8 +301,7 @@ history_tile(const HistArgs a, int64_t slots) {
     }
     l_part += sum;
     __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-    for (int ps = 0; ps < PS; ++ps) pv_step(slot, ps, pk[ps]);
+    pv(slot, 0, std::integral_constant<int, PS>{}, pk);
     __builtin_amdgcn_s_setprio(0);
   };
   // Half a stage (32 keys) of any other kind: the mask, where rows without a max
@@ -278,8 +334,7 @@ history_tile(const HistArgs a, int64_t slots) {
     }
     if (DOCS && __ballot(sum != 0.f) == 0) return;
     l_part += sum;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) pv_step(slot, 2 * kb + h, pk[h]);
+    pv(slot, 2 * kb, std::integral_constant<int, 2>{}, pk);
   };
 
   if (n > 0) {
@@ -312,15 +367,7 @@ history_tile(const HistArgs a, int64_t slots) {
     wait_vmcnt<0>();                                      // the query fragments included
     ring_barrier();
     f32x16 s_a[KB], s_b[KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) s_a[kb] = f32x16{};
-    if (nw > 0) {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        qk_step(0, ks, s_a);
-        if (ks % 2 == 1) __builtin_amdgcn_sched_barrier(0);
-      }
-    }
+    if (nw > 0) qk(0, s_a);
     ring_barrier();                                       // K slot 0 has been read
     // A step reads K of stage kt + 1 and V of stage kt; their other slots were
     // released by the last barrier and take K of kt + 2 and V of kt + 1.
@@ -355,15 +402,7 @@ history_tile(const HistArgs a, int64_t slots) {
       load(kt, slot);
       half(slot, b0, 0, s_a);
       half(slot, b0, 1, s_a);
-      if (kt + 1 < nw) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s_a[kb] = f32x16{};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          qk_step(slot ^ 1, ks, s_a);
-          if (ks % 2 == 1) __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+      if (kt + 1 < nw) qk(slot ^ 1, s_a);
       pass(kt);
       ++kt;
     };
