@@ -76,20 +76,21 @@ __device__ __forceinline__ float plain_score(float s, int c, const RowRule& r, f
 }
 
 // Scores of one 16-key step (elements 8 half .. + 7 of the block at key offset
-// 32 kb) in exp2 units, in place; keys from `base` (of the stage).
+// 32 kb) in exp2 units, less `ref`, in place; keys from `base` (of the stage).
 template <int SCORE, typename V>
-__device__ __forceinline__ void score_step(V& s, int kb, int half, const RowRule& r, int base, int hh) {
+__device__ __forceinline__ void score_step(V& s, int kb, int half, const RowRule& r, int base, int hh,
+                                           float ref) {
   const float rel = (float)(r.pos - base - 4 * hh);
+  const float none = (SCORE & kCap) != 0 ? r.cap2 - ref : -ref;
 #pragma unroll
   for (int e = 8 * half; e < 8 * half + 8; ++e) {
     const int c = 32 * kb + 8 * (e / 4) + e % 4;
-    float y;
+    float shift = none;
+    if constexpr ((SCORE & kBias) != 0) shift = fmaf(-r.slope2, fabsf(rel - (float)c), none);
     if constexpr ((SCORE & kCap) != 0)
-      y = fmaf(-2.0f * r.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[e] * r.cap_in)), r.cap2);
+      s[e] = fmaf(-2.0f * r.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[e] * r.cap_in)), shift);
     else
-      y = s[e] * r.scale2;
-    if constexpr ((SCORE & kBias) != 0) y = fmaf(-r.slope2, fabsf(rel - (float)c), y);
-    s[e] = y;
+      s[e] = fmaf(s[e], r.scale2, shift);
   }
 }
 

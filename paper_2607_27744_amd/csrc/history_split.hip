@@ -34,6 +34,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   constexpr int STAGE = kKeys * ROWB;
   constexpr int KPI = 1024 / ROWB;        // rows of a DMA load
   constexpr int NI = kKeys / KPI;         // loads of a stage and operand
+  constexpr int kAhead = 4;               // fragments in flight (see reads_ahead)
   static_assert(kRows * D * 4 <= 2 * STAGE, "a wave's partial output takes its staging");
   __shared__ __attribute__((aligned(1024))) char lds[kWaves * 2 * STAGE];
   __shared__ __attribute__((aligned(16))) int32_t doc_ids[DOCS ? kWaves * 2 * 64 : 4];
@@ -145,18 +146,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     wait_vmcnt<NI>();                                     // K of this stage (V may be in flight)
     asm volatile("" ::: "memory");
     f32x16 s = {};
+    {
+      auto frag = [&](int ks) __attribute__((always_inline)) {
+        return *reinterpret_cast<const ROCS_LDS bf16x8*>(lds3 + (ka0 ^ (32u * ks)));
+      };
+      bf16x8 f[kAhead];
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8 f = *reinterpret_cast<const ROCS_LDS bf16x8*>(lds3 + (ka0 ^ (32u * ks)));
-      s = mfma32(f, qf[ks], s);
+      for (int ks = 0; ks < kAhead; ++ks) f[ks] = frag(ks);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        s = mfma32(f[ks % kAhead], qf[ks], s);
+        if (ks + kAhead < KS) f[ks % kAhead] = frag(ks + kAhead);
+      }
+      reads_ahead<kAhead, 1, KS>();
     }
     wait_lgkmcnt0();                                      // K's fragments are in registers
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
     if (more) issue_k(next, off, slot ^ 1);
     if constexpr (SCORE != 0) {
-      score_step<SCORE>(s, 0, 0, rule, base, hh);
-      score_step<SCORE>(s, 0, 1, rule, base, hh);
+      score_step<SCORE>(s, 0, 0, rule, base, hh, 0.f);
+      score_step<SCORE>(s, 0, 1, rule, base, hh, 0.f);
     }
     if (base + kKeys > plain) {
       const ROCS_LDS int32_t* ids = (const ROCS_LDS int32_t*)doc_ids + (DOCS ? (2 * wave + slot) * 64 : 0);
@@ -204,18 +215,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
     l_part += sum;
     if (more) wait_vmcnt<NI + (DOCS ? 1 : 0)>(); else wait_vmcnt<0>();   // V of this stage
     asm volatile("" ::: "memory");
-#pragma unroll
-    for (int ps = 0; ps < PS; ++ps) {
-      const bf16x8 pf = as_bf16x8(u32x4{pk[ps][0], pk[ps][1], pk[ps][2], pk[ps][3]});
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const uint32_t o = ps * 16 * ROWB;
+    {
+      auto frag = [&](int i) __attribute__((always_inline)) {
+        const uint32_t o = (i / DB) * 16 * ROWB, db = i % DB;
         const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (ROCS_LDS i16x4*)(lds3 + ((va0[0] ^ (64u * db)) + o))));
         const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (ROCS_LDS i16x4*)(lds3 + ((va0[1] ^ (64u * db)) + o))));
-        oacc[db] = mfma32(as_bf16x8(u32x4{x[0], x[1], y[0], y[1]}), pf, oacc[db]);
+        return as_bf16x8(u32x4{x[0], x[1], y[0], y[1]});
+      };
+      bf16x8 f[kAhead];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) f[i] = frag(i);
+#pragma unroll
+      for (int i = 0; i < PS * DB; ++i) {
+        const uint32_t (&w)[4] = pk[i / DB];
+        oacc[i % DB] = mfma32(f[i % kAhead], as_bf16x8(u32x4{w[0], w[1], w[2], w[3]}), oacc[i % DB]);
+        if (i + kAhead < PS * DB) f[i % kAhead] = frag(i + kAhead);
       }
+      reads_ahead<kAhead, 2, PS * DB>();
     }
     wait_lgkmcnt0();                                      // V's fragments are in registers
     __builtin_amdgcn_sched_barrier(0);

@@ -182,25 +182,14 @@ history_tile(const HistArgs a, int64_t slots) {
     }
     reads_ahead<kAhead, 1, NM>();
   };
-  // Weights of step ps as packed bf16 B fragments, against ms. FINAL: the
-  // scores are in exp2 units already; else they are raw, of a stage without a
-  // mask, and the rules and the subtraction share their fused multiply-adds.
-  // Each pair is a scalar of its own (see dca_attn_bf16).
-  auto weights = [&](auto final, const f32x16 (&s)[KB], int ps, int base, float ms, uint32_t (&pk)[4],
-                     float& sum) __attribute__((always_inline)) {
-    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
-    const float lin = plain_shift<SCORE>(rule, base, hh) - ms;
+  // Weights of step ps as packed bf16 B fragments, from scores in exp2 units less
+  // the max. Each pair is a scalar of its own (see dca_attn_bf16).
+  const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+  auto weights = [&](const f32x16 (&s)[KB], int ps, uint32_t (&pk)[4], float& sum) __attribute__((always_inline)) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      float e[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int el = 8 * (ps % 2) + 2 * w + i;
-        const float x = s[ps / 2][el];
-        if constexpr (decltype(final)::value) e[i] = x - ms;
-        else e[i] = plain_score<SCORE>(x, 32 * (ps / 2) + 8 * (el / 4) + el % 4, rule, lin);
-      }
-      pk[w] = pack_bf16x2(__builtin_amdgcn_exp2f(e[0]), __builtin_amdgcn_exp2f(e[1]));
+      const int el = 8 * (ps % 2) + 2 * w;
+      pk[w] = pack_bf16x2(__builtin_amdgcn_exp2f(s[ps / 2][el]), __builtin_amdgcn_exp2f(s[ps / 2][el + 1]));
       sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[w]), ones, sum, false);
     }
   };
@@ -247,57 +236,69 @@ history_tile(const HistArgs a, int64_t slots) {
     reads_ahead<kAhead, 2, NF>();
   };
   // A stage that every row of the wave sees whole: its weights and PV product,
-  // with the scores of the next stage on the matrix cores meanwhile.
+  // with the scores of the next stage on the matrix cores meanwhile. A matrix
+  // instruction holds up its wave until the last one is through, so they are
+  // dealt out: step i issues one product and forms two weights, of which each
+  // transcendental waits a step for the one before it (D = 128; 16 requests of
+  // 2,048 rows behind a prefix, 8 heads on 2, capped: 323 us in the compiler's
+  // order, 281 so; one of 16,384 rows, 8 heads, no cap: 530 and 480).
   auto stage = [&](int slot, int base, f32x16 (&s)[KB], f32x16 (&sn)[KB]) __attribute__((always_inline)) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) sn[kb] = f32x16{};
     uint32_t pk[PS][4];
     float sum = 0.f;
-    constexpr int NP = 4 * PS, LAG = (SCORE & kCap) != 0 ? 2 : 0;
+    constexpr int NP = 4 * PS, LAG = (SCORE & kCap) != 0 ? 2 : 0;  // pairs; steps from score to weight
     bf16x8 kf[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) kf[i] = k_frag(slot ^ 1, i);
     const float lin = plain_shift<SCORE>(rule, base, hh) - m_run;
-    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
     float x[NP][2];
 #pragma unroll
     for (int i = 0; i < NP + LAG + 1; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
       if (i < NP && i % (NP / NM) == 0) {
         const int j = i / (NP / NM);
         sn[j % KB] = mfma32(kf[j % kAhead], qf[j / KB], sn[j % KB]);
         if (j + kAhead < NM) kf[j % kAhead] = k_frag(slot ^ 1, j + kAhead);
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        auto raw = [&](int at) __attribute__((always_inline)) { return s[at / 8][2 * (at % 8) + h]; };
-        auto key = [&](int at) { return 32 * (at / 8) + 8 * ((2 * (at % 8)) / 4) + (2 * (at % 8)) % 4 + h; };
-        if constexpr ((SCORE & kCap) != 0) {
-          if (i < NP) x[i][h] = __builtin_amdgcn_exp2f(raw(i) * rule.cap_in);
-          if (i >= 1 && i - 1 < NP) x[i - 1][h] = __builtin_amdgcn_rcpf(1.0f + x[i - 1][h]);
-          if (i >= 2 && i - 2 < NP) {
-            float shift = lin;
-            if constexpr ((SCORE & kBias) != 0) shift = fmaf(rule.slope2, (float)key(i - 2), shift);
-            x[i - 2][h] = __builtin_amdgcn_exp2f(fmaf(-2.0f * rule.cap2, x[i - 2][h], shift));
-          }
-        } else {
-          if (i < NP) x[i][h] = __builtin_amdgcn_exp2f(plain_score<SCORE>(raw(i), key(i), rule, lin));
-        }
       }
       const int d = i - LAG - 1;
       if (d >= 0 && d < NP) {
         pk[d / 4][d % 4] = pack_bf16x2(x[d][0], x[d][1]);
         sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[d / 4][d % 4]), ones, sum, false);
       }
+      float in[3][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        auto raw = [&](int at) __attribute__((always_inline)) { return s[at / 8][2 * (at % 8) + h]; };
+        auto key = [&](int at) { return 32 * (at / 8) + 8 * ((2 * (at % 8)) / 4) + (2 * (at % 8)) % 4 + h; };
+        if constexpr ((SCORE & kCap) != 0) {
+          if (i < NP) in[0][h] = raw(i) * rule.cap_in;
+          if (i >= 1 && i - 1 < NP) in[1][h] = 1.0f + x[i - 1][h];
+          if (i >= 2 && i - 2 < NP) {
+            float shift = lin;
+            if constexpr ((SCORE & kBias) != 0) shift = fmaf(rule.slope2, (float)key(i - 2), shift);
+            in[2][h] = fmaf(-2.0f * rule.cap2, x[i - 2][h], shift);
+          }
+        } else {
+          if (i < NP) in[0][h] = plain_score<SCORE>(raw(i), key(i), rule, lin);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (i < NP) x[i][h] = __builtin_amdgcn_exp2f(in[0][h]);
+        if (LAG == 2 && i >= 1 && i - 1 < NP) x[i - 1][h] = __builtin_amdgcn_rcpf(in[1][h]);
+        if (LAG == 2 && i >= 2 && i - 2 < NP) x[i - 2][h] = __builtin_amdgcn_exp2f(in[2][h]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);
     if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
 #pragma unroll
-      for (int ps = 0; ps < PS; ++ps) score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh);
+      for (int ps = 0; ps < PS; ++ps) score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh, 0.f);
       const float ms = move_max(max_across_halves(fmaxf(row_max(s[0]), row_max(s[1]))));
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb] -= ms;
       sum = 0.f;
 #pragma unroll
-      for (int ps = 0; ps < PS; ++ps) weights(std::true_type{}, s, ps, base, ms, pk[ps], sum);
+      for (int ps = 0; ps < PS; ++ps) weights(s, ps, pk[ps], sum);
     }
     l_part += sum;
     __builtin_amdgcn_s_setprio(1);
@@ -310,27 +311,29 @@ history_tile(const HistArgs a, int64_t slots) {
     const int key = base + 32 * kb;
     if (key >= lim_hi) return;
     const ROCS_LDS int32_t* ids = (const ROCS_LDS int32_t*)doc_ids + (DOCS ? kStageKeys * slot : 0);
+    float ref = m_run == -INFINITY ? 0.f : m_run;              // what the scores are less
 #pragma unroll
-    for (int h = 0; h < 2; ++h) score_step<SCORE>(s[kb], kb, h, rule, base, hh);
+    for (int h = 0; h < 2; ++h) score_step<SCORE>(s[kb], kb, h, rule, base, hh, ref);
     if (DOCS || key + 32 > lim_lo) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) mask_step<DOCS>(s[kb], kb, h, rule, base, hh, ids);
     }
-    float ms = m_run;
     if (__ballot(m_run == -INFINITY) != 0) {
       const float mx = max_across_halves(row_max(s[kb]));
       if (m_run == -INFINITY) m_run = mx;                      // nothing summed yet
-      ms = m_run == -INFINITY ? 0.f : m_run;
+      const float to = m_run == -INFINITY ? 0.f : m_run;
+      s[kb] -= to - ref;
+      ref = to;
     }
     uint32_t pk[2][4];
     float sum = 0.f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) weights(std::true_type{}, s, 2 * kb + h, base, ms, pk[h], sum);
+    for (int h = 0; h < 2; ++h) weights(s, 2 * kb + h, pk[h], sum);
     if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
-      ms = move_max(max_across_halves(row_max(s[kb])));
+      s[kb] -= move_max(max_across_halves(row_max(s[kb])) + ref) - ref;
       sum = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) weights(std::true_type{}, s, 2 * kb + h, base, ms, pk[h], sum);
+      for (int h = 0; h < 2; ++h) weights(s, 2 * kb + h, pk[h], sum);
     }
     if (DOCS && __ballot(sum != 0.f) == 0) return;
     l_part += sum;
