@@ -242,7 +242,8 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
 // part), then they share the parts, eight in flight. A part without a seen key
 // has l = 0 and no O; its loads are not skipped (a branch would put one latency
 // after the other) but dropped. Rows that are done already (kDone) are left.
-// Bound by latency for few rows, else by the read of the parts.
+// Bound by latency for few rows (8 rows in 9 parts: 2.9 us; 1,024 in 11:
+// 5.4), else by the read of the parts.
 // ---------------------------------------------------------------------------
 constexpr int kMaxSplits = 256;
 
@@ -360,19 +361,22 @@ HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_le
   };
   // A history is cut where the tiles alone leave the chip idle: two workgroups a
   // CU, chunks of at least 256 keys. (More parts than that do not pay at 128 rows:
-  // chunks over six cached histories of 2,400 to 12,800 rows take 435 us in 504
-  // whole tiles, 520 in four parts.)
+  // chunks over six cached histories of 2,400 to 12,800 rows take 418 us in 504
+  // whole tiles, 508 in four parts.)
   int64_t splits = parts(512 / tiles, 256);
   if (p.rows == 32) {
     // Few rows: a read of K and V. With two rounds of the chip in chunks of 512
-    // keys, a workgroup takes up to four heads and chunks are many, so that ragged
-    // histories end together (128 histories of 3,125 rows on average, 8 heads x
-    // 128: 301 us; a head a workgroup: 326; 40 of them: 95 and 126). With less,
-    // the waves of a head share its keys, which is fewer steps one after the
-    // other (one history of 16,384 rows: 18 us, by four heads 34).
-    const int hw = Hk % 4 == 0 ? 4 : Hk % 2 == 0 ? 2 : 1;
+    // keys, chunks are many, so that ragged histories end together, and a workgroup
+    // takes as many heads, up to four, as still make two rounds (128 histories of
+    // 3,100 rows on average, 8 heads x 128: 287 us; a head a workgroup: 323; 40 of
+    // them: 96 by two heads, 102 as below). With less, the waves of a head share
+    // its keys, which is fewer steps one after the other (one history of 16,384
+    // rows: 20 us, by four heads 24).
+    const int64_t chunks = (max_len + 511) / 512;
+    int hw = Hk % 4 == 0 ? 4 : Hk % 2 == 0 ? 2 : 1;
+    while (hw > 1 && R * (Hk / hw) * chunks < 1024) hw /= 2;
     const int64_t wide = R * (Hk / hw);
-    if (wide * ((max_len + 511) / 512) >= 1024) {
+    if (wide * chunks >= 1024) {
       p.heads = hw;
       splits = parts(4096 / wide, 512);
     } else {
