@@ -32,6 +32,7 @@ struct HistArgs {
   // results per (split, row, head): {max (log2 units), sum} and the sums.
   int splits, chunk;
   int heads;                // K/V heads a workgroup of the 32-row kernel: 1, 2 or 4
+  int deal;                 // 128-row kernel: XCDs that a head's tiles are dealt to, or 1
   float* part_ml;           // [splits][N * H][2]
   float* part_o;            // [splits][N * H][D]
 };

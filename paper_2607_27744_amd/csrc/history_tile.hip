@@ -15,7 +15,8 @@
 // The rows of a tile need not have seen a key yet when a stage starts
 // (documents), so a row's max may stay -inf; its weights are then 0.
 // Work order. Under the causal mask a request's last tiles are the longest:
-// they come first, so that the launch does not end with them.
+// they come first, so that the launch does not end with them. An XCD takes one
+// head (or few) and a run of requests (see launch_history_tile).
 // Head dims. D is 64 or 128; a head_dim below it (a multiple of 8) has zeros in
 // the query fragments' places past its end, its last 16 bytes once more in the
 // K/V stage's, and those columns of the result are not stored.
@@ -53,10 +54,18 @@ history_tile(const HistArgs a, int64_t slots) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hh = lane >> 5;
-  const uint32_t work = xcd_remap(blockIdx.x, gridDim.x);
   const uint32_t per_head = (uint32_t)slots * (uint32_t)a.splits;
-  const int hk = (int)(work / per_head);
-  const uint32_t rest = work - (uint32_t)hk * per_head;
+  uint32_t hk, rest;
+  if (a.deal > 1) {
+    const uint32_t m = (uint32_t)a.deal, xcd = blockIdx.x % kNumXcd;
+    hk = xcd / m;
+    rest = blockIdx.x / kNumXcd * m + xcd % m;
+    if (rest >= per_head) return;
+  } else {
+    const uint32_t work = xcd_remap(blockIdx.x, gridDim.x);
+    hk = work / per_head;
+    rest = work - hk * per_head;
+  }
   const int split = (int)(rest % (uint32_t)a.splits);
   const HistTile t = hist_tile(a, slots - 1 - rest / (uint32_t)a.splits, kRows);
   if (t.rows <= 0) return;
@@ -530,9 +539,17 @@ hipError_t launch_dim(const HistArgs& a, int64_t slots, int64_t blocks, hipStrea
 
 }  // namespace
 
-hipError_t launch_history_tile(const HistArgs& a, hipStream_t s) {
-  const int64_t slots = a.R + (a.N * a.G + kRows - 1) / kRows;
-  const int64_t blocks = slots * a.Hk * a.splits;
+hipError_t launch_history_tile(const HistArgs& args, hipStream_t s) {
+  HistArgs a = args;
+  const int64_t slots = a.R + (a.N * a.G + kRows - 1) / kRows, per_head = slots * a.splits;
+  // Where m XCDs share a head, each takes a run of its requests, whose K and V then
+  // pass through one L2. Few requests that do not come out even leave XCDs idle;
+  // those are dealt out tile by tile (one of 16,384 rows, 8 heads on 4: 499 us
+  // instead of 753; 3 of 4,096: 124 and 143; on 2 K/V heads 5: 189 and 211, but 11:
+  // 388 and 368; 16 of 2,048 on one: 172 and 155).
+  const int m = kNumXcd % a.Hk == 0 ? (int)kNumXcd / a.Hk : 1;
+  a.deal = a.R % m != 0 && a.R < (2 * m > 8 ? 2 * m : 8) ? m : 1;
+  const int64_t blocks = a.deal > 1 ? (per_head + m - 1) / m * kNumXcd : per_head * a.Hk;
   if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
   return a.D > 64 ? launch_dim<128>(a, slots, blocks, s) : launch_dim<64>(a, slots, blocks, s);
 }

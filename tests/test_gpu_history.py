@@ -101,6 +101,16 @@ def test_packed_against_oracle(gpu_lib, shape, rule):
     check(got, *want, max(kv_len), "bf16" if dtype == BF else "fp32")
 
 
+@pytest.mark.parametrize("requests, hk", [(1, 1), (3, 1), (16, 1), (17, 1), (1, 2), (4, 2), (5, 2),
+                                          (1, 4), (3, 4), (6, 4), (9, 4), (1, 3), (5, 8)])
+def test_tiles_over_the_dies(gpu_lib, requests, hk):
+    # Few requests and K/V heads, where a head's tiles are dealt out in more than one way.
+    lens = [40 + (37 * r) % 230 for r in range(requests)]
+    q, k, v = _case(BF, 2 * hk, hk, 64, lens, lens, seed=requests)
+    got = ops.history_attention(q, k, v, _off(lens), _off(lens))
+    check(got, *oracle.attention(_np(q), _np(k), _np(v), lens, lens), max(lens), "bf16")
+
+
 def _paged(k, v, kv_len, page, seed=0, spare=5, slots=None, fill=0.0):
     """The packed K/V of each request in shuffled pages: (pool, table, lens, slots)."""
     rng = np.random.default_rng(seed)
