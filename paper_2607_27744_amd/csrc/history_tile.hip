@@ -27,8 +27,8 @@
 // clock that the power holds down (one history of 16,384 rows, 8 heads x 128,
 // causal: 480 us, 1,145 TFLOP/s; a large bf16 product reaches 1,258). A cap
 // makes it the VALU (three transcendentals a score, 690 TFLOP/s). Where ragged
-// histories are a few stages long, the masked stages, at twice the VALU work, and
-// the latency from a tile's start to its first stage (256 of 640 rows, 4 heads x
+// histories are a few stages long, latency: from a tile's start to its first
+// stage, and between stages of which half are masked (256 of 640 rows, 4 heads x
 // 64, with a bias: 146 us, 442 TFLOP/s, 2.3 TB/s).
 #include "history_mfma.h"
 #include "launch.h"
