@@ -22,7 +22,9 @@
  *   that a row does not see have no part in it, whatever they hold: infinities
  *   and NaN there do not reach the row.
  *   Scores, softmax and sums are fp32; the bf16 kernels round the softmax
- *   weights to bf16 for the product with V and sum the rounded weights.
+ *   weights to bf16 for the product with V and sum the rounded weights. Their
+ *   cap adds an error of at most 2^-22 cap to a score for caps up to 128, and of
+ *   2^-19 of the score itself for larger ones (which take more instructions).
  */
 #ifndef ROCS_HISTORY_H
 #define ROCS_HISTORY_H

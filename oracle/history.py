@@ -11,6 +11,7 @@ by at most 2 e times it) and a bound on the scores' own error in fp32.
 import numpy as np
 
 U32 = 2.0 ** -24
+CAP_TURN = 128.0      # up to this cap its error may be relative to the cap, beyond it to the score
 
 
 def attention(q, k, v, q_len, kv_len, *, causal=True, prefix=None, q_docs=None, kv_docs=None,
@@ -39,7 +40,7 @@ def attention(q, k, v, q_len, kv_len, *, causal=True, prefix=None, q_docs=None, 
             e = (d + 8) * U32 * (np.abs(qh) @ np.abs(kh).T) * abs(scale)
             if cap > 0:
                 s = cap * np.tanh(s / cap)
-                e = e + 32 * U32 * cap
+                e = e + 32 * U32 * np.maximum(np.abs(s), min(cap, CAP_TURN))
             if slopes is not None:
                 away = slopes[head] * np.abs(pos - j)
                 e = e + 4 * U32 * (np.abs(s) + away)

@@ -14,7 +14,9 @@
 namespace rocs {
 
 constexpr int kStageKeys = 64;
-constexpr int kCap = 1, kBias = 2;          // SCORE: a cap, a bias by distance
+// SCORE: a cap up to kCapTurn, a bias by distance, a cap above kCapTurn.
+constexpr int kCap = 1, kBias = 2, kWideCap = 4;
+constexpr float kCapTurn = 128.0f;
 constexpr float kLazyMove = 64.0f;          // log2 of the largest unnormalised weight
 constexpr float kStageBound = 0x1p64f;      // per-lane stage sum taken without a row max
 
@@ -48,16 +50,53 @@ struct KeyFeed {
 // ---------------------------------------------------------------------------
 // Scores. The cap in exp2 units: cap tanh(x / cap) = cap (1 - 2 / (1 + e^(2x/cap))),
 // two transcendentals; both tails come out exactly (rcp of infinity and of 1).
-// Its error is a few units of 2^-24 cap, absolute, which is what a softmax
-// weight feels. The bias in a stage that lies wholly before a row needs no
+// Around 0 the difference cancels: its error is up to 2^-22 cap, absolute, at
+// any score (2.5e-5 at a cap of 128, what an fp32 sum of 128 products is off by;
+// at 1e5 it would be 0.02, at 1e8 all scores one value). Caps above kCapTurn
+// therefore take another form, whose error is relative to the score as that of the
+// score itself is. It costs more instructions (16 requests of 2,048 rows, 8 heads x
+// 128, causal: 207 us, 195 with a cap of 30, 167 without one), so the caps in use
+// keep this form. The bias in a stage that lies wholly before a row needs no
 // distance: -slope (p - j) is linear in j.
 // ---------------------------------------------------------------------------
 struct RowRule {
   float scale2;            // scale log2(e)
-  float cap_in, cap2;      // 2 scale log2(e) / cap, cap log2(e)
+  float cap_in, cap2;      // 2 scale log2(e) / cap (wide: scale / cap), cap log2(e)
   float slope2;            // slope log2(e)
   int pos, lim, doc;
 };
+
+// The score rules of query head `head`. Both limits to finite values: a factor
+// of infinity would make a score of 0 NaN.
+template <int SCORE>
+__device__ __forceinline__ void score_rules(RowRule& r, const HistArgs& a, int head) {
+  constexpr float kMax = 3.402823466e38f;
+  r.scale2 = a.scale * kLog2e;
+  r.cap_in = r.cap2 = r.slope2 = 0.f;
+  if constexpr ((SCORE & kCap) != 0) r.cap_in = fminf(2.0f * r.scale2 / a.cap, kMax);
+  if constexpr ((SCORE & kWideCap) != 0) r.cap_in = fminf(a.scale / a.cap, kMax);
+  if constexpr ((SCORE & (kCap | kWideCap)) != 0) r.cap2 = fminf(a.cap * kLog2e, kMax);
+  if constexpr ((SCORE & kBias) != 0) r.slope2 = a.slopes[head] * kLog2e;
+}
+
+// A capped score in exp2 units without the cancellation. Up to u = x / cap of 1/4 the
+// series tanh(u) / u = 1 - u^2/3 + 2u^4/15 - 17u^6/315 + 62u^8/2835 (its next
+// term is below 2^-26 there): scale log2(e) times it, from w = u^2.
+constexpr float kSeriesEnd = 1.0f / 16.0f;  // of w
+__device__ __forceinline__ float cap_series(float w, const RowRule& r) {
+  float t = fmaf(w, 62.0f / 2835.0f * r.scale2, -17.0f / 315.0f * r.scale2);
+  t = fmaf(w, t, 2.0f / 15.0f * r.scale2);
+  t = fmaf(w, t, -1.0f / 3.0f * r.scale2);
+  return fmaf(w, t, r.scale2);
+}
+// Beyond it the form with the exponential, whose value is no longer small
+// against its error (2^-19 relative at most).
+__device__ __forceinline__ float wide_cap(float s, const RowRule& r) {
+  const float u = s * r.cap_in, w = u * u;
+  const float e = __builtin_amdgcn_exp2f(u * (2.0f * kLog2e));
+  const float far = r.cap2 * fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + e), 1.0f);
+  return w <= kSeriesEnd ? s * cap_series(w, r) : far;
+}
 
 // One score in exp2 units for a stage that needs no mask and lies before the
 // row: key offset c in the stage, shift = plain_shift, less the running max.
@@ -67,11 +106,18 @@ __device__ __forceinline__ float plain_shift(const RowRule& r, int base, int hh)
   if constexpr ((SCORE & kBias) != 0) x -= r.slope2 * (float)(r.pos - base - 4 * hh);
   return x;
 }
+// A wide cap takes the series whatever the score; reach follows the largest w,
+// and a stage that it takes past kSeriesEnd forms its scores again.
 template <int SCORE>
-__device__ __forceinline__ float plain_score(float s, int c, const RowRule& r, float shift) {
+__device__ __forceinline__ float plain_score(float s, int c, const RowRule& r, float shift, float& reach) {
   if constexpr ((SCORE & kBias) != 0) shift = fmaf(r.slope2, (float)c, shift);
   if constexpr ((SCORE & kCap) != 0)
     return fmaf(-2.0f * r.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * r.cap_in)), shift);
+  if constexpr ((SCORE & kWideCap) != 0) {
+    const float u = s * r.cap_in, w = u * u;
+    reach = fmaxf(reach, w);
+    return fmaf(s, cap_series(w, r), shift);
+  }
   return fmaf(s, r.scale2, shift);
 }
 
@@ -89,6 +135,8 @@ __device__ __forceinline__ void score_step(V& s, int kb, int half, const RowRule
     if constexpr ((SCORE & kBias) != 0) shift = fmaf(-r.slope2, fabsf(rel - (float)c), none);
     if constexpr ((SCORE & kCap) != 0)
       s[e] = fmaf(-2.0f * r.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[e] * r.cap_in)), shift);
+    else if constexpr ((SCORE & kWideCap) != 0)
+      s[e] = wide_cap(s[e], r) + shift;
     else
       s[e] = fmaf(s[e], r.scale2, shift);
   }
@@ -214,6 +262,12 @@ __device__ __forceinline__ int doc_stages(DocList& list, const int32_t* kv_docs,
   }
   __syncthreads();
   return list.count;
+}
+
+// SCORE of a call.
+inline int score_of(const HistArgs& a) {
+  const int cap = a.cap > kCapTurn ? kWideCap : a.cap > 0.f ? kCap : 0;
+  return cap | (a.slopes != nullptr ? kBias : 0);
 }
 
 // Whether the accumulators hold an infinity or NaN (0 times either is NaN).

@@ -64,10 +64,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
   const int row = t.row0 + min(l32, t.rows - 1);              // clamped; extra rows never stored
   const int token = row / a.G, head = hk * a.G + row % a.G;
   RowRule rule;
-  rule.scale2 = a.scale * kLog2e;
-  rule.cap_in = a.cap > 0.f ? 2.0f * rule.scale2 / a.cap : 0.f;
-  rule.cap2 = a.cap * kLog2e;
-  rule.slope2 = (SCORE & kBias) != 0 ? a.slopes[head] * kLog2e : 0.f;
+  score_rules<SCORE>(rule, a, head);
   rule.pos = position_of(t, token);
   rule.lim = limit_of(a, t, token);
   rule.doc = DOCS ? a.q_docs[t.q0 + token] : 0;
@@ -302,11 +299,14 @@ hipError_t launch_score(const HistArgs& a, int64_t slots, int64_t blocks, hipStr
 
 template <int D>
 hipError_t launch_dim(const HistArgs& a, int64_t slots, int64_t blocks, hipStream_t s) {
-  const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
-  if (cap && bias) return launch_score<D, kCap | kBias>(a, slots, blocks, s);
-  if (cap) return launch_score<D, kCap>(a, slots, blocks, s);
-  if (bias) return launch_score<D, kBias>(a, slots, blocks, s);
-  return launch_score<D, 0>(a, slots, blocks, s);
+  switch (score_of(a)) {
+    case kCap: return launch_score<D, kCap>(a, slots, blocks, s);
+    case kWideCap: return launch_score<D, kWideCap>(a, slots, blocks, s);
+    case kBias: return launch_score<D, kBias>(a, slots, blocks, s);
+    case kCap | kBias: return launch_score<D, kCap | kBias>(a, slots, blocks, s);
+    case kWideCap | kBias: return launch_score<D, kWideCap | kBias>(a, slots, blocks, s);
+    default: return launch_score<D, 0>(a, slots, blocks, s);
+  }
 }
 
 }  // namespace

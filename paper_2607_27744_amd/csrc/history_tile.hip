@@ -75,10 +75,7 @@ history_tile(const HistArgs a, int64_t slots) {
   const int row = t.row0 + min(wrow0 + l32, t.rows - 1);      // clamped; extra rows never stored
   const int token = row / a.G, head = hk * a.G + row % a.G;
   RowRule rule;
-  rule.scale2 = a.scale * kLog2e;
-  rule.cap_in = a.cap > 0.f ? 2.0f * rule.scale2 / a.cap : 0.f;
-  rule.cap2 = a.cap * kLog2e;
-  rule.slope2 = (SCORE & kBias) != 0 ? a.slopes[head] * kLog2e : 0.f;
+  score_rules<SCORE>(rule, a, head);
   rule.pos = position_of(t, token);
   rule.lim = limit_of(a, t, token);
   rule.doc = DOCS ? a.q_docs[t.q0 + token] : 0;
@@ -263,7 +260,7 @@ history_tile(const HistArgs a, int64_t slots) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) sn[kb] = f32x16{};
     uint32_t pk[PS][4];
-    float sum = 0.f;
+    float sum = 0.f, reach = 0.f;
     constexpr int NP = 4 * PS, LAG = (SCORE & kCap) != 0 ? 2 : 0;  // pairs; steps from score to weight
     bf16x8 kf[kAhead];
 #pragma unroll
@@ -296,7 +293,7 @@ history_tile(const HistArgs a, int64_t slots) {
             in[2][h] = fmaf(-2.0f * rule.cap2, x[i - 2][h], shift);
           }
         } else {
-          if (i < NP) in[0][h] = plain_score<SCORE>(raw(i), key(i), rule, lin);
+          if (i < NP) in[0][h] = plain_score<SCORE>(raw(i), key(i), rule, lin, reach);
         }
       }
 #pragma unroll
@@ -307,9 +304,14 @@ history_tile(const HistArgs a, int64_t slots) {
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
+    bool again = !(sum <= kStageBound);
+    if constexpr ((SCORE & kWideCap) != 0) again = again || !(reach <= kSeriesEnd);
+    if (__builtin_expect(__ballot(again) != 0, 0)) {
+      RowRule anew = rule;
+      // (Laundered: or what the first pass formed is kept for this one, in scratch.)
+      if constexpr ((SCORE & kWideCap) != 0) asm volatile("" : "+v"(anew.cap_in));
 #pragma unroll
-      for (int ps = 0; ps < PS; ++ps) score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, rule, base, hh, 0.f);
+      for (int ps = 0; ps < PS; ++ps) score_step<SCORE>(s[ps / 2], ps / 2, ps % 2, anew, base, hh, 0.f);
       const float ms = move_max(max_across_halves(fmaxf(row_max(s[0]), row_max(s[1]))));
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) s[kb] -= ms;
@@ -530,11 +532,14 @@ hipError_t launch_score(const HistArgs& a, int64_t slots, int64_t blocks, hipStr
 
 template <int D>
 hipError_t launch_dim(const HistArgs& a, int64_t slots, int64_t blocks, hipStream_t s) {
-  const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
-  if (cap && bias) return launch_score<D, kCap | kBias>(a, slots, blocks, s);
-  if (cap) return launch_score<D, kCap>(a, slots, blocks, s);
-  if (bias) return launch_score<D, kBias>(a, slots, blocks, s);
-  return launch_score<D, 0>(a, slots, blocks, s);
+  switch (score_of(a)) {
+    case kCap: return launch_score<D, kCap>(a, slots, blocks, s);
+    case kWideCap: return launch_score<D, kWideCap>(a, slots, blocks, s);
+    case kBias: return launch_score<D, kBias>(a, slots, blocks, s);
+    case kCap | kBias: return launch_score<D, kCap | kBias>(a, slots, blocks, s);
+    case kWideCap | kBias: return launch_score<D, kWideCap | kBias>(a, slots, blocks, s);
+    default: return launch_score<D, 0>(a, slots, blocks, s);
+  }
 }
 
 }  // namespace
