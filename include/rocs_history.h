@@ -142,11 +142,13 @@ int32_t rocs_paged_attention(const void* q, int64_t q_row_stride, const void* k_
  * so equal calls give equal tables. An operator that needs pages does all of
  * its work or none; it writes status[2]: {0, 0} when done, else
  *   ROCS_CACHE_NO_PAGES    status[1] = the pages that were missing
- *   ROCS_CACHE_TABLE_FULL  a slot would need more than table_width pages
+ *   ROCS_CACHE_TABLE_FULL  a slot would need more than table_width pages (in
+ *                          reserve also one that holds more than that already)
  *   ROCS_CACHE_BAD_SLOT    a slot outside [0, num_slots), one named twice (as
  *                          an entry of reserve, or a child of fork), a child
  *                          that is not empty or that is a parent as well, a
- *                          slot whose length cannot be one
+ *                          slot with a negative length, a parent with more
+ *                          rows than table_width pages hold
  * (the last cause in this list that holds). Nothing else is changed then.
  *
  * The lists of a call do not overlap the cache's arrays or its outputs.

@@ -153,9 +153,11 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(
       continue;
     }
     const int add = i == tid ? add0 : max(row_off[i + 1] - row_off[i], 0);
-    const int64_t now = pages_of((uint32_t)l + (uint32_t)add, page);
-    if (now > width) wide = 1;
-    want += now - pages_of(l, page);
+    if ((int64_t)l + add > width * page) {             // (below 2^31, so the rest is in 32 bits)
+      wide = 1;
+      continue;
+    }
+    want += pages_of(l + add, page) - pages_of(l, page);
   }
   if (want > 0) atomicAdd(&wanted, (unsigned long long)want);
   __syncthreads();
