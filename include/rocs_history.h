@@ -63,6 +63,15 @@ extern "C" {
  *   workspace    at least rocs_history_workspace_size(R, N, num_heads,
  *                kv_heads, head_dim, max_kv_len or num_kv_rows, dtype) bytes,
  *                256-byte aligned; may be NULL when that is 0. Scratch.
+ *                That size is the one call's: fewer requests, rows or keys may
+ *                need more (they are cut into more parts). One workspace for
+ *                calls of many sizes takes the largest of theirs, or
+ *                  4 (head_dim + 2) min(num_heads N P, C) + 512 bytes,
+ *                  P = min(256, ceil(max_kv_len / 256)),
+ *                  C = 524,288 (bf16 and head_dim a multiple of 8 up to 128)
+ *                      or 8,192 (all others),
+ *                which is enough for any number of requests and up to N rows
+ *                and max_kv_len keys.
  *
  * Fast path (bf16 MFMA kernels): bf16, head_dim a multiple of 8 up to 128
  * (fastest at 64 and 128), strides multiples of 8 elements, pointers 16-byte
@@ -105,7 +114,9 @@ int32_t rocs_history_attention(const void* q, int64_t q_row_stride, const void* 
  *   slots        [R] int32, the slot of each request, or NULL: request r is
  *                slot r (then R <= num_slots)
  *   max_kv_len   an upper bound on the lengths, or 0 for the table's width
- * Every other argument, the result, the workspace and the limits are those of
+ *   workspace    sized as above with min(max_kv_len, table_width * page_size)
+ *                keys, or that product without a bound
+ * Every other argument, the result and the limits are those of
  * rocs_history_attention. Page ids and slots are device data: one outside its
  * range is clamped into it (wrong rows, never an access outside the pages).
  * Rows of a page past a history's end are not read.

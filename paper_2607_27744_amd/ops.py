@@ -785,6 +785,9 @@ def _launch(device, stream, name, *args):
 
 
 def history_workspace_size(num_requests, num_rows, heads, kv_heads, head_dim, max_kv_len, dtype):
+    """Bytes of workspace of one history_attention call over at most max_kv_len keys a request, or
+    of a paged_attention call (there at most table width * page size keys). A smaller call may
+    need more: include/rocs_history.h has a bound for one workspace under calls of many sizes."""
     code = _lib.DTYPE_BF16 if dtype == torch.bfloat16 else _lib.DTYPE_F32
     return int(_lib.load().rocs_history_workspace_size(num_requests, num_rows, heads, kv_heads,
                                                        head_dim, max_kv_len, code))
