@@ -212,7 +212,7 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
       l += pl[w][i] * f;
       y += *reinterpret_cast<const f32x4*>(&po[w][i][d0]) * f;
     }
-    if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3]))) odd[i] = 1;
+    if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3])) && may_differ(l, D, DP)) odd[i] = 1;
     const int rw = t.row0 + i;
     const int64_t at = (t.q0 + rw / a.G) * a.H + hk * a.G + rw % a.G;
     if (a.splits > 1 && d0 == 0) {

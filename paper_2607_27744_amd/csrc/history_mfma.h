@@ -55,8 +55,8 @@ struct KeyFeed {
 // at 1e5 it would be 0.02, at 1e8 all scores one value). Caps above kCapTurn
 // therefore take another form, whose error is relative to the score as that of the
 // score itself is. It costs more instructions (16 requests of 2,048 rows, 8 heads x
-// 128, causal: 207 us, 195 with a cap of 30, 167 without one), so the caps in use
-// keep this form. The bias in a stage that lies wholly before a row needs no
+// 128, causal: 207 us, 195 with a cap of 30, 167 without one; 370 where all stages
+// hold scores past a quarter of the cap), so the caps in use keep this form. The bias in a stage that lies wholly before a row needs no
 // distance: -slope (p - j) is linear in j.
 // ---------------------------------------------------------------------------
 struct RowRule {

@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void h
       l += pl[w][i] * f;
       y += *reinterpret_cast<const ROCS_LDS f32x4*>(lds3 + w * 2 * STAGE + i * D * 4 + 16 * (piece ^ (i & 15))) * f;
     }
-    if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3]))) odd[hs][i] = 1;
+    if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3])) && may_differ(l, a.D, D)) odd[hs][i] = 1;
     const int rw = t.row0 + i;
     const int64_t at = (t.q0 + rw / a.G) * a.H + (hk0 + hs) * a.G + rw % a.G;
     const int64_t to = (int64_t)split * a.N * a.H + at;

@@ -464,7 +464,7 @@ history_tile(const HistArgs a, int64_t slots) {
   asm volatile("" : "+v"(lane_e));
   const int l32e = lane_e & 31, hhe = lane_e >> 5;
   const float l = sum_across_halves(l_part);
-  const uint64_t odd = __ballot(any_odd(oacc, l));
+  const uint64_t odd = __ballot(any_odd(oacc, l) && may_differ(l, a.D, D));
   const int mine = min(t.rows - wrow0, 32);
   uint32_t again = ((uint32_t)odd | (uint32_t)(odd >> 32)) & (mine == 32 ? ~0u : (1u << mine) - 1u);
   auto out_row = [&](int i) -> int64_t {                  // row i of the wave
