@@ -189,7 +189,7 @@ int32_t rocs_cache_reserve(const int32_t* slots, const int32_t* row_offsets, int
 
 /* Row m of x (x_row_stride bytes apart, row_bytes bytes) into row rows[m] of
  * one layer's pool of num_pool_rows rows. A row number outside the pool is
- * passed over; one that is named twice gets either row. */
+ * passed over; a pool row that is named twice holds any mix of the two. */
 int32_t rocs_cache_write(const void* x, int64_t x_row_stride, const int32_t* rows,
                          int64_t num_rows, void* pool, int64_t num_pool_rows, int64_t row_bytes,
                          void* stream);
@@ -221,8 +221,9 @@ int32_t rocs_cache_compact(int32_t* page_table, int64_t table_width, int64_t num
 
 /* Page src_pages[i] of src_pool into page dst_pages[i] of dst_pool, in every
  * layer (the pools may be one, or of different page counts). A pair with an id
- * outside its pool is passed over; a page written twice, or written and read,
- * in one call holds either content. page_bytes = page_size * row_bytes. */
+ * outside its pool is passed over. A page that is written twice in one call
+ * holds any mix of its sources, other ones in other layers; so does a copy of a
+ * page that the same call writes. page_bytes = page_size * row_bytes. */
 int32_t rocs_cache_copy(const int32_t* src_pages, const int32_t* dst_pages, int64_t entries,
                         const void* src_pool, int64_t src_num_pages, void* dst_pool,
                         int64_t dst_num_pages, int64_t num_layers, int64_t page_bytes,

@@ -1010,7 +1010,7 @@ def cache_reserve(slots, row_offsets, num_rows, page_table, lens, refs, page_siz
 def cache_write(x, rows, pool, *, stream=None):
     """rocs_cache_write: row m of x [M, ...] into pool row rows[m] (from cache_reserve) of one
     layer's pool [pages, page_size, ...]. x's rows may be strided; rows that are -1 are passed
-    over."""
+    over; a pool row that is named twice holds any mix of the two."""
     if (_binding or _native()).cache_write(x, rows, pool, stream) is not None:
         return pool
     _need(pool.dim() >= 3 and pool.is_contiguous() and pool.numel() > 0,
@@ -1091,7 +1091,8 @@ def cache_compact(page_table, lens, refs, pool, *, status=None, workspace=None, 
 
 def cache_copy(src_pages, dst_pages, src_pool, dst_pool=None, *, stream=None):
     """rocs_cache_copy: page src_pages[i] of src_pool into page dst_pages[i] of dst_pool (None: the
-    same pool), in every layer of [layers, pages, page_size, ...]."""
+    same pool), in every layer of [layers, pages, page_size, ...]. A page that is written twice in
+    one call, or read and written, leaves any mix of the contents (of each layer its own)."""
     dst_pool = src_pool if dst_pool is None else dst_pool
     layers, page, row_bytes = _cache_layers(src_pool, src_pool.shape[1])
     _need(_cache_layers(dst_pool, dst_pool.shape[1]) == (layers, page, row_bytes),
