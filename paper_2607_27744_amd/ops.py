@@ -961,11 +961,11 @@ def _cache_state(page_table, lens, refs):
     return page_table.shape[0], page_table.shape[1], refs.numel()
 
 
-def _cache_layers(pool, pages):
+def _cache_layers(pool, pages=None):
     """(layers, page_size, bytes of a row) of a pool [layers, pages, page_size, ...]."""
-    _need(pool.dim() >= 4 and pool.is_contiguous() and pool.shape[1] == pages
+    _need(pool.dim() >= 4 and pool.is_contiguous() and pages in (None, pool.shape[1])
           and pool.numel() > 0, "pool must be a contiguous [layers, pages, page_size, ...] tensor")
-    layers, _, page = pool.shape[:3]
+    layers, pages, page = pool.shape[:3]
     return layers, page, pool.numel() // (layers * pages * page) * pool.element_size()
 
 
@@ -1094,8 +1094,8 @@ def cache_copy(src_pages, dst_pages, src_pool, dst_pool=None, *, stream=None):
     same pool), in every layer of [layers, pages, page_size, ...]. A page that is written twice in
     one call, or read and written, leaves any mix of the contents (of each layer its own)."""
     dst_pool = src_pool if dst_pool is None else dst_pool
-    layers, page, row_bytes = _cache_layers(src_pool, src_pool.shape[1])
-    _need(_cache_layers(dst_pool, dst_pool.shape[1]) == (layers, page, row_bytes),
+    layers, page, row_bytes = _cache_layers(src_pool)
+    _need(_cache_layers(dst_pool) == (layers, page, row_bytes),
           "the pools must have the same layers and pages of the same size")
     _need(src_pool.dtype == dst_pool.dtype, "the pools must share one dtype")
     n = src_pages.numel()
