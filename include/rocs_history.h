@@ -78,7 +78,10 @@ extern "C" {
  * Fast path (bf16 MFMA kernels): bf16, head_dim a multiple of 8 up to 128
  * (fastest at 64 and 128), strides multiples of 8 elements, pointers 16-byte
  * aligned. Other cases run a general kernel (fp32 matrix instructions),
- * head_dim up to 256.
+ * head_dim up to 256. One kernel and one cut of the histories serve a whole
+ * call, by the average rows of a request and the bound on the lengths: single
+ * rows beside long chunks, or one very long history beside many short ones, are
+ * faster as calls of their own.
  * Limits: N * num_heads <= 2^30, num_heads < 2^16, num_kv_rows < 2^31.
  * ---------------------------------------------------------------------------
  */
