@@ -82,7 +82,9 @@ extern "C" {
  * call, by the average rows of a request and the bound on the lengths: single
  * rows beside long chunks, or one very long history beside many short ones, are
  * faster as calls of their own.
- * Limits: N * num_heads <= 2^30, num_heads < 2^16, num_kv_rows < 2^31.
+ * Limits: N * num_heads <= 2^30, num_heads < 2^16, num_kv_rows <= 2^31 - 4096,
+ * and fewer than 2^24 workgroups (of 128, 32 or, in the general kernel, 16 rows
+ * of one request and K/V head, times the parts that histories are cut into).
  * ---------------------------------------------------------------------------
  */
 size_t rocs_history_workspace_size(int64_t num_requests, int64_t num_rows, int32_t num_heads,
@@ -122,8 +124,9 @@ int32_t rocs_history_attention(const void* q, int64_t q_row_stride, const void* 
  *   workspace    sized as above with min(max_kv_len, table_width * page_size)
  *                keys, or that product without a bound
  * Every other argument, the result and the limits are those of
- * rocs_history_attention. Page ids and slots are device data: one outside its
- * range is clamped into it (wrong rows, never an access outside the pages).
+ * rocs_history_attention, and table_width * page_size <= 2^31 - 4096. Page ids
+ * and slots are device data: one outside its range is clamped into it (wrong
+ * rows, never an access outside the pages).
  * Rows of a page past a history's end are not read.
  *
  * Fast path: as above, with page_size a multiple of 16.

@@ -16,6 +16,9 @@ namespace {
 // Rows (token, head) of a call: their numbers, rounded up to a tile, stay in 32 bits.
 constexpr int64_t kMaxRows = int64_t(1) << 30;
 
+// Keys of a history: the kernels step past its end in 32 bits, by less than this.
+constexpr int64_t kMaxKeys = (int64_t(1) << 31) - 4096;
+
 // The checks that both attentions share, and the launch.
 int32_t attend(const char* name, HistArgs a, int64_t R, int64_t kv_rows, int64_t k_bytes,
                float scale, int64_t max_len, int32_t dtype, void* workspace, size_t workspace_bytes,
@@ -178,7 +181,7 @@ int32_t rocs_history_attention(const void* q, int64_t q_row_stride, const void* 
                                 max_kv_len, dtype);
   if (st != ROCS_OK) return st;
   if (num_kv_rows < 0) return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: num_kv_rows < 0", name);
-  if (num_kv_rows > kMaxI32) return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
+  if (num_kv_rows > kMaxKeys) return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
   if ((q_docs == nullptr) != (kv_docs == nullptr))
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: q_docs and kv_docs go together", name);
   if (N == 0) return ok();
@@ -215,9 +218,9 @@ int32_t rocs_paged_attention(const void* q, int64_t q_row_stride, const void* k_
   if (table_width < 1 || num_slots < 0 || num_pages < 1 || page_size < 1 || page_stride < 0)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: table_width, num_pages and page_size must be at "
                 "least 1", name);
-  if (table_width > kMaxI32 || table_width * page_size > kMaxI32 || num_pages > kMaxI32 ||
+  if (table_width > kMaxI32 || table_width * page_size > kMaxKeys || num_pages > kMaxI32 ||
       num_slots > kMaxI32)
-    return fail(ROCS_ERR_UNSUPPORTED, "%s: table_width * page_size must stay below 2^31", name);
+    return fail(ROCS_ERR_UNSUPPORTED, "%s: table_width * page_size must not pass 2^31 - 4096", name);
   const int64_t kv_stride = kv_row_stride != 0 ? kv_row_stride : (int64_t)Hk * D;
   const int64_t extent = (page_size - 1) * kv_stride + (int64_t)Hk * D;      // of one page
   if (page_stride != 0 && page_stride < extent)
