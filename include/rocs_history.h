@@ -21,8 +21,9 @@
  *   A row that sees no key (or whose seen scores are all -inf) is zero. Keys
  *   that a row does not see have no part in it, whatever they hold: infinities
  *   and NaN there do not reach the row.
- *   Infinities and NaN in V cost time: a row whose tile meets one is formed
- *   again by a slow path (200 to 600 times a long call's time where all rows do).
+ *   Infinities and NaN in V cost time (in q and K too, at head_dims that are
+ *   not the kernels' own 64 and 128): a row whose tile meets one is formed again
+ *   by a slow path, 200 to 600 times a long call's time where all rows do.
  *   Scores, softmax and sums are fp32; the bf16 kernels round the softmax
  *   weights to bf16 for the product with V and sum the rounded weights. Their
  *   cap adds an error of at most 2^-22 cap to a score for caps up to 128, and of

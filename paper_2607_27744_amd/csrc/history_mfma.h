@@ -56,8 +56,9 @@ struct KeyFeed {
 // therefore take another form, whose error is relative to the score as that of the
 // score itself is. It costs more instructions (16 requests of 2,048 rows, 8 heads x
 // 128, causal: 207 us, 195 with a cap of 30, 167 without one; 370 where all stages
-// hold scores past a quarter of the cap), so the caps in use keep this form. The bias in a stage that lies wholly before a row needs no
-// distance: -slope (p - j) is linear in j.
+// hold scores past a quarter of the cap), so the caps in use keep this form.
+// The bias in a stage that lies wholly before a row needs no distance: -slope
+// (p - j) is linear in j.
 // ---------------------------------------------------------------------------
 struct RowRule {
   float scale2;            // scale log2(e)

@@ -199,8 +199,9 @@ history_tile(const HistArgs a, int64_t slots) {
   // Weights of step ps as packed bf16 B fragments, from scores in exp2 units less
   // the max. bf16 weights let their product with V run at eight times the
   // rate of the fp32 instruction; the row's sum adds the rounded weights, so that
-  // a common part of the rounding cancels. Results are off by 2.1e-3 relative against
-  // 1.7e-3 with exact weights, most of it their own rounding to bf16. Each pair is a scalar of its own (see dca_attn_bf16).
+  // a common part of the rounding cancels. Results are off by 2.1e-3 relative,
+  // 1.7e-3 of it their own rounding to bf16 (the errors' squares add). Each pair
+  // is a scalar of its own (see dca_attn_bf16).
   const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
   auto weights = [&](const f32x16 (&s)[KB], int ps, uint32_t (&pk)[4], float& sum) __attribute__((always_inline)) {
 #pragma unroll
