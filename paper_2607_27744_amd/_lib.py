@@ -1,5 +1,5 @@
-"""ctypes loader for librocs.so and the declarations of its C ABI (include/rocs.h
-and include/rocs_history.h)."""
+"""ctypes loader for librocs.so and the declarations of its C ABI (include/rocs.h,
+include/rocs_history.h and include/rocs_layer.h)."""
 
 import ctypes
 import os
@@ -80,6 +80,25 @@ HISTORY_SIGNATURES = {
                                   _size, _vp]),
     "rocs_cache_copy": (_i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp]),
 }
+
+# name -> (restype, argtypes), mirroring include/rocs_layer.h
+LAYER_SIGNATURES = {
+    "rocs_adapter_workspace_size": (_size, [_i64, _i64, _i64, _i64, _i32, _i32]),
+    "rocs_adapter_linear": (_i32, [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64,
+                                   _i64, _i32, _i64, _i32, _i32, _vp, _vp, _size, _vp]),
+    "rocs_rotate": (_i32, [_vp, _i64, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i32,
+                           _i32, _i32, _vp, _vp]),
+    "rocs_cache_append": (_i32, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp,
+                                 _i64, _i64, _i64, _i32, _i32, _i32, _i32, _vp, _i64, _i32, _vp,
+                                 _vp]),
+    "rocs_fp4_row_bytes": (_size, [_i32, _i32]),
+    "rocs_cache_read_fp4": (_i32, [_vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _vp]),
+    "rocs_paged_fp4_workspace_size": (_size, [_i64, _i64, _i32, _i32, _i32, _i64, _i32]),
+    "rocs_paged_attention_fp4": (_i32, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp,
+                                        _i64, _i64, _i64, _i32, _i32, _i32, _i32, _f32, _f32, _i32,
+                                        _i64, _i32, _vp, _vp, _size, _vp]),
+}
+POOL_ROWS, POOL_FP4 = 0, 1
 CACHE_NO_PAGES, CACHE_TABLE_FULL, CACHE_BAD_SLOT = 1, 2, 3   # status[0] of the page operators
 
 ABI_VERSION = 5
@@ -107,7 +126,7 @@ def load(path=LIB_PATH):
             f"{path} is missing: build it with `python -c 'import __graft_entry__ as g; "
             "g.build()'` (hipcc, gfx950). There is no fallback implementation.")
     lib = ctypes.CDLL(path)
-    for name, (res, args) in {**SIGNATURES, **HISTORY_SIGNATURES}.items():
+    for name, (res, args) in {**SIGNATURES, **HISTORY_SIGNATURES, **LAYER_SIGNATURES}.items():
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args

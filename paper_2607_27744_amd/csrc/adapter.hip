@@ -1,0 +1,141 @@
+// A shared projection with the low-rank adapter of each row's request beside it:
+//
+//   out[n] = act( W x[n] + bias + B_a t[n] ),  t[n] = s_a A_a x[n],  a = ids[request of n]
+//
+// t comes first, in a launch of its own (every output column needs all of it).
+#include "common.h"
+#include "launch.h"
+#include "layer.h"
+
+namespace rocs {
+namespace {
+
+__device__ __forceinline__ int64_t rows_of(const AdapterArgs& a) {
+  return min(a.N, max((int64_t)a.off[a.R], (int64_t)0));
+}
+
+// Adapter of row n, -1: none.
+__device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t n) {
+  const int id = a.ids[owner_of(a.off, a.R, n)];
+  return (uint32_t)id < (uint32_t)a.A ? id : -1;
+}
+
+// ---------------------------------------------------------------------------
+// General path: any dtype, sizes and alignment; t in fp32.
+// ---------------------------------------------------------------------------
+
+// A wave a row: four of the row's rank at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void shrink_general(const AdapterArgs a, int cols) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n_rows = rows_of(a);
+  for (int64_t n = (int64_t)blockIdx.x * 4 + wave; n < n_rows; n += (int64_t)gridDim.x * 4) {
+    const int id = adapter_of(a, n);
+    if (id < 0) continue;
+    const T* x = static_cast<const T*>(a.x) + n * a.x_stride;
+    const T* w = static_cast<const T*>(a.a) + (int64_t)id * a.rank * a.K;
+    const float s = a.scales != nullptr ? a.scales[id] : 1.f;
+    float* t = static_cast<float*>(a.t) + n * cols;
+    for (int j0 = 0; j0 < a.rank; j0 += 4) {
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int k = lane; k < a.K; k += 64) {
+        const float xv = load_f32(x + k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          sum[i] += xv * load_f32(w + (int64_t)min(j0 + i, a.rank - 1) * a.K + k);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum[i] += __shfl_xor(sum[i], o);
+        if (lane == 0 && j0 + i < a.rank) t[j0 + i] = s * sum[i];
+      }
+    }
+  }
+}
+
+// A 16 x 16 tile (features x rows) a workgroup and step; its four waves split K and
+// the rank, and add up through LDS in a fixed order. Products as in the general
+// linear: the fp32 matrix instruction, operands from global memory, four
+// consecutive k a lane.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void adapter_general(const AdapterArgs a, int cols, int tiles_m,
+                                                       int64_t tiles) {
+  __shared__ f32x4 red[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int l = lane & 15, g = lane >> 4;
+  const int64_t n_rows = rows_of(a);
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int d0 = (int)(tile % tiles_m) * 16;
+    const int64_t n0 = tile / tiles_m * 16;
+    if (n0 >= n_rows) return;              // the later tiles lie behind the rows as well
+    const int d = d0 + l;
+    const int64_t n = n0 + l;
+    const bool dok = d < a.D, nok = n < n_rows;
+    const T* x = static_cast<const T*>(a.x) + n * a.x_stride;
+    const T* w = static_cast<const T*>(a.w) + (int64_t)d * a.K;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 16 * wave + 4 * g; k < (a.K + 15) / 16 * 16; k += 64) {
+      const int left = a.K - k;
+      const f32x4 av = load4_f32<T, VEC>(w + k, dok ? left : 0);
+      const f32x4 bv = load4_f32<T, VEC>(x + k, nok ? left : 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(av[i], bv[i], acc, 0, 0, 0);
+    }
+    // Element i: feature d0 + 4 g + i of row n.
+    const int id = nok ? adapter_of(a, n) : -1;
+    if (id >= 0) {
+      const T* b = static_cast<const T*>(a.b) + ((int64_t)id * a.D + d0 + 4 * g) * a.rank;
+      const float* t = static_cast<const float*>(a.t) + n * cols;
+      for (int j = wave; j < a.rank; j += 4) {
+        const float tv = t[j];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (d0 + 4 * g + i < a.D) acc[i] += tv * load_f32(b + (int64_t)i * a.rank + j);
+      }
+    }
+    red[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0 && nok) {
+      f32x4 s = ((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int df = d0 + 4 * g + i;
+        if (df >= a.D) break;
+        if (a.bias != nullptr) s[i] += a.bias[df];
+        if (a.relu) s[i] = fmaxf(s[i], 0.f);
+        static_cast<T*>(a.out)[n * a.D + df] = from_f32<T>(s[i]);
+      }
+    }
+    __syncthreads();                       // red is free for the next tile
+  }
+}
+
+template <typename T>
+hipError_t launch_general(const AdapterArgs& a, hipStream_t s) {
+  const int cols = adapter_cols(a.rank);
+  if (a.A > 0) {
+    const int64_t blocks = (a.N + 3) / 4 < (1 << 20) ? (a.N + 3) / 4 : 1 << 20;
+    const hipError_t e = launch_kernel(shrink_general<T>, dim3((uint32_t)blocks), dim3(256), s, a, cols);
+    if (e != hipSuccess) return e;
+  }
+  const int tiles_m = (a.D + 15) / 16;
+  const int64_t tiles = (a.N + 15) / 16 * tiles_m;
+  const uint32_t grid = (uint32_t)(tiles < (1 << 20) ? tiles : 1 << 20);
+  auto ok = [](const void* p, int64_t stride) {
+    return stride % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0;
+  };
+  const bool vec = a.K % 4 == 0 && ok(a.x, a.x_stride) && ok(a.w, 0);
+  return launch_kernel(vec ? adapter_general<T, true> : adapter_general<T, false>, dim3(grid),
+                       dim3(256), s, a, cols, tiles_m, tiles);
+}
+
+}  // namespace
+
+hipError_t launch_adapter(const AdapterArgs& a, bool fast, hipStream_t s) {
+  (void)fast;
+  return a.bf16 ? launch_general<bf16_t>(a, s) : launch_general<float>(a, s);
+}
+
+}  // namespace rocs

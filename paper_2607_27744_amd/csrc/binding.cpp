@@ -15,7 +15,7 @@
 #include <ATen/Functions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
-#include "../../include/rocs_history.h"
+#include "../../include/rocs_layer.h"
 
 namespace {
 
@@ -769,6 +769,149 @@ PyObject* cache_compact(PyObject* const* a) {
   return result(a[4], status);
 }
 
+// --- adapters, rotated rows, a cache in 4 bits --------------------------------
+
+// x, w, a, b, offsets, adapter_ids, scales, bias, activation, out, workspace, stream
+PyObject* adapter(PyObject* const* a) {
+  Call c(a[11]);
+  const Ten x = c.must(a[0]), w = c.must(a[1]), la = c.must(a[2]), lb = c.must(a[3]),
+            off = c.must(a[4]), ids = c.must(a[5]), scales = c.get(a[6]), bias = c.get(a[7]);
+  on_current_device(c);
+  need(x->dim() == 2 && w->dim() == 2 && la->dim() == 3 && lb->dim() == 3);
+  const int64_t n = x->size(0), k = x->size(1), d = w->size(0), count = la->size(0), rank = la->size(1);
+  need(w->size(1) == k && k >= 1 && d >= 1 && rank >= 1 && rank <= INT32_MAX && lb->size(0) == count &&
+       la->size(2) == k && lb->size(1) == d && lb->size(2) == rank);
+  const int32_t code = dtype_code(x), act = activation(a[8]);
+  const c10::ScalarType type = x->scalar_type();
+  need(w->scalar_type() == type && la->scalar_type() == type && lb->scalar_type() == type);
+  need(w->is_contiguous() && la->is_contiguous() && lb->is_contiguous());
+  need((k == 1 || x->stride(1) == 1) && (n <= 1 || x->stride(0) >= k));
+  const int64_t r = off->numel() - 1;
+  need(r >= 0);
+  offsets(off, r);
+  int_vector(ids, r);
+  need(!scales || (scales->scalar_type() == c10::kFloat && scales->dim() == 1 &&
+                   scales->size(0) == count && scales->is_contiguous()));
+  need(!bias || (bias->scalar_type() == c10::kFloat && bias->dim() == 1 && bias->size(0) == d &&
+                 bias->is_contiguous()));
+  const Ten out = c.or_new(a[9], {n, d}, type);
+  const Ten ws = scratch(c, a[10], rocs_adapter_workspace_size(r, n, k, d, (int32_t)rank, code));
+  void* s = stream_of(c.stream);
+  run("rocs_adapter_linear", rocs_adapter_linear, x.ptr(), n > 1 ? x->stride(0) : 0, w.ptr(),
+      la.ptr(), lb.ptr(), scales.f32(), bias.f32(), off.i32(), ids.i32(), r, n, k, d, (int32_t)rank,
+      count, code, act, data(out), data(ws), nbytes(ws), s);
+  return result(a[9], out);
+}
+
+// k, v, rows, pool, freqs, q, positions, offsets, slots, lens, interleaved,
+// q_out, stream
+PyObject* append(PyObject* const* a) {
+  Call c(a[12]);
+  const Ten k = c.must(a[0]), v = c.must(a[1]), rows = c.must(a[2]), pool = c.must(a[3]),
+            freqs = c.get(a[4]), q = c.get(a[5]), pos = c.get(a[6]), off = c.get(a[7]),
+            slots = c.get(a[8]), lens = c.get(a[9]);
+  on_current_device(c);
+  need(k->dim() == 3 && k->sizes() == v->sizes() && k->scalar_type() == v->scalar_type());
+  const int64_t m = k->size(0), hk = k->size(1), d = k->size(2);
+  need(hk >= 1 && d >= 1 && hk <= INT32_MAX && d <= INT32_MAX);
+  const int32_t code = dtype_code(k), inter = truth(a[10]);
+  const int64_t stride = row_stride(k);
+  need(row_stride(v) == stride);
+  int_vector(rows, m);
+  int_vector(pos, m);
+  int64_t rot = 0, r = 0, n_slots = 0;
+  if (freqs) {
+    need(freqs->scalar_type() == c10::kFloat && freqs->dim() == 1 && freqs->is_contiguous() &&
+         2 * freqs->numel() <= d);
+    rot = 2 * freqs->numel();
+  }
+  if (off) {
+    r = off->numel() - 1;
+    need(r >= 0);
+    offsets(off, r);
+    int_vector(slots, r);
+    if (lens) {
+      n_slots = lens->numel();
+      int_vector(lens, n_slots);
+      need(slots || r <= n_slots);
+    }
+  } else {
+    need(!slots && !lens);
+  }
+  need(rot == 0 || pos || (off && lens));
+  int32_t form = ROCS_POOL_ROWS;
+  need(pool->is_contiguous() && pool->dim() >= 3 && pool->size(0) >= 1 && pool->size(1) >= 1);
+  const int64_t pool_rows = pool->size(0) * pool->size(1);
+  if (pool->scalar_type() == c10::kByte) {
+    form = ROCS_POOL_FP4;
+    const int64_t row = (int64_t)rocs_fp4_row_bytes((int32_t)hk, (int32_t)d);
+    need(pool->dim() == 3 && row > 0 && pool->size(2) == row);
+  } else {
+    need(pool->scalar_type() == k->scalar_type() && pool->dim() == 5 && pool->size(2) == 2 &&
+         pool->size(3) == hk && pool->size(4) == d);
+  }
+  int64_t h = 0, q_stride = 0;
+  Ten q_out;
+  need(q || a[11] == Py_None);
+  if (q) {
+    need(q->dim() == 3 && q->size(0) == m && q->size(1) >= 1 && q->size(1) <= INT32_MAX &&
+         q->size(2) == d && q->scalar_type() == k->scalar_type());
+    h = q->size(1);
+    q_stride = row_stride(q);
+    q_out = c.or_new(a[11], q->sizes(), q->scalar_type());
+  }
+  void* s = stream_of(c.stream);
+  run("rocs_cache_append", rocs_cache_append, q.ptr(), q_stride, k.ptr(), v.ptr(), stride,
+      rows.i32(), freqs.f32(), (int32_t)rot, inter, pos.i32(), off.i32(), slots.i32(), lens.i32(), r,
+      n_slots, m, (int32_t)h, (int32_t)hk, (int32_t)d, code, pool.ptr(), pool_rows, form,
+      data(q_out), s);
+  if (!q) Py_RETURN_TRUE;
+  return result(a[11], q_out);
+}
+
+// q, pages, page_table, kv_lens, q_offsets, kv_heads, slots, causal,
+// prefix_lens, slopes, cap, max_kv_len, scale, out, workspace, stream
+PyObject* paged_fp4(PyObject* const* a) {
+  Call c(a[15]);
+  const Ten q = c.must(a[0]), pages = c.must(a[1]), table = c.must(a[2]), lens = c.must(a[3]),
+            qo = c.must(a[4]), slots = c.get(a[6]), prefix = c.get(a[8]), slopes = c.get(a[9]);
+  on_current_device(c);
+  need(q->dim() == 3);
+  const int64_t n = q->size(0), h = q->size(1), d = q->size(2), hk = integer(a[5]);
+  need(hk >= 1 && hk <= h && h <= INT32_MAX && h % hk == 0 && d <= INT32_MAX);
+  const int32_t code = dtype_code(q), causal = truth(a[7]);
+  const int64_t row = (int64_t)rocs_fp4_row_bytes((int32_t)hk, (int32_t)d);
+  need(row > 0 && pages->scalar_type() == c10::kByte && pages->dim() == 3 && pages->is_contiguous() &&
+       pages->size(2) == row && pages->size(0) >= 1 && pages->size(1) >= 1 &&
+       pages->size(1) <= INT32_MAX);
+  const int64_t n_pages = pages->size(0), page = pages->size(1), r = qo->numel() - 1;
+  need(r >= 0);
+  offsets(qo, r);
+  int_vector(prefix, r);
+  int_vector(slots, r);
+  need(!slopes || (slopes->scalar_type() == c10::kFloat && slopes->dim() == 1 &&
+                   slopes->size(0) == h && slopes->is_contiguous()));
+  const float cap = scale_of(a[10]), scale = scale_of(a[12]);
+  need(cap == 0.f || (cap >= 1e-30f && cap < 3.4e38f));
+  const int64_t most = count_of(a[11]);
+  need(table->scalar_type() == c10::kInt && table->dim() == 2 && table->is_contiguous() &&
+       table->size(1) >= 1);
+  const int64_t n_slots = table->size(0), width = table->size(1);
+  need(width <= INT32_MAX / page);
+  int_vector(lens, n_slots);
+  need(slots || r <= n_slots);
+  const int64_t qs = row_stride(q), all = width * page, bound = most > 0 && most < all ? most : all;
+  const Ten out = c.or_new(a[13], q->sizes(), q->scalar_type());
+  const Ten ws = scratch(c, a[14], rocs_paged_fp4_workspace_size(r, n, (int32_t)h, (int32_t)hk,
+                                                                 (int32_t)d, bound, code));
+  void* s = stream_of(c.stream);
+  run("rocs_paged_attention_fp4", rocs_paged_attention_fp4, q.ptr(), qs, pages.ptr(), table.i32(),
+      width, lens.i32(), slots.i32(), n_slots, qo.i32(), prefix.i32(), slopes.f32(), r, n, n_pages,
+      (int32_t)page, (int32_t)h, (int32_t)hk, (int32_t)d, scale, cap, causal, most, code, data(out),
+      data(ws), nbytes(ws), s);
+  return result(a[13], out);
+}
+
 #define ROCS_ENTRY(name, n) \
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<n, name>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
@@ -776,7 +919,9 @@ PyMethodDef g_methods[] = {
     ROCS_ENTRY(fm_linear, 10), ROCS_ENTRY(lcb, 11),        ROCS_ENTRY(plan, 7),
     ROCS_ENTRY(attention, 16), ROCS_ENTRY(history, 16),    ROCS_ENTRY(paged, 16),
     ROCS_ENTRY(cache_reserve, 11), ROCS_ENTRY(cache_write, 4), ROCS_ENTRY(cache_fork, 9),
-    ROCS_ENTRY(cache_free, 6), ROCS_ENTRY(cache_compact, 7), {nullptr, nullptr, 0, nullptr}};
+    ROCS_ENTRY(cache_free, 6), ROCS_ENTRY(cache_compact, 7),
+    ROCS_ENTRY(adapter, 12),  ROCS_ENTRY(append, 13),     ROCS_ENTRY(paged_fp4, 16),
+    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};
 

@@ -2,6 +2,7 @@
 // that cuts a call up, the general kernel and the join of a split history.
 #include "history_device.h"
 #include "launch.h"
+#include "layer.h"
 #include "status.h"
 
 namespace rocs {
@@ -45,13 +46,15 @@ __device__ __forceinline__ f32x4 row4(const T* row, int d, int D) {
 }
 
 // DP: head_dim rounded up to 32, 64, 128 or 256. VEC: rows of q, k and v are
-// aligned to four elements and head_dim is a multiple of four.
-template <typename T, int DP, bool VEC>
+// aligned to four elements and head_dim is a multiple of four. FP4: a cache in 4
+// bits, of which lane (l16, g) takes a quarter of key l16's dims, DP / 4 from DP / 4 g,
+// and the NB dims from NB l16 of V's keys, as PIPE does.
+template <typename T, int DP, bool VEC, bool FP4 = false>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void history_general(
     const HistArgs a) {
   constexpr int NB = DP / 16;              // 16-dim blocks
-  constexpr bool PIPE = VEC && DP <= 128;
+  constexpr bool PIPE = VEC && DP <= 128 && !FP4;
   constexpr int LP = DP + 4;               // LDS row (floats), padded against bank conflicts
   __shared__ __attribute__((aligned(16))) float po[4][kGenTile][LP];
   __shared__ float pm[4][kGenTile], pl[4][kGenTile];
@@ -79,7 +82,7 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
   const T* v = static_cast<const T*>(a.v) + (int64_t)hk * D;
   f32x4 qf[NB];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) qf[b] = row4<T, VEC>(q, 16 * b + 4 * g, D);
+  for (int b = 0; b < NB; ++b) qf[b] = row4<T, VEC>(q, FP4 ? 4 * NB * g + 4 * b : 16 * b + 4 * g, D);
   float m = -INFINITY, lsum = 0.f;
   f32x4 o[NB];
 #pragma unroll
@@ -110,7 +113,47 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
 #pragma unroll
     for (int b = 0; b < NB; ++b) o[b] *= alpha;
   };
-  if constexpr (PIPE) {
+  if constexpr (FP4) {
+    // Words of eight values; past the head the last ones stand in, where q is 0 and
+    // the result is not stored.
+    const Fp4Row fr{a.Hk, D};
+    const char* base = static_cast<const char*>(a.k);
+    constexpr int WORDS = (DP / 4 + 7) / 8, VW = (NB + 7) / 8;
+    for (int kb = lo + 16 * wave; kb < hi; kb += 64) {
+      const char* kr = base + key_row(a, t, min(kb + l16, hi - 1));
+      const char* vr[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vr[i] = base + key_row(a, t, min(kb + 4 * g + i, hi - 1));
+      uint32_t vw[4][VW];
+      float vs[4][VW];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < VW; ++c) {
+          const int d = min(NB * l16 + 8 * c, D - 1);
+          vw[i][c] = *reinterpret_cast<const uint32_t*>(vr[i] + fr.values(1, hk) + d / 8 * 4) >> (4 * (d % 8));
+          vs[i][c] = fp4_scale((uint8_t)vr[i][fr.scales(1, hk) + d / kFp4Block]);
+        }
+      f32x4 part[4] = {};
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) {
+        const int d = min(DP / 4 * g + 8 * w, D - 8);
+        const uint32_t word = *reinterpret_cast<const uint32_t*>(kr + fr.values(0, hk) + d / 2);
+        const float ks = fp4_scale((uint8_t)kr[fr.scales(0, hk) + d / kFp4Block]);
+#pragma unroll
+        for (int i = 0; i < (DP / 4 < 8 ? DP / 4 : 8); ++i)
+          part[i % 4] = __builtin_amdgcn_mfma_f32_16x16x4f32(fp4_value(word, i, ks), qf[2 * w + i / 4][i % 4],
+                                                             part[i % 4], 0, 0, 0);
+      }
+      f32x4 p;
+      softmax(kb, (part[0] + part[1]) + (part[2] + part[3]), p);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fp4_value(vw[i][b / 8], b % 8, vs[i][b / 8]), p[i], o[b], 0, 0, 0);
+    }
+  } else if constexpr (PIPE) {
     constexpr int NV = NB < 4 ? NB : 4;    // dims of one V load
     auto key_at = [&](int j) __attribute__((always_inline)) { return key_row(a, t, min(j, hi - 1)); };
     int64_t kr = 0, vr[4] = {};
@@ -190,12 +233,12 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
     pm[wave][l16] = m;
     pl[wave][l16] = lsum;
   }
-  // Element i of o[b] is dim 16 b + 4 g + i of row l16, or (PIPE) NB (4 g + i) + b.
+  // Element i of o[b] is dim 16 b + 4 g + i of row l16, or (PIPE, FP4) NB (4 g + i) + b.
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      po[wave][l16][PIPE ? NB * (4 * g + i) + b : 16 * b + 4 * g + i] = o[b][i];
+      po[wave][l16][PIPE || FP4 ? NB * (4 * g + i) + b : 16 * b + 4 * g + i] = o[b][i];
   __syncthreads();
   // Merge the four partial softmaxes, four dims a step.
   const int64_t part0 = (int64_t)split * a.N * a.H;
@@ -233,7 +276,7 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
   __syncthreads();
   for (int i = wave; i < t.rows; i += 4)
     if (__builtin_amdgcn_readfirstlane(odd[i]) != 0)
-      redo_row<T>(a, t, t.row0 + i, hk, lo, hi, split, direct);
+      redo_row<T, FP4>(a, t, t.row0 + i, hk, lo, hi, split, direct);
 }
 
 // ---------------------------------------------------------------------------
@@ -322,6 +365,24 @@ hipError_t launch_general(const HistArgs& a, hipStream_t s) {
                        dim3((uint32_t)slots, (uint32_t)a.Hk, (uint32_t)a.splits), dim3(256), s, a);
 }
 
+// A 4-bit cache: head_dim is a multiple of 32, so q's rows are aligned to four
+// elements if its pointer and stride are.
+template <typename T, int DP>
+hipError_t launch_general_fp4(const HistArgs& a, hipStream_t s) {
+  const int64_t slots = a.R + (a.N * a.G + kGenTile - 1) / kGenTile;
+  if (!grid_fits(slots, 256)) return hipErrorInvalidConfiguration;
+  const bool vec = a.q_stride % 4 == 0 && reinterpret_cast<uintptr_t>(a.q) % (4 * sizeof(T)) == 0;
+  return launch_kernel(vec ? history_general<T, DP, true, true> : history_general<T, DP, false, true>,
+                       dim3((uint32_t)slots, (uint32_t)a.Hk, (uint32_t)a.splits), dim3(256), s, a);
+}
+template <typename T>
+hipError_t launch_general_fp4(const HistArgs& a, hipStream_t s) {
+  if (a.D <= 32) return launch_general_fp4<T, 32>(a, s);
+  if (a.D <= 64) return launch_general_fp4<T, 64>(a, s);
+  if (a.D <= 128) return launch_general_fp4<T, 128>(a, s);
+  return launch_general_fp4<T, 256>(a, s);
+}
+
 template <typename T>
 hipError_t launch_general(const HistArgs& a, hipStream_t s) {
   if (a.D <= 32) return launch_general<T, 32>(a, s);
@@ -401,6 +462,19 @@ hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hip
                  : fast && rows == 32 ? launch_history_split(a, s)
                  : bf16              ? launch_general<bf16_t>(a, s)
                                      : launch_general<float>(a, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  return bf16 ? launch_join<bf16_t>(a, s) : launch_join<float>(a, s);
+}
+
+HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
+  (void)bf16;
+  return history_plan(R, N, H, Hk, D, max_len, false);
+}
+
+hipError_t launch_history_fp4(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s) {
+  (void)rows;
+  (void)fast;
+  const hipError_t e = bf16 ? launch_general_fp4<bf16_t>(a, s) : launch_general_fp4<float>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
   return bf16 ? launch_join<bf16_t>(a, s) : launch_join<float>(a, s);
 }

@@ -1,7 +1,7 @@
 // Device-side parts shared by the history attention kernels.
 #pragma once
 
-#include "common.h"
+#include "fp4.h"
 #include "history.h"
 
 namespace rocs {
@@ -65,7 +65,7 @@ __device__ __forceinline__ bool tile_alone(const HistArgs& a, int most) {
 }
 constexpr float kDone = -1.f;
 
-// Element offset of K/V row j (of all heads).
+// Element offset of K/V row j (of all heads); in a 4-bit pool the byte offset.
 __device__ __forceinline__ int64_t key_row(const HistArgs& a, const HistTile& t, int j) {
   if (t.pages == nullptr) return (t.kv0 + j) * a.kv_stride;
   const int c = (int)((uint32_t)j / (uint32_t)a.page_size);
@@ -94,14 +94,25 @@ __device__ __forceinline__ float wave_sum(float v) {
 // Results as the partial form: max in log2 units, sum, and dims lane, lane + 64, ..
 // of the weighted sum.
 // ---------------------------------------------------------------------------
-template <typename T>
+
+// Dim d of K (v 0) or V (1) of head hk in the K/V row at `at`.
+template <typename T, bool FP4>
+__device__ __forceinline__ float kv_value(const HistArgs& a, int64_t at, int v, int hk, int d) {
+  if constexpr (FP4) {
+    const Fp4Row fr{a.Hk, a.D};
+    const uint8_t* row = static_cast<const uint8_t*>(a.k) + at;
+    return fp4_value(row[fr.values(v, hk) + d / 2], d & 1, fp4_scale(row[fr.scales(v, hk) + d / kFp4Block]));
+  } else {
+    return load_f32(static_cast<const T*>(v ? a.v : a.k) + (int64_t)hk * a.D + at + d);
+  }
+}
+
+template <typename T, bool FP4>
 __device__ __forceinline__ void lone_row(const HistArgs& a, const HistTile& t, int row, int hk,
                                          int lo, int hi, float& m, float& l, float (&acc)[4]) {
   const int lane = (int)(threadIdx.x & 63);
   const int token = row / a.G, h = hk * a.G + row % a.G;
   const T* q = static_cast<const T*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)h * a.D;
-  const T* k = static_cast<const T*>(a.k) + (int64_t)hk * a.D;
-  const T* v = static_cast<const T*>(a.v) + (int64_t)hk * a.D;
   const int pos = position_of(t, token);
   hi = min(hi, limit_of(a, t, token));
   const float slope = a.slopes != nullptr ? a.slopes[h] : 0.f;
@@ -117,7 +128,7 @@ __device__ __forceinline__ void lone_row(const HistArgs& a, const HistTile& t, i
     float s = -INFINITY;
     if (seen) {
       s = 0.f;
-      for (int d = 0; d < a.D; ++d) s += load_f32(q + d) * load_f32(k + at + d);
+      for (int d = 0; d < a.D; ++d) s += load_f32(q + d) * kv_value<T, FP4>(a, at, 0, hk, d);
       s *= a.scale;
       if (a.cap > 0.f) s = a.cap * tanhf(s / a.cap);
       if (a.slopes != nullptr) s -= slope * fabsf((float)(pos - j));
@@ -138,18 +149,18 @@ __device__ __forceinline__ void lone_row(const HistArgs& a, const HistTile& t, i
       const int64_t row_at = __shfl(at, i);
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (lane + 64 * c < a.D) acc[c] += pj * load_f32(v + row_at + lane + 64 * c);
+        if (lane + 64 * c < a.D) acc[c] += pj * kv_value<T, FP4>(a, row_at, 1, hk, lane + 64 * c);
     }
   }
   m *= kLog2e;
 }
 
 // The lone row's result where the kernel's own would have gone.
-template <typename T>
+template <typename T, bool FP4 = false>
 __device__ __forceinline__ void redo_row(const HistArgs& a, const HistTile& t, int row, int hk,
                                          int lo, int hi, int split, bool direct) {
   float m, l, acc[4];
-  lone_row<T>(a, t, row, hk, lo, hi, m, l, acc);
+  lone_row<T, FP4>(a, t, row, hk, lo, hi, m, l, acc);
   const int lane = (int)(threadIdx.x & 63);
   const int64_t at = (t.q0 + row / a.G) * a.H + hk * a.G + row % a.G;
   if (!direct) {

@@ -31,6 +31,8 @@ __all__ = [
     "history_attention", "paged_attention", "history_workspace_size", "cache_pool", "cache_reserve",
     "cache_write", "cache_fork", "cache_free", "cache_compact", "cache_copy", "cache_check",
     "cache_workspace_size",
+    "adapter_linear", "adapter_workspace_size", "rotate", "cache_append", "cache_pool_fp4",
+    "fp4_row_bytes", "cache_read_fp4", "paged_attention_fp4", "paged_fp4_workspace_size",
 ]
 
 RocsError = _lib.RocsError
@@ -52,6 +54,7 @@ class _PythonPath:
 
     linear = glm_linear = mlp2 = fm_linear = lcb = plan = attention = _none
     history = paged = cache_reserve = cache_write = cache_fork = cache_free = cache_compact = _none
+    adapter = append = paged_fp4 = _none
 
 
 def _native():
@@ -1119,3 +1122,254 @@ def cache_check(status):
         raise RocsError(_lib.INVALID_ARGUMENT,
                         f"the cache is unchanged: {why.get(code, f'status {code}')}")
     return detail
+
+
+# --- adapters beside a projection, rotated rows, a cache in 4 bits -----------
+
+def adapter_workspace_size(num_requests, num_rows, k, d_out, rank, dtype):
+    code = _lib.DTYPE_BF16 if dtype == torch.bfloat16 else _lib.DTYPE_F32
+    return int(_lib.load().rocs_adapter_workspace_size(num_requests, num_rows, k, d_out, rank, code))
+
+
+def adapter_linear(x, w, a, b, offsets, adapter_ids, *, scales=None, bias=None, activation="none",
+                   out=None, workspace=None, stream=None):
+    """rocs_adapter_linear: out[n] = act(W x[n] + bias + s B (A x[n])) with the low-rank adapter
+    (A, B, s) of the request that owns row n, beside the projection that all rows share.
+
+    x [N, K] (rows may be strided), w [D, K], a [adapters, rank, K], b [adapters, D, rank], offsets
+    int32 [R + 1], adapter_ids int32 [R] (an id outside [0, adapters): no adapter), scales float32
+    [adapters], bias float32 [D]. Rows past offsets[R] stay as they are in `out`. Adapters of other
+    ranks than the array's are padded with zeros."""
+    done = (_binding or _native()).adapter(x, w, a, b, offsets, adapter_ids, scales, bias, activation,
+                                           out, workspace, stream)
+    if done is not None:
+        return done
+    _need(x.dim() == 2 and w.dim() == 2 and x.shape[1] == w.shape[1] and w.shape[0] >= 1
+          and w.shape[1] >= 1, "x must be [N, K] and w [D, K]")
+    n, k = x.shape
+    d = w.shape[0]
+    _need(a.dim() == 3 and b.dim() == 3 and a.shape[0] == b.shape[0] and a.shape[2] == k
+          and b.shape[1] == d and a.shape[1] == b.shape[2] and a.shape[1] >= 1,
+          "a must be [adapters, rank, K] and b [adapters, D, rank]")
+    count, rank = a.shape[:2]
+    code = _dtype_code(x)
+    _need(w.dtype == x.dtype and a.dtype == x.dtype and b.dtype == x.dtype,
+          "x, w, a and b must share one dtype")
+    _need(w.is_contiguous() and a.is_contiguous() and b.is_contiguous(),
+          "w, a and b must be contiguous")
+    _need((k == 1 or x.stride(1) == 1) and (n <= 1 or x.stride(0) >= k), "x's rows must be dense")
+    _need(offsets.numel() >= 1, "offsets needs R + 1 entries")
+    r = offsets.numel() - 1
+    _offsets(offsets, r)
+    _int_vector(adapter_ids, r, "adapter_ids")
+    _need(scales is None or (scales.dtype == torch.float32 and scales.shape == (count,)
+                             and scales.is_contiguous()), "scales must be contiguous float32 [adapters]")
+    _need(bias is None or (bias.dtype == torch.float32 and bias.shape == (d,) and bias.is_contiguous()),
+          "bias must be contiguous float32 [D]")
+    _need(activation in _ACT, f"activation must be one of {sorted(k for k in _ACT if k)}")
+    _need(out is None or (out.shape == (n, d) and out.dtype == x.dtype and out.is_contiguous()),
+          "out must be a contiguous [N, D] tensor of x's dtype")
+    _on_gpu(x, w, a, b, offsets, adapter_ids, scales, bias, out)
+    if out is None:
+        out = _new((n, d), x.dtype, x.device, stream)
+    workspace, ws_bytes = _history_scratch(
+        workspace, adapter_workspace_size(r, n, k, d, rank, x.dtype), x.device, stream)
+    _on_gpu(x, workspace)
+    _launch(x.device, stream, "rocs_adapter_linear", _ptr(x), x.stride(0) if n > 1 else 0, _ptr(w),
+            _ptr(a), _ptr(b), _ptr(scales), _ptr(bias), _ptr(offsets), _ptr(adapter_ids), r, n, k, d,
+            rank, count, code, _ACT[activation], _ptr(out), _ptr(workspace), ws_bytes)
+    return out
+
+
+def _turn(m, d, freqs, positions, offsets, slots, lens, interleaved):
+    """The checks of a rotation's arguments: (rot_dim, R, num_slots)."""
+    rot = 0
+    if freqs is not None:
+        _need(freqs.dtype == torch.float32 and freqs.dim() == 1 and freqs.is_contiguous()
+              and 2 * freqs.numel() <= d, "freqs must be contiguous float32 [rot_dim / 2], rot_dim <= d")
+        rot = 2 * freqs.numel()
+    _int_vector(positions, m, "positions")
+    _need(interleaved in (True, False), "interleaved must be True or False")
+    if offsets is None:
+        _need(slots is None and lens is None, "slots and lens need offsets")
+        _need(positions is not None or rot == 0, "a rotation needs positions, or offsets and lens")
+        return rot, 0, 0
+    _need(offsets.numel() >= 1, "offsets needs R + 1 entries")
+    r = offsets.numel() - 1
+    _offsets(offsets, r)
+    _int_vector(slots, r, "slots")
+    n_slots = 0
+    if lens is not None:
+        n_slots = lens.numel()
+        _int_vector(lens, n_slots, "lens")
+        _need(slots is not None or r <= n_slots, "without slots, request r is slot r: R <= slots")
+    _need(lens is not None or positions is not None or rot == 0,
+          "a rotation needs positions, or offsets and lens")
+    return rot, r, n_slots
+
+
+def rotate(x, freqs, *, positions=None, offsets=None, slots=None, lens=None, interleaved=False,
+           out=None, stream=None):
+    """rocs_rotate: the position rotation of x [M, heads, d] (rows may be strided). Pair i of a head's
+    first 2 * len(freqs) dims, dims (i, i + len(freqs)) or with `interleaved` (2 i, 2 i + 1), turns by
+    position * freqs[i] (float32, radians). Positions are `positions` (int32 [M]), or those of the
+    last rows of each request's history: offsets int32 [R + 1], slots int32 [R] (None: request r is
+    slot r), lens int32 [slots], as paged_attention takes them."""
+    _need(x.dim() == 3 and x.shape[1] >= 1 and x.shape[2] >= 1, "x must be [M, heads, d]")
+    m, h, d = x.shape
+    code = _dtype_code(x)
+    rot, r, n_slots = _turn(m, d, freqs, positions, offsets, slots, lens, interleaved)
+    stride = _rows_of(x, "x")
+    _need(out is None or (out.shape == x.shape and out.dtype == x.dtype and out.is_contiguous()),
+          "out must be a contiguous [M, heads, d] tensor of x's dtype")
+    _on_gpu(x, freqs, positions, offsets, slots, lens, out)
+    if out is None:
+        out = _new(x.shape, x.dtype, x.device, stream)
+    _launch(x.device, stream, "rocs_rotate", _ptr(x), stride, _ptr(freqs), rot, int(interleaved),
+            _ptr(positions), _ptr(offsets), _ptr(slots), _ptr(lens), r, n_slots, m, h, d, code,
+            _ptr(out))
+    return out
+
+
+def fp4_row_bytes(kv_heads, head_dim):
+    """Bytes of a row (K and V of all heads) of a 4-bit cache; head_dim a multiple of 32."""
+    n = int(_lib.load().rocs_fp4_row_bytes(kv_heads, head_dim))
+    _need(n > 0, "a cache in 4 bits needs a head_dim that is a multiple of 32, up to 256")
+    return n
+
+
+def cache_pool_fp4(layers, pages, page_size, kv_heads, head_dim, *, slots, table_width,
+                   device="cuda"):
+    """An empty cache in 4 bits: cache_pool's tuple with a pool of bytes [layers, pages, page_size,
+    fp4_row_bytes(kv_heads, head_dim)]. cache_append writes its rows, paged_attention_fp4 and
+    cache_read_fp4 read them; cache_reserve, _fork, _free, _compact and _copy keep its pages as
+    they do another pool's."""
+    pool = torch.zeros((layers, pages, page_size, fp4_row_bytes(kv_heads, head_dim)),
+                       dtype=torch.uint8, device=device)
+    table = torch.full((slots, table_width), -1, dtype=torch.int32, device=device)
+    return (pool, table, torch.zeros(slots, dtype=torch.int32, device=device),
+            torch.zeros(pages, dtype=torch.int32, device=device))
+
+
+def _pool_rows_fp4(pool, kv_heads, head_dim):
+    """Rows of one layer's 4-bit pool [pages, page_size, row bytes]."""
+    row = fp4_row_bytes(kv_heads, head_dim)
+    _need(pool.dtype == torch.uint8 and pool.dim() == 3 and pool.is_contiguous()
+          and pool.shape[2] == row and pool.shape[0] >= 1 and pool.shape[1] >= 1,
+          f"a pool in 4 bits must be contiguous uint8 [pages, page_size, {row}]")
+    return pool.shape[0] * pool.shape[1]
+
+
+def cache_append(k, v, rows, pool, freqs=None, *, q=None, positions=None, offsets=None, slots=None,
+                 lens=None, interleaved=False, q_out=None, stream=None):
+    """rocs_cache_append: row m of k and v [M, kv_heads, d] (column slices of one projection) into
+    pool row rows[m] (from cache_reserve) of one layer's pool, k turned by its position as rotate()
+    does; with q [M, heads, d] the same rows' queries are turned too and returned (q_out). The pool
+    is [pages, page_size, 2, kv_heads, d] of k's dtype, or a 4-bit layer's bytes [pages, page_size,
+    fp4_row_bytes]. Rows that are -1 are passed over; without freqs nothing is turned."""
+    done = (_binding or _native()).append(k, v, rows, pool, freqs, q, positions, offsets, slots, lens,
+                                          interleaved, q_out, stream)
+    if done is not None:
+        return None if q is None else done
+    _need(k.dim() == 3 and k.shape == v.shape and k.shape[1] >= 1 and k.shape[2] >= 1,
+          "k and v must be [M, kv_heads, d]")
+    m, hk, d = k.shape
+    code = _dtype_code(k)
+    _need(v.dtype == k.dtype, "k and v must share one dtype")
+    stride = _rows_of(k, "k")
+    _need(_rows_of(v, "v") == stride, "k and v must share a row stride")
+    _int_vector(rows, m, "rows")
+    rot, r, n_slots = _turn(m, d, freqs, positions, offsets, slots, lens, interleaved)
+    if pool.dtype == torch.uint8:
+        form, pool_rows = _lib.POOL_FP4, _pool_rows_fp4(pool, hk, d)
+    else:
+        form = _lib.POOL_ROWS
+        _need(pool.dtype == k.dtype and pool.dim() == 5 and pool.is_contiguous()
+              and tuple(pool.shape[2:]) == (2, hk, d) and pool.shape[0] >= 1 and pool.shape[1] >= 1,
+              "pool must be contiguous [pages, page_size, 2, kv_heads, d] of k's dtype, or 4-bit rows")
+        pool_rows = pool.shape[0] * pool.shape[1]
+    h, q_stride = 0, 0
+    _need(q is not None or q_out is None, "q_out needs q")
+    if q is not None:
+        _need(q.dim() == 3 and q.shape[0] == m and q.shape[1] >= 1 and q.shape[2] == d
+              and q.dtype == k.dtype, "q must be [M, heads, d] of k's dtype")
+        h, q_stride = q.shape[1], _rows_of(q, "q")
+        _need(q_out is None or (q_out.shape == q.shape and q_out.dtype == q.dtype
+                                and q_out.is_contiguous()),
+              "q_out must be a contiguous [M, heads, d] tensor of q's dtype")
+    _on_gpu(k, v, rows, pool, freqs, q, positions, offsets, slots, lens, q_out)
+    if q is not None and q_out is None:
+        q_out = _new(q.shape, q.dtype, q.device, stream)
+    _launch(k.device, stream, "rocs_cache_append", _ptr(q), q_stride, _ptr(k), _ptr(v), stride,
+            _ptr(rows), _ptr(freqs), rot, int(interleaved), _ptr(positions), _ptr(offsets),
+            _ptr(slots), _ptr(lens), r, n_slots, m, h, hk, d, code, _ptr(pool), pool_rows, form,
+            _ptr(q_out))
+    return q_out
+
+
+def cache_read_fp4(rows, pool, kv_heads, head_dim, *, dtype=torch.bfloat16, out=None, stream=None):
+    """rocs_cache_read_fp4: rows rows[m] (int32 [M]) of one layer's 4-bit pool as values [M, 2,
+    kv_heads, head_dim] (K, then V) in bfloat16 (exactly) or float32; a row outside the pool is
+    zero."""
+    _need(dtype in (torch.bfloat16, torch.float32), "dtype must be bfloat16 or float32")
+    pool_rows = _pool_rows_fp4(pool, kv_heads, head_dim)
+    m = rows.numel()
+    _int_vector(rows, m, "rows")
+    shape = (m, 2, kv_heads, head_dim)
+    _need(out is None or (out.shape == shape and out.dtype == dtype and out.is_contiguous()),
+          "out must be a contiguous [M, 2, kv_heads, head_dim] tensor of dtype")
+    _on_gpu(rows, pool, out)
+    if out is None:
+        out = _new(shape, dtype, pool.device, stream)
+    _launch(pool.device, stream, "rocs_cache_read_fp4", _ptr(rows), m, _ptr(pool), pool_rows, kv_heads,
+            head_dim, _dtype_code(out), _ptr(out))
+    return out
+
+
+def paged_fp4_workspace_size(num_requests, num_rows, heads, kv_heads, head_dim, max_kv_len, dtype):
+    """Bytes of workspace of one paged_attention_fp4 call over at most max_kv_len keys a request (at
+    most table width * page size)."""
+    code = _lib.DTYPE_BF16 if dtype == torch.bfloat16 else _lib.DTYPE_F32
+    return int(_lib.load().rocs_paged_fp4_workspace_size(num_requests, num_rows, heads, kv_heads,
+                                                         head_dim, max_kv_len, code))
+
+
+def paged_attention_fp4(q, pages, page_table, kv_lens, q_offsets, *, kv_heads, slots=None,
+                        causal=True, prefix_lens=None, slopes=None, cap=0.0, max_kv_len=None,
+                        scale=None, out=None, workspace=None, stream=None):
+    """rocs_paged_attention_fp4: paged_attention over one layer's pages in 4 bits, uint8 [pages,
+    page_size, fp4_row_bytes(kv_heads, d)]; q [N, H, d] with d a multiple of 32. The other
+    arguments, the masks and the result are paged_attention's."""
+    done = (_binding or _native()).paged_fp4(q, pages, page_table, kv_lens, q_offsets, kv_heads, slots,
+                                             causal, prefix_lens, slopes, cap, max_kv_len, scale, out,
+                                             workspace, stream)
+    if done is not None:
+        return done
+    _need(q.dim() == 3, "q must be [N, heads, d]")
+    n, h, d = q.shape
+    _need(kv_heads >= 1 and h >= 1 and h % kv_heads == 0, "kv_heads must divide q's heads")
+    _pool_rows_fp4(pages, kv_heads, d)
+    n_pages, page = pages.shape[:2]
+    # The rules that every attention checks, with q in the place of K and V.
+    own = q[:, :kv_heads]
+    r, cap, most = _score_rules(q, own, own, own, prefix_lens, q_offsets, slopes, cap, causal,
+                                max_kv_len, out)
+    _need(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
+          and page_table.shape[1] >= 1, "page_table must be a contiguous int32 [slots, width]")
+    n_slots, width = page_table.shape
+    _int_vector(kv_lens, n_slots, "kv_lens")
+    _int_vector(slots, r, "slots")
+    _need(slots is not None or r <= n_slots, "without slots, request r is slot r: R <= slots")
+    q_stride = _rows_of(q, "q")
+    _on_gpu(q, pages, page_table, kv_lens, q_offsets, slots, prefix_lens, slopes, out)
+    if out is None:
+        out = _new(q.shape, q.dtype, q.device, stream)
+    bound = min(most or width * page, width * page)
+    need = paged_fp4_workspace_size(r, n, h, kv_heads, d, bound, q.dtype)
+    workspace, ws_bytes = _history_scratch(workspace, need, q.device, stream)
+    _on_gpu(q, workspace)
+    _launch(q.device, stream, "rocs_paged_attention_fp4", _ptr(q), q_stride, _ptr(pages),
+            _ptr(page_table), width, _ptr(kv_lens), _ptr(slots), n_slots, _ptr(q_offsets),
+            _ptr(prefix_lens), _ptr(slopes), r, n, n_pages, page, h, kv_heads, d, float(scale or 0.0),
+            cap, int(causal), most, _dtype_code(q), _ptr(out), _ptr(workspace), ws_bytes)
+    return out

@@ -1,0 +1,163 @@
+"""GPU: a projection with low-rank adapters of many requests against the float64 oracle.
+
+Tolerance per element, from the roundings: fp32 sums of K products (K 2^-24 of the weight of |x| |w|),
+t = s A x summed alike (K 2^-24 of s |A| |x|, moved on by |B|) and, in bf16, rounded once (2^-8 of
+|B| |t|), the product with B (rank 2^-24), and the result's own rounding."""
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import dev_i32
+from oracle import layer as oracle
+from paper_2607_27744_amd import ops
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+U32 = 2.0 ** -24
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def make(counts, ids, k, d, rank, adapters, dtype, seed=0, bias=False, pad=0, stride=0):
+    g = torch.Generator().manual_seed(seed)
+    n = int(np.sum(counts)) + pad
+    rnd = lambda *s: torch.randn(*s, generator=g)   # noqa: E731
+    x = rnd(n, k + stride).to(dtype).cuda()[:, :k]
+    case = dict(x=x, w=(rnd(d, k) * k ** -0.5).to(dtype).cuda(),
+                a=(rnd(adapters, rank, k) * k ** -0.5).to(dtype).cuda(),
+                b=(rnd(adapters, d, rank) * rank ** -0.5).to(dtype).cuda(),
+                offsets=dev_i32(np.concatenate([[0], np.cumsum(counts)])), adapter_ids=dev_i32(ids))
+    kw = dict(scales=torch.rand(adapters, generator=g).cuda() + 0.5)
+    if bias:
+        kw["bias"] = rnd(d).cuda()
+    return case, kw
+
+
+def check(case, kw, counts, ids, got, relu=False, rows=None):
+    n = int(np.sum(counts))
+    x, w, a, b = (_np(case[c]) for c in "xwab")
+    scales, bias = _np(kw["scales"]), _np(kw["bias"]) if "bias" in kw else None
+    want, t, move, weight = oracle.adapter_linear(x[:n], w, a, b, counts, ids, scales, bias, relu)
+    bf = 2.0 ** -8 if case["x"].dtype == BF else 0.0
+    k, rank = x.shape[1], a.shape[1]
+    # |B| (s |A| |x|): what an error of t's sums is weighed with.
+    wide = oracle.adapter_linear(np.abs(x[:n]), np.abs(w), np.abs(a), np.abs(b), counts, ids, scales)[2]
+    tol = (k + 8) * U32 * (weight + wide) + (bf + (rank + 8) * U32) * move
+    if bias is not None:
+        tol = tol + 4 * U32 * np.abs(bias)
+    tol = tol + (bf if bf else U32) * (np.abs(want) + tol) + 1e-30
+    got = _np(got)[:n]
+    off = np.abs(got - want)
+    assert np.all(np.isfinite(got))
+    worst = np.unravel_index(np.argmax(off / tol), off.shape)
+    assert np.all(off <= tol), f"{off[worst]:.3g} off at {worst}, {tol[worst]:.3g} allowed"
+
+
+CASES = [  # counts, ids, k, d, rank, adapters, dtype
+    ([1] * 8, [0, 1, 2, 0, -1, 1, 5, 0], 256, 512, 8, 3, BF),
+    ([1], [0], 64, 4, 8, 1, BF), ([1], [-1], 64, 68, 8, 1, BF),
+    ([1] * 70, list(range(70)), 128, 260, 16, 70, BF),
+    ([3, 0, 1, 40, 17, 128, 2], [2, 0, 1, 1, -1, 0, 3], 72, 100, 24, 4, BF),
+    ([200, 333, 1, 0, 64], [1, 0, -1, 1, 0], 512, 384, 32, 2, BF),
+    ([700, 900], [0, 1], 320, 260, 64, 2, BF),
+    ([130, 5, 300], [1, 1, 0], 128, 256, 136, 2, BF),
+    ([40, 60], [0, 1], 64, 64, 256, 2, BF),
+    ([5, 30], [0, 1], 100, 77, 8, 2, BF),                        # K off the fast path
+    ([5, 30], [0, 1], 96, 76, 5, 2, BF), ([9], [0], 7, 3, 1, 1, BF),
+    ([1, 20, 0, 3], [1, 0, 0, -1], 101, 77, 5, 2, F32), ([64, 64], [0, 1], 128, 64, 16, 2, F32),
+    ([1] * 33, [i % 5 - 1 for i in range(33)], 36, 20, 4, 4, F32),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{sum(c[0])}x{c[2]}.{c[3]}r{c[4]}-{str(c[6])[6:]}")
+def test_against_oracle(gpu_lib, case):
+    counts, ids, k, d, rank, adapters, dtype = case
+    c, kw = make(counts, ids, k, d, rank, adapters, dtype, seed=k + d)
+    check(c, kw, counts, ids, ops.adapter_linear(**c, **kw))
+    c, kw = make(counts, ids, k, d, rank, adapters, dtype, seed=k + d + 1, bias=True)
+    check(c, kw, counts, ids, ops.adapter_linear(**c, **kw, activation="relu"), relu=True)
+
+
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 33, 64, 65, 127, 129, 255, 257, 600, 1500])
+def test_row_counts(gpu_lib, n):
+    counts, ids = [n // 3, n - n // 3], [1, 0]
+    c, kw = make(counts, ids, 192, 132, 16, 2, BF, seed=n)
+    check(c, kw, counts, ids, ops.adapter_linear(**c, **kw))
+
+
+@pytest.mark.parametrize("dtype, k", [(BF, 64), (BF, 60), (F32, 64)])
+def test_strided_rows_and_a_padded_batch(gpu_lib, dtype, k):
+    counts, ids = [3, 0, 50, 1], [1, 0, 0, -1]
+    for stride, pad in ((8, 0), (40, 13), (3, 5)):
+        c, kw = make(counts, ids, k, 72, 8, 2, dtype, pad=pad, stride=stride)
+        out = torch.full((54 + pad, 72), 7.0, dtype=dtype, device="cuda")
+        assert ops.adapter_linear(**c, **kw, out=out) is out
+        check(c, kw, counts, ids, out)
+        assert torch.all(out[54:] == 7.0)
+
+
+def test_rows_without_an_adapter_are_the_projection(gpu_lib):
+    # The same rows in a call with adapters and one without: rows of no adapter have the same bits.
+    for n, k, d in ((40, 256, 192), (900, 512, 256)):
+        counts, ids = [n // 2, n - n // 2], [-1, 0]
+        c, kw = make(counts, ids, k, d, 16, 1, BF, seed=n)
+        with_one = ops.adapter_linear(**c, **kw)
+        none = ops.adapter_linear(**{**c, "adapter_ids": dev_i32([-1, 9])}, **kw)
+        assert torch.equal(with_one[:n // 2], none[:n // 2])
+        assert not torch.equal(with_one[n // 2:], none[n // 2:])
+        empty = {**c, "a": c["a"][:0], "b": c["b"][:0]}
+        assert torch.equal(ops.adapter_linear(**empty), none)
+
+
+def test_an_odd_row_stays_by_itself(gpu_lib):
+    # NaN and infinities in one request's rows and adapter do not reach another's.
+    counts, ids = [20, 1, 30], [0, 1, 0]
+    for dtype, k in ((BF, 64), (F32, 64), (BF, 60)):
+        c, kw = make(counts, ids, k, 96, 8, 2, dtype)
+        want = ops.adapter_linear(**c, **kw)
+        x = c["x"].clone()
+        x[20] = float("nan")
+        a, b = c["a"].clone(), c["b"].clone()
+        a[1], b[1] = float("inf"), float("nan")
+        got = ops.adapter_linear(**{**c, "x": x, "a": a, "b": b}, **kw)
+        keep = torch.arange(51) != 20
+        assert torch.equal(got[keep], want[keep]) and torch.all(torch.isnan(got[20]))
+
+
+def test_calls_that_share_a_workspace(gpu_lib):
+    # One workspace for calls one after the other, the second smaller; equal calls, equal bits.
+    ws = torch.empty(ops.adapter_workspace_size(3, 700, 256, 128, 32, BF), dtype=torch.uint8, device="cuda")
+    big, kw = make([300, 100, 300], [0, 1, -1], 256, 128, 32, 2, BF)
+    small, kw2 = make([1, 3], [1, 0], 256, 64, 16, 2, BF)
+    a = ops.adapter_linear(**big, **kw, workspace=ws)
+    b = ops.adapter_linear(**small, **kw2, workspace=ws)
+    assert torch.equal(ops.adapter_linear(**big, **kw, workspace=ws), a)
+    assert torch.equal(ops.adapter_linear(**small, **kw2), b)
+    with pytest.raises(ops.RocsError, match="workspace needs"):
+        ops.adapter_linear(**big, **kw, workspace=ws[:256])
+
+
+@pytest.mark.parametrize("counts", [[1] * 9, [200, 1, 399]])
+def test_captured_and_on_another_stream(gpu_lib, counts):
+    ids = [(i % 3) - 1 for i in range(len(counts))]
+    c, kw = make(counts, ids, 256, 192, 16, 2, BF)
+    want = ops.adapter_linear(**c, **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    on_side = ops.adapter_linear(**c, **kw, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(on_side, want)
+    out = torch.empty_like(want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ops.adapter_linear(**c, **kw, out=out)
+    for i in range(3):
+        c["x"].copy_(torch.randn_like(c["x"]))
+        out.zero_()
+        g.replay()
+        want = ops.adapter_linear(**c, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
