@@ -410,6 +410,20 @@ hipError_t launch_join(const HistArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// The plan with histories in `splits` chunks of whole stages, and what that needs.
+static HistPlan cut_in(HistPlan p, int64_t splits, int64_t N, int H, int D, int64_t max_len) {
+  if (splits > kMaxSplits) splits = kMaxSplits;
+  if (splits < 1) splits = 1;
+  p.chunk = (int)(((max_len + splits - 1) / splits + 63) / 64 * 64);
+  p.splits = p.chunk > 0 ? (int)((max_len + p.chunk - 1) / p.chunk) : 1;
+  if (p.splits < 1) p.splits = 1;
+  if (p.splits > 1) {
+    p.ml_bytes = align256((size_t)p.splits * N * H * 2 * sizeof(float));
+    p.o_bytes = align256((size_t)p.splits * N * H * D * sizeof(float));
+  }
+  return p;
+}
+
 HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
   HistPlan p{};
   const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
@@ -445,16 +459,7 @@ HistPlan history_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_le
       if (more > splits) splits = more;
     }
   }
-  if (splits > kMaxSplits) splits = kMaxSplits;
-  if (splits < 1) splits = 1;
-  p.chunk = (int)(((max_len + splits - 1) / splits + 63) / 64 * 64);
-  p.splits = p.chunk > 0 ? (int)((max_len + p.chunk - 1) / p.chunk) : 1;
-  if (p.splits < 1) p.splits = 1;
-  if (p.splits > 1) {
-    p.ml_bytes = align256((size_t)p.splits * N * H * 2 * sizeof(float));
-    p.o_bytes = align256((size_t)p.splits * N * H * D * sizeof(float));
-  }
-  return p;
+  return cut_in(p, splits, N, H, D, max_len);
 }
 
 hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s) {
@@ -467,14 +472,32 @@ hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hip
 }
 
 HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
-  (void)bf16;
-  return history_plan(R, N, H, Hk, D, max_len, false);
+  const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
+  if (!(bf16 && D <= 128) || each > 32) {
+    HistPlan general = history_plan(R, N, H, Hk, D, max_len, false);
+    general.rows = 0;
+    return general;
+  }
+  HistPlan p{};
+  p.rows = each <= 16 ? 16 : 32;
+  const auto parts = [max_len](int64_t most, int64_t least_keys) {
+    const int64_t n = (max_len + least_keys - 1) / least_keys;
+    return n < most ? n : most;
+  };
+  const int64_t chunks = (max_len + 511) / 512;
+  int hw = Hk % 4 == 0 ? 4 : Hk % 2 == 0 ? 2 : 1;
+  while (hw > 1 && R * (Hk / hw) * chunks < 1024) hw /= 2;
+  const int64_t wide = R * (Hk / hw);
+  p.heads = wide * chunks >= 1024 ? hw : 1;
+  int64_t splits = wide * chunks >= 1024 ? parts(4096 / wide, 512) : parts(2048 / (R * Hk), 512);
+  return cut_in(p, splits, N, H, D, max_len);
 }
 
 hipError_t launch_history_fp4(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s) {
-  (void)rows;
-  (void)fast;
-  const hipError_t e = bf16 ? launch_general_fp4<bf16_t>(a, s) : launch_general_fp4<float>(a, s);
+  const hipError_t e = fast && rows > 0
+                           ? launch_history_fp4_few(a, rows, s)
+                       : bf16 ? launch_general_fp4<bf16_t>(a, s)
+                              : launch_general_fp4<float>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
   return bf16 ? launch_join<bf16_t>(a, s) : launch_join<float>(a, s);
 }

@@ -1,0 +1,358 @@
+// Attention over a cache held in 4 bits, the bf16 kernel for few rows: 16 or 32
+// rows (token, head of the group) of one request a wave.
+//
+// A call over single events is a read of the cache, of which 4 bits leave a
+// quarter of the bytes: what a byte costs in instructions decides. K goes from
+// memory to the matrix cores through registers alone: lane (l16, g) holds key l16's
+// dims from D / 4 g on (16 bytes at head_dim 128: one block of a scale), which
+// the conversion instruction turns into the A operands of D / 32 products; the
+// order of a product's inner dims is free as long as q's fragments follow it.
+// V's products run over keys, and a lane has them for one dim: V is converted a
+// block a lane (its scale with it) and turned around through LDS, 32 keys at a time, by
+// the transposing read. (Turned as codes, a quarter of the LDS bytes, a scale would
+// have to go into the weights, of another block and key in each.)
+// 16 x 16 x 32 products: the heads of a group rarely fill more rows, and a score
+// costs an exponential. Waves and parts share a call as in history_split.
+#include "history_mfma.h"
+#include "launch.h"
+
+namespace rocs {
+namespace {
+
+constexpr int kWaves = 4;
+
+// 16-byte chunk of a staged V row at which chunk c of `key` stands: c ^ this. The
+// eight rows of a half wave's transposing read and the quarter wave of a write fall on
+// distinct banks.
+template <int D>
+__device__ __forceinline__ int v_swizzle(int key) {
+  if constexpr (D == 128) return (key & 3) | ((((key >> 2) & 3) ^ ((key & 1) << 1)) << 2);
+  else return ((key >> 1) & 3) | (((key >> 1) & 1) << 2);
+}
+
+// Row number in the pool of key j.
+__device__ __forceinline__ int pool_row(const HistArgs& a, const int32_t* pages, int j) {
+  const int c = a.page_size == 1 ? j : (int)(__umulhi((uint32_t)j, a.page_magic) >> a.page_shift);
+  const uint32_t p = min((uint32_t)pages[c], (uint32_t)(a.pages - 1));
+  return (int)(p * (uint32_t)a.page_size) + (j - c * a.page_size);
+}
+
+template <int D, int SCORE, int NR>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR == 1 ? 3 : 2))) void
+history_fp4_few(const HistArgs a, int64_t slots) {
+  constexpr int kRows = 16 * NR;
+  constexpr int KS = D / 32, DB = D / 16;   // products of a score, output blocks
+  constexpr int BPR = D / kFp4Block;        // blocks of a key: V's loads of a lane and stage
+  constexpr int KW32 = D / 32;              // 32-bit words of a lane's part of a K row
+  constexpr int ROWB = 2 * D;               // a staged V row
+  constexpr int STAGE = 32 * ROWB > kRows * D * 4 ? 32 * ROWB : kRows * D * 4;
+  __shared__ __attribute__((aligned(1024))) char lds[kWaves * STAGE];
+  __shared__ float pm[kWaves][kRows], pl[kWaves][kRows];
+  __shared__ int odd[kWaves][kRows];        // by head and row: to form again
+  ROCS_LDS char* const lds3 = (ROCS_LDS char*)lds;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const uint32_t b8 = blockIdx.x & ~7u;     // as in history_split
+  const uint32_t work = b8 + 8 > gridDim.x ? blockIdx.x : b8 + ((blockIdx.x + (blockIdx.x >> 3)) & 7u);
+  const int HW = a.heads, KW = kWaves / HW;
+  const uint32_t groups_n = (uint32_t)(a.Hk / HW);
+  const int hk0 = (int)(work % groups_n) * HW, hk = hk0 + wave % HW;
+  const uint32_t rest = work / groups_n;
+  const int split = (int)(rest % (uint32_t)a.splits);
+  const HistTile t = hist_tile(a, slots - 1 - rest / (uint32_t)a.splits, kRows);
+  if (t.rows <= 0) return;
+  for (int i = tid; i < kWaves * kRows; i += 256) odd[i / kRows][i % kRows] = 0;
+
+  RowRule rule[NR];
+  bf16x8 qf[NR][KS];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const int row = t.row0 + min(16 * r + l16, t.rows - 1);     // clamped; extra rows never stored
+    const int token = row / a.G, head = hk * a.G + row % a.G;
+    score_rules<SCORE>(rule[r], a, head);
+    rule[r].pos = position_of(t, token);
+    rule[r].lim = limit_of(a, t, token);
+    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * a.D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const int d = D / 4 * g + 8 * ks;
+      qf[r][ks] = as_bf16x8(load16(q + d, d < a.D));
+    }
+  }
+  const int lim_lo = limit_of(a, t, t.row0 / a.G);
+  const int most = limit_of(a, t, (t.row0 + t.rows - 1) / a.G);
+  const int lo = split * a.chunk, hi = split_end(a, split, most);
+  const bool alone = tile_alone(a, most), direct = a.splits == 1 || alone;
+  if (alone && split > 0) return;
+
+  // This lane's places in a row: its part of K and that part's scale; the block of
+  // V (the n-th of a stage: key 64 / BPR n + lane / BPR) and its scale. Below the
+  // kernel's own width the head's last ones stand in (q is 0 there, or the result is not stored).
+  const Fp4Row fr{a.Hk, a.D};
+  const char* const base = static_cast<const char*>(a.k);
+  const int k_at = fr.values(0, hk) + min(D / 8 * g, a.D / 2 - D / 8);
+  const int ks_at = fr.scales(0, hk) + min(D / 4 * g / kFp4Block, a.D / kFp4Block - 1);
+  const int vb = min(lane % BPR, a.D / kFp4Block - 1);
+  const int v_at = fr.values(1, hk) + 16 * vb, vs_at = fr.scales(1, hk) + vb;
+  const uint32_t row_bytes = (uint32_t)a.kv_stride;
+
+  uint32_t kw[4][KW32], kse[4];
+  u32x4 vw[BPR];
+  uint32_t vse[BPR];
+  auto load_k = [&](int rows) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      const char* p = base + (uint64_t)(uint32_t)__shfl(rows, 16 * kb + l16) * row_bytes;
+      if constexpr (KW32 == 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(p + k_at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kw[kb][i] = x[i];
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(p + k_at);
+        kw[kb][0] = x[0];
+        kw[kb][1] = x[1];
+      }
+      kse[kb] = (uint8_t)p[ks_at];
+    }
+  };
+  auto load_v = [&](int rows) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < BPR; ++n) {
+      const char* p = base + (uint64_t)(uint32_t)__shfl(rows, 64 / BPR * n + lane / BPR) * row_bytes;
+      vw[n] = *reinterpret_cast<const u32x4*>(p + v_at);
+      vse[n] = (uint8_t)p[vs_at];
+    }
+  };
+  auto rows_of = [&](int at) __attribute__((always_inline)) { return pool_row(a, t.pages, min(at + lane, hi - 1)); };
+
+  float m[NR], l_part[NR];
+  f32x4 o[NR][DB];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    m[r] = -INFINITY;
+    l_part[r] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[r][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const uint32_t st0 = (uint32_t)(wave * STAGE);
+  // Transposing reads of V^T: rows 16 x + 4 g + jl / 4 of the staged 32, 16 dims.
+  uint32_t va[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int key = 16 * x + 4 * g + (l16 >> 2);
+    va[x] = st0 + (uint32_t)(key * ROWB + 16 * (((l16 & 3) >> 1) ^ v_swizzle<D>(key)) + 8 * (l16 & 1));
+  }
+
+  int at = lo + 64 * (wave / HW);
+  int rows_now = 0, rows_next = 0;
+  if (at < hi) {
+    rows_now = rows_of(at);
+    load_k(rows_now);
+    load_v(rows_now);
+    rows_next = rows_of(at + 64 * KW);
+  }
+  for (; at < hi; at += 64 * KW) {
+    const bool more = at + 64 * KW < hi;
+    f32x4 s[NR][4];
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      const float scale = fp4_scale(kse[kb]);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) s[r][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 kf = as_bf16x8(fp4_to_bf16x8(kw[kb][ks], scale));
+#pragma unroll
+        for (int r = 0; r < NR; ++r) s[r][kb] = mfma16(kf, qf[r][ks], s[r][kb]);
+      }
+    }
+    rows_now = rows_next;
+    if (more) {
+      load_k(rows_now);
+      rows_next = rows_of(at + 128 * KW);
+    }
+    // V's first 32 keys, a block a lane.
+    auto stage_v = [&](int half) __attribute__((always_inline)) {
+#pragma unroll
+      for (int n = BPR / 2 * half; n < BPR / 2 * (half + 1); ++n) {
+        const int key = 64 / BPR * n + lane / BPR - 32 * half;
+        const float scale = fp4_scale(vse[n]);
+        const uint32_t to = st0 + (uint32_t)(key * ROWB);
+        const int c0 = 4 * (lane % BPR), sw = v_swizzle<D>(key);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          *reinterpret_cast<ROCS_LDS u32x4*>(lds3 + to + 16 * ((c0 + c) ^ sw)) = fp4_to_bf16x8(vw[n][c], scale);
+      }
+    };
+    stage_v(0);
+    uint32_t pk[NR][4][2];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      const RowRule& rr = rule[r];
+      f32x4(&sr)[4] = s[r];
+      if constexpr (SCORE != 0) {
+        const float rel = (float)(rr.pos - at - 4 * g);
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float shift = (SCORE & kCap) != 0 ? rr.cap2 : 0.f;
+            if constexpr ((SCORE & kBias) != 0) shift = fmaf(-rr.slope2, fabsf(rel - (float)(16 * kb + i)), shift);
+            const float x = sr[kb][i];
+            if constexpr ((SCORE & kCap) != 0)
+              sr[kb][i] = fmaf(-2.0f * rr.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * rr.cap_in)), shift);
+            else if constexpr ((SCORE & kWideCap) != 0)
+              sr[kb][i] = wide_cap(x, rr) + shift;
+            else
+              sr[kb][i] = fmaf(x, rr.scale2, shift);
+          }
+      }
+      if (at + 64 > lim_lo) {
+        const int seen = rr.lim - at - 4 * g;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (16 * kb + i >= seen) sr[kb][i] = -INFINITY;
+      }
+      const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+      auto weights = [&](float ms) __attribute__((always_inline)) {
+        float sum = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            float e0 = sr[kb][2 * w], e1 = sr[kb][2 * w + 1];
+            if constexpr (SCORE == 0) {
+              e0 = fmaf(e0, rr.scale2, -ms);
+              e1 = fmaf(e1, rr.scale2, -ms);
+            } else {
+              e0 -= ms;
+              e1 -= ms;
+            }
+            pk[r][kb][w] = pack_bf16x2(__builtin_amdgcn_exp2f(e0), __builtin_amdgcn_exp2f(e1));
+            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[r][kb][w]), ones, sum, false);
+          }
+        return sum;
+      };
+      float sum = weights(m[r]);
+      if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
+        float mx = sr[0][0];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sr[kb][i]);
+        mx = max_across_rows(mx) * (SCORE == 0 ? rr.scale2 : 1.0f);
+        const bool need = mx > m[r] + kLazyMove;
+        const float alpha = need ? exp2f(m[r] - mx) : 1.0f;
+        if (need) m[r] = mx;
+        l_part[r] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[r][db] *= alpha;
+        sum = weights(m[r] == -INFINITY ? 0.f : m[r]);      // no key seen yet: weights 0
+      }
+      l_part[r] += sum;
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (half == 1) stage_v(1);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (ROCS_LDS i16x4*)(lds3 + (va[0] ^ (32u * db)))));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (ROCS_LDS i16x4*)(lds3 + (va[1] ^ (32u * db)))));
+        const bf16x8 vf = as_bf16x8(u32x4{x[0], x[1], y[0], y[1]});
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+          o[r][db] = mfma16(vf, as_bf16x8(u32x4{pk[r][2 * half][0], pk[r][2 * half][1],
+                                                pk[r][2 * half + 1][0], pk[r][2 * half + 1][1]}), o[r][db]);
+      }
+    }
+    if (more) load_v(rows_now);
+  }
+
+  // This wave's partial softmax into its staging area, 16-byte pieces of a row
+  // swizzled by the row: element i of o[r][db] is O[16 r + l16][16 db + 4 g + i].
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const float l_sum = sum_across_rows(l_part[r]);
+    if (g == 0) {
+      pm[wave][16 * r + l16] = m[r];
+      pl[wave][16 * r + l16] = l_sum;
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+      *reinterpret_cast<ROCS_LDS f32x4*>(lds3 + st0 + (16 * r + l16) * D * 4 + 16 * ((4 * db + g) ^ l16)) = o[r][db];
+  }
+  __syncthreads();
+  // 16-byte pieces of (head, row); the head's waves are hs, hs + HW, ..
+  const int CF = a.D / 4;
+  for (int c = tid; c < HW * t.rows * CF; c += 256) {
+    const int piece = c % CF, i = c / CF % t.rows, hs = c / CF / t.rows;
+    float mx = pm[hs][i];
+    for (int w = hs + HW; w < kWaves; w += HW) mx = fmaxf(mx, pm[w][i]);
+    const float ms = mx == -INFINITY ? 0.f : mx;
+    float l = 0.f;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int w = hs; w < kWaves; w += HW) {
+      const float f = exp2f(pm[w][i] - ms);
+      l += pl[w][i] * f;
+      y += *reinterpret_cast<const ROCS_LDS f32x4*>(lds3 + w * STAGE + i * D * 4 + 16 * (piece ^ (i & 15))) * f;
+    }
+    if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3])) && may_differ(l, a.D, D)) odd[hs][i] = 1;
+    const int rw = t.row0 + i;
+    const int64_t to_row = (t.q0 + rw / a.G) * a.H + (hk0 + hs) * a.G + rw % a.G;
+    const int64_t to = (int64_t)split * a.N * a.H + to_row;
+    if (a.splits > 1 && piece == 0) {
+      a.part_ml[2 * to] = mx;
+      a.part_ml[2 * to + 1] = alone ? kDone : l;
+    }
+    if (!direct) {
+      if (l != 0.f) *reinterpret_cast<f32x4*>(a.part_o + to * a.D + 4 * piece) = y;
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      *reinterpret_cast<u32x2*>(static_cast<bf16_t*>(a.out) + to_row * a.D + 4 * piece) =
+          u32x2{pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv)};
+    }
+  }
+  __syncthreads();
+  for (int i = wave; i < HW * t.rows; i += kWaves)        // see lone_row
+    if (__builtin_amdgcn_readfirstlane(odd[i / t.rows][i % t.rows]) != 0)
+      redo_row<bf16_t, true>(a, t, t.row0 + i % t.rows, hk0 + i / t.rows, lo, hi, split, direct);
+}
+
+template <int D, int NR>
+hipError_t launch_few(const HistArgs& a, int64_t slots, int64_t blocks, hipStream_t s) {
+  auto go = [&](auto kernel) {
+    return launch_kernel(kernel, dim3((uint32_t)blocks), dim3(256), s, a, slots);
+  };
+  switch (score_of(a)) {
+    case kCap: return go(history_fp4_few<D, kCap, NR>);
+    case kWideCap: return go(history_fp4_few<D, kWideCap, NR>);
+    case kBias: return go(history_fp4_few<D, kBias, NR>);
+    case kCap | kBias: return go(history_fp4_few<D, kCap | kBias, NR>);
+    case kWideCap | kBias: return go(history_fp4_few<D, kWideCap | kBias, NR>);
+    default: return go(history_fp4_few<D, 0, NR>);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_history_fp4_few(const HistArgs& args, int rows, hipStream_t s) {
+  HistArgs a = args;
+  // j / page_size for j below 2^31 as a product's upper half and a shift: with l =
+  // ceil(log2 page_size), floor(2^(31 + l) / page_size) + 1 is exact.
+  int l = 0;
+  while ((int64_t(1) << l) < a.page_size) ++l;
+  a.page_magic = a.page_size > 1 ? (uint32_t)((uint64_t(1) << (31 + l)) / (uint64_t)a.page_size + 1) : 0;
+  a.page_shift = l > 0 ? l - 1 : 0;
+  const int64_t slots = a.R + (a.N * a.G + rows - 1) / rows;
+  const int64_t blocks = slots * (a.Hk / a.heads) * a.splits;
+  if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+  if (rows == 16) return a.D > 64 ? launch_few<128, 1>(a, slots, blocks, s) : launch_few<64, 1>(a, slots, blocks, s);
+  return a.D > 64 ? launch_few<128, 2>(a, slots, blocks, s) : launch_few<64, 2>(a, slots, blocks, s);
+}
+
+}  // namespace rocs
