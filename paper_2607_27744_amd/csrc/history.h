@@ -25,7 +25,7 @@ struct HistArgs {
   int64_t width, pages;     // table columns, pages in the cache
   int R, S, H, Hk, G, D, page_size;              // G = H / Hk
   uint32_t page_magic;      // 2^32 / (page_size / 16) + 1 (MFMA kernels); for a 4-bit
-  int page_shift;           // pool see launch_history_fp4_few
+  int page_shift;           // pool see set_page_divisor
   float scale, cap;
   int causal;
   int64_t max_len;          // bound on a history's length

@@ -473,7 +473,8 @@ hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hip
 
 HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
   const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
-  if (!(bf16 && D <= 128) || each > 32) {
+  if (bf16 && D <= 128 && each > 32) return history_plan(R, N, H, Hk, D, max_len, true);
+  if (!(bf16 && D <= 128)) {
     HistPlan general = history_plan(R, N, H, Hk, D, max_len, false);
     general.rows = 0;
     return general;
@@ -494,10 +495,10 @@ HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, b
 }
 
 hipError_t launch_history_fp4(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s) {
-  const hipError_t e = fast && rows > 0
-                           ? launch_history_fp4_few(a, rows, s)
-                       : bf16 ? launch_general_fp4<bf16_t>(a, s)
-                              : launch_general_fp4<float>(a, s);
+  const hipError_t e = fast && rows == 128 ? launch_history_fp4_tile(a, s)
+                       : fast && rows > 0  ? launch_history_fp4_few(a, rows, s)
+                       : bf16              ? launch_general_fp4<bf16_t>(a, s)
+                                           : launch_general_fp4<float>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;
   return bf16 ? launch_join<bf16_t>(a, s) : launch_join<float>(a, s);
 }

@@ -1,4 +1,4 @@
-// Attention over a cache held in 4 bits, the bf16 kernel for few rows: 16 or 32
+// Attention over a cache held in 4 bits: the tiled kernel's launch, and the bf16 kernel for few rows: 16 or 32
 // rows (token, head of the group) of one request a wave.
 //
 // A call over single events is a read of the cache, of which 4 bits leave a
@@ -13,7 +13,7 @@
 // have to go into the weights, of another block and key in each.)
 // 16 x 16 x 32 products: the heads of a group rarely fill more rows, and a score
 // costs an exponential. Waves and parts share a call as in history_split.
-#include "history_mfma.h"
+#include "history_tile.h"
 #include "launch.h"
 
 namespace rocs {
@@ -28,13 +28,6 @@ template <int D>
 __device__ __forceinline__ int v_swizzle(int key) {
   if constexpr (D == 128) return (key & 3) | ((((key >> 2) & 3) ^ ((key & 1) << 1)) << 2);
   else return ((key >> 1) & 3) | (((key >> 1) & 1) << 2);
-}
-
-// Row number in the pool of key j.
-__device__ __forceinline__ int pool_row(const HistArgs& a, const int32_t* pages, int j) {
-  const int c = a.page_size == 1 ? j : (int)(__umulhi((uint32_t)j, a.page_magic) >> a.page_shift);
-  const uint32_t p = min((uint32_t)pages[c], (uint32_t)(a.pages - 1));
-  return (int)(p * (uint32_t)a.page_size) + (j - c * a.page_size);
 }
 
 template <int D, int SCORE, int NR>
@@ -342,17 +335,18 @@ hipError_t launch_few(const HistArgs& a, int64_t slots, int64_t blocks, hipStrea
 
 hipError_t launch_history_fp4_few(const HistArgs& args, int rows, hipStream_t s) {
   HistArgs a = args;
-  // j / page_size for j below 2^31 as a product's upper half and a shift: with l =
-  // ceil(log2 page_size), floor(2^(31 + l) / page_size) + 1 is exact.
-  int l = 0;
-  while ((int64_t(1) << l) < a.page_size) ++l;
-  a.page_magic = a.page_size > 1 ? (uint32_t)((uint64_t(1) << (31 + l)) / (uint64_t)a.page_size + 1) : 0;
-  a.page_shift = l > 0 ? l - 1 : 0;
+  set_page_divisor(a);
   const int64_t slots = a.R + (a.N * a.G + rows - 1) / rows;
   const int64_t blocks = slots * (a.Hk / a.heads) * a.splits;
   if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
   if (rows == 16) return a.D > 64 ? launch_few<128, 1>(a, slots, blocks, s) : launch_few<64, 1>(a, slots, blocks, s);
   return a.D > 64 ? launch_few<128, 2>(a, slots, blocks, s) : launch_few<64, 2>(a, slots, blocks, s);
+}
+
+hipError_t launch_history_fp4_tile(const HistArgs& args, hipStream_t s) {
+  HistArgs a = args;
+  set_page_divisor(a);
+  return launch_tile<true>(a, s);
 }
 
 }  // namespace rocs
