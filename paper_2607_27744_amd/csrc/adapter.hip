@@ -112,6 +112,101 @@ __global__ __launch_bounds__(256) void adapter_general(const AdapterArgs a, int 
   }
 }
 
+// ---------------------------------------------------------------------------
+// Fast path, first launch: t = s A x in bf16 (a rounding whose error is half a
+// bf16 step of the adapter's part of the result, and lets its product with B run at
+// the bf16 rate), and the rows' adapters.
+//
+// A workgroup takes 32 RB rows of one request (tiles as in common.h: tile_base) and all
+// of the rank, 32 RK columns at a time; its eight waves split K, operands straight from
+// global memory, and add up through LDS in a fixed order.
+// ---------------------------------------------------------------------------
+template <int RB, int RK>
+__global__ __launch_bounds__(512) void shrink_rows(const AdapterArgs a, bf16_t* __restrict__ t,
+                                                   int32_t* __restrict__ aid, int cols) {
+  constexpr int TILE = 32 * RB;
+  constexpr int U = RB == 1 ? 8 : 2;           // steps of a wave in flight
+  __shared__ f32x4 red[8][4][kWave];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, hh = lane >> 5;
+  const int r = request_of_slot(a.off, a.R, blockIdx.x, 1, TILE);
+  const int64_t end = min((int64_t)a.off[r + 1], a.N);
+  const int64_t n0 = a.off[r] + ((int64_t)blockIdx.x - tile_base(a.off, r, 1, TILE)) * TILE;
+  const int rows = (int)max(min(end - n0, (int64_t)TILE), (int64_t)0);
+  if (rows == 0) return;
+  const int given = a.ids[r], id = (uint32_t)given < (uint32_t)a.A ? given : -1;
+  for (int i = tid; i < rows; i += 512) aid[n0 + i] = id;
+  if (id < 0) return;
+  const float scale = a.scales != nullptr ? a.scales[id] : 1.f;
+  const bf16_t* x[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+    x[b] = static_cast<const bf16_t*>(a.x) + (n0 + min(32 * b + l32, rows - 1)) * a.x_stride + 8 * hh;
+  for (int j0 = 0; j0 < a.rank; j0 += 32 * RK) {
+    const bf16_t* w[RK];
+#pragma unroll
+    for (int k = 0; k < RK; ++k)
+      w[k] = static_cast<const bf16_t*>(a.a) + ((int64_t)id * a.rank + min(j0 + 32 * k + l32, a.rank - 1)) * a.K + 8 * hh;
+    f32x16 acc[RK][RB];
+#pragma unroll
+    for (int k = 0; k < RK; ++k)
+#pragma unroll
+      for (int b = 0; b < RB; ++b) acc[k][b] = f32x16{};
+    for (int k0 = 16 * wave; k0 < a.K; k0 += 128 * U) {
+      u32x4 av[U][RK], xv[U][RB];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + 128 * u;
+        const bool ok = k + 8 * hh < a.K;
+#pragma unroll
+        for (int i = 0; i < RK; ++i) av[u][i] = load16(w[i] + k, ok);
+#pragma unroll
+        for (int b = 0; b < RB; ++b) xv[u][b] = load16(x[b] + k, ok);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (k0 + 128 * u >= a.K) break;
+#pragma unroll
+        for (int i = 0; i < RK; ++i)
+#pragma unroll
+          for (int b = 0; b < RB; ++b) acc[i][b] = mfma32(as_bf16x8(av[u][i]), as_bf16x8(xv[u][b]), acc[i][b]);
+      }
+    }
+    // Quad q of a block: columns 8 q + 4 hh .. + 3 of row l32.
+#pragma unroll
+    for (int i = 0; i < RK; ++i)
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          red[wave][q][lane] = f32x4{acc[i][b][4 * q], acc[i][b][4 * q + 1], acc[i][b][4 * q + 2], acc[i][b][4 * q + 3]};
+        __syncthreads();
+        if (tid < 256) {
+          const int q = tid >> 6;
+          f32x4 s = red[0][q][lane];
+#pragma unroll
+          for (int w8 = 1; w8 < 8; ++w8) s += red[w8][q][lane];
+          const int j = j0 + 32 * i + 8 * q + 4 * hh;
+          if (j >= a.rank) s = f32x4{0.f, 0.f, 0.f, 0.f};       // the rank is a multiple of 8
+          else s *= scale;
+          if (32 * b + l32 < rows && j < cols)
+            *reinterpret_cast<u32x2*>(t + (n0 + 32 * b + l32) * cols + j) =
+                u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+        }
+        __syncthreads();
+      }
+  }
+}
+
+template <int RB, int RK>
+hipError_t launch_shrink(const AdapterArgs& a, bf16_t* t, int32_t* aid, hipStream_t s) {
+  const int64_t slots = a.R + (a.N + 32 * RB - 1) / (32 * RB);
+  if (!grid_fits(slots, 512)) return hipErrorInvalidConfiguration;
+  return launch_kernel(shrink_rows<RB, RK>, dim3((uint32_t)slots), dim3(512), s, a, t, aid,
+                       adapter_cols(a.rank));
+}
+
 template <typename T>
 hipError_t launch_general(const AdapterArgs& a, hipStream_t s) {
   const int cols = adapter_cols(a.rank);
@@ -134,8 +229,16 @@ hipError_t launch_general(const AdapterArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_adapter(const AdapterArgs& a, bool fast, hipStream_t s) {
-  (void)fast;
-  return a.bf16 ? launch_general<bf16_t>(a, s) : launch_general<float>(a, s);
+  if (!fast) return a.bf16 ? launch_general<bf16_t>(a, s) : launch_general<float>(a, s);
+  bf16_t* t = static_cast<bf16_t*>(a.t);
+  int32_t* aid = reinterpret_cast<int32_t*>(static_cast<char*>(a.t) + adapter_t_bytes(a.N, a.rank));
+  const bool tall = a.N / a.R >= 128;
+  const hipError_t e = tall ? (a.rank > 32 ? launch_shrink<4, 2>(a, t, aid, s) : launch_shrink<4, 1>(a, t, aid, s))
+                            : (a.rank > 32 ? launch_shrink<1, 2>(a, t, aid, s) : launch_shrink<1, 1>(a, t, aid, s));
+  if (e != hipSuccess) return e;
+  const LowRank lr{t, static_cast<const bf16_t*>(a.b), aid, a.ids, a.off, a.x_stride, adapter_cols(a.rank),
+                   a.rank, a.A, a.R};
+  return launch_adapter_gemm(a, lr, s);
 }
 
 }  // namespace rocs

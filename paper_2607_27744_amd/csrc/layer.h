@@ -61,6 +61,20 @@ struct AdapterArgs {
 inline int adapter_cols(int rank) { return (rank + 15) / 16 * 16; }
 hipError_t launch_adapter(const AdapterArgs& a, bool fast, hipStream_t s);
 
+// What the fast path's product reads beside x and W.
+struct LowRank {
+  const __bf16* t;          // [N, cols]: s A x, rounded; zeros from rank on
+  const __bf16* b;          // [A, D, rank]
+  const int32_t* aid;       // [N] each row's adapter, or -1
+  const int32_t* ids;       // [R]
+  const int32_t* off;       // [R + 1]
+  int64_t x_stride;
+  int cols, rank, adapters, R;
+};
+hipError_t launch_adapter_gemm(const AdapterArgs& a, const LowRank& lr, hipStream_t s);
+// Bytes of t in the workspace; the rows' adapters [N] lie behind them on the fast path.
+inline size_t adapter_t_bytes(int64_t N, int rank) { return ((size_t)N * adapter_cols(rank) * 4 + 255) & ~size_t(255); }
+
 // Attention over a 4-bit pool: HistArgs with k = the pool, kv_stride = bytes of
 // a row and page_stride = bytes of a page.
 HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16);

@@ -83,7 +83,7 @@ size_t rocs_adapter_workspace_size(int64_t R, int64_t N, int64_t K, int64_t D, i
   if (R <= 0 || N <= 0 || K < 1 || D < 1 || rank < 1 || rank > 256 || N > kMaxI32 ||
       !valid_dtype(dtype))
     return 0;
-  return align256((size_t)N * adapter_cols(rank) * 4);
+  return adapter_t_bytes(N, rank) + align256((size_t)N * 4);
 }
 
 int32_t rocs_adapter_linear(const void* x, int64_t x_row_stride, const void* w, const void* a,

@@ -16,6 +16,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "launch.h"
+#include "layer.h"
 #include "linear_rule.h"
 
 #include <atomic>
@@ -234,6 +235,13 @@ hipError_t launch_request(const LinearArgs& a, int cus, int tiles_d, int req_til
 // kernel, so the two give the same values), then the activation; the wave's
 // block goes through LDS so that a store instruction covers whole row
 // segments.
+// ADAPT: the low-rank adapters of the rows' requests (adapter.hip) as further columns
+// of K, with operands straight from global memory: B_a's rows and t's. A block
+// of 32 rows takes the adapters that its rows have one after the other, four steps of
+// loads in flight; a row keeps the products of its own (a select, not a zero in t:
+// an infinity in another request's adapter stays there). Rows behind the last request are
+// not stored.
+//
 // What bounds it: reads of the two operands through L2 (each 128 x 128 tile
 // reads 256 rows of K) and the output stores; the slab depth, the request rows
 // in the prologue or the epilogue and two to four waves a SIMD all measured
@@ -245,12 +253,12 @@ hipError_t launch_request(const LinearArgs& a, int cus, int tiles_d, int req_til
 // ---------------------------------------------------------------------------
 __device__ __constant__ u32x4 g_zero_chunk = {0u, 0u, 0u, 0u};
 
-template <int BM, int BN, int BK, int S, bool HAS_ADD, int WVM>
+template <int BM, int BN, int BK, int S, bool HAS_ADD, int WVM, bool ADAPT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 void ikbo_gemm_tile(
     const bf16_t* __restrict__ x, const bf16_t* __restrict__ xadd, const bf16_t* __restrict__ w,
     const float* __restrict__ z, const int32_t* __restrict__ ids, bf16_t* __restrict__ out,
-    int64_t N, int K, int D, int tiles_m, int relu, int R) {
+    int64_t N, int K, int D, int tiles_m, int relu, int R, LowRank lr) {
   constexpr int WM = BM / WVM, WN = BN / (4 / WVM);   // wave block
   constexpr int FM = WM / 32, FN = WN / 32;
   constexpr bool ZLATE = HAS_ADD;              // request rows loaded in the epilogue
@@ -274,6 +282,9 @@ void ikbo_gemm_tile(
   const int m0 = (int)(tile % (uint32_t)tiles_m) * BM;
   const int64_t n0 = (int64_t)(tile / (uint32_t)tiles_m) * BN;
   const int wm0 = wave % WVM * WM, wn0 = wave / WVM * WN;
+  const int64_t xs = ADAPT ? lr.x_stride : K;
+  const int64_t n_rows = ADAPT ? min(N, (int64_t)lr.off[lr.R]) : N;
+  if (ADAPT && n0 >= n_rows) return;
   const uint32_t lbase = lds_addr(lds);
   auto swz = [](int row) { return CPR == 8 ? (row >> 1) & 7 : (row >> 2) & 3; };
 
@@ -292,7 +303,7 @@ void ikbo_gemm_tile(
   for (int i = 0; i < NB; ++i) {
     const int row = RPI * (NB * wave + i) + lane / CPR;
     chunk_b[i] = 8 * ((lane % CPR) ^ swz(row));
-    pb[i] = reinterpret_cast<const char*>(x + min(n0 + row, N - 1) * K + chunk_b[i]);
+    pb[i] = reinterpret_cast<const char*>(x + min(n0 + row, N - 1) * xs + chunk_b[i]);
   }
   const int64_t to_add = HAS_ADD ? reinterpret_cast<const char*>(xadd) - reinterpret_cast<const char*>(x) : 0;
   const char* const zeros = reinterpret_cast<const char*>(&g_zero_chunk);
@@ -391,6 +402,53 @@ void ikbo_gemm_tile(
   }
   ring_barrier();                              // the ring is free
 
+  if constexpr (ADAPT) {
+    __shared__ int list[4][32];                // adapters of this wave's 32 rows
+    const int steps = lr.cols / 16;
+#pragma unroll
+    for (int fn = 0; fn < FN; ++fn) {
+      const int64_t n = n0 + wn0 + 32 * fn + l32;
+      const int mine = n < n_rows ? lr.aid[n] : -1;
+      const bf16_t* t = lr.t + min(n, n_rows - 1) * lr.cols + 8 * hh;
+      int count = 0;
+      for (uint64_t todo = __ballot(mine >= 0); todo != 0; ++count) {
+        const int id = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
+        todo &= ~__ballot(mine == id);
+        if (lane == 0) list[wave][count] = id;
+      }
+      wait_lgkmcnt0();                         // the list is in LDS (one wave's own)
+      asm volatile("" ::: "memory");
+      constexpr int U = FM == 1 ? 4 : 2;       // steps in flight
+      for (int p0 = 0; p0 < count * steps; p0 += U) {
+        u32x4 wb[U][FM], tb[U];
+        int id[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int p = min(p0 + u, count * steps - 1), at = p % steps;
+          id[u] = __builtin_amdgcn_readfirstlane(list[wave][p / steps]);
+#pragma unroll
+          for (int fm = 0; fm < FM; ++fm) {
+            const int d = min(m0 + wm0 + 32 * fm + l32, D - 1);
+            wb[u][fm] = load16(lr.b + ((int64_t)id[u] * D + d) * lr.rank + 16 * at + 8 * hh,
+                               16 * at + 8 * hh < lr.rank);
+          }
+          tb[u] = *reinterpret_cast<const u32x4*>(t + 16 * at);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (p0 + u >= count * steps) break;
+          const bool own = mine == id[u];
+#pragma unroll
+          for (int fm = 0; fm < FM; ++fm) {
+            const f32x16 y = mfma32(as_bf16x8(wb[u][fm]), as_bf16x8(tb[u]), acc[fm][fn]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[fm][fn][e] = own ? y[e] : acc[fm][fn][e];
+          }
+        }
+      }
+    }
+  }
+
   // Element 4 q + i of acc[fm][fn] is feature 32 fm + 8 q + 4 hh + i of
   // candidate 32 fn + l32. After the half-wave swap lane (l32, hh) holds
   // features 32 fm + 16 j + 8 hh .. + 7: one 16-byte chunk of its row in the
@@ -433,7 +491,7 @@ void ikbo_gemm_tile(
             lds3 + st + r * ORB + 16 * (c ^ (r & (ORB / 16 - 1))));
         const int64_t n = nw + 32 * fn + r;
         const int d = dw + 8 * c;
-        if (n < N && d < D) *reinterpret_cast<u32x4*>(out + n * D + d) = v;
+        if (n < n_rows && d < D) *reinterpret_cast<u32x4*>(out + n * D + d) = v;
       }
     } else {
       constexpr int LPR = ORB / 8;
@@ -444,7 +502,7 @@ void ikbo_gemm_tile(
             lds3 + st + r * ORB + 16 * ((c >> 1) ^ (r & (ORB / 16 - 1))) + 8 * (c & 1));
         const int64_t n = nw + 32 * fn + r;
         const int d = dw + 4 * c;
-        if (n < N && d < D) *reinterpret_cast<u32x2*>(out + n * D + d) = v;
+        if (n < n_rows && d < D) *reinterpret_cast<u32x2*>(out + n * D + d) = v;
       }
     }
   }
@@ -490,6 +548,10 @@ void ikbo_gemm_tile(
 // the last slab has just released (after a barrier): 32 rows at a time
 // written in that layout, read back row-contiguous, and stored as 8 rows x
 // 128 bytes per instruction.
+//
+// ADAPT: tiles hold rows of one request, so all of a tile's rows have one low-rank adapter
+// (adapter.hip): rank / 16 further steps after the tile's last, operands (B_a's rows and
+// t's) straight from global memory.
 //
 // Rows past the tile's end are clamped loads whose results are not stored.
 // ---------------------------------------------------------------------------
@@ -581,12 +643,12 @@ uint64_t next_epoch() {
   return counter.fetch_add(1, std::memory_order_relaxed);
 }
 
-template <bool HAS_ZB, bool RELU, bool FUSED>
+template <bool HAS_ZB, bool RELU, bool FUSED, bool ADAPT = false>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w,
                       const float* __restrict__ zb, const int32_t* __restrict__ off_g,
                       bf16_t* __restrict__ out, int R, int64_t N, int K, int D, int tiles_m,
-                      int n_slots, StreamStep step_g, FusedRequest fr) {
+                      int n_slots, StreamStep step_g, FusedRequest fr, LowRank lr) {
   constexpr int BM = kStreamBM, BN = kStreamBN, BK = kStreamBK;
   constexpr int NSA = 2, NSB = 3;                // ring depths: weights, candidates
   constexpr int ROWB = BK * 2;                   // bytes of one slab row (128)
@@ -789,7 +851,7 @@ void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w
   f32x4 zv[2][4];
   auto load_zb = [&](const StreamTile& c) __attribute__((always_inline)) {
     if constexpr (HAS_ZB) {
-      const auto rz = buffer_rsrc(zb + (int64_t)c.r * D, (uint32_t)D * 4u);
+      const auto rz = buffer_rsrc(zb + (ADAPT ? 0 : (int64_t)c.r * D), (uint32_t)D * 4u);
       const uint32_t vo = 4u * (uint32_t)(c.m0 + wm0 + h4);
 #pragma unroll
       for (int fm = 0; fm < 2; ++fm)
@@ -797,6 +859,31 @@ void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w
         for (int q = 0; q < 4; ++q)
           zv[fm][q] = __builtin_bit_cast(
               f32x4, __builtin_amdgcn_raw_buffer_load_b128(rz, vo + 4u * (32 * fm + 8 * q), 0, 0));
+    }
+  };
+
+  // The adapter of the tile's request, added to the tile's sums.
+  auto add_adapter = [&](const StreamTile& c) __attribute__((always_inline)) {
+    const int id = __builtin_amdgcn_readfirstlane(lr.ids[c.r]);
+    if ((uint32_t)id >= (uint32_t)lr.adapters) return;
+    const bf16_t* pb[2];
+    const bf16_t* pt[4];
+#pragma unroll
+    for (int fm = 0; fm < 2; ++fm)
+      pb[fm] = lr.b + ((int64_t)id * D + min(c.m0 + wm0 + 32 * fm + l32, D - 1)) * lr.rank + 8 * hh;
+#pragma unroll
+    for (int fn = 0; fn < 4; ++fn)
+      pt[fn] = lr.t + (c.n0 + min(wn0 + 32 * fn + l32, c.rows - 1)) * lr.cols + 8 * hh;
+    for (int j = 0; j < lr.rank; j += 16) {
+      bf16x8 wb[2], tb[4];
+#pragma unroll
+      for (int fm = 0; fm < 2; ++fm) wb[fm] = as_bf16x8(load16(pb[fm] + j, j + 8 * hh < lr.rank));
+#pragma unroll
+      for (int fn = 0; fn < 4; ++fn) tb[fn] = *reinterpret_cast<const bf16x8*>(pt[fn] + j);
+#pragma unroll
+      for (int fm = 0; fm < 2; ++fm)
+#pragma unroll
+        for (int fn = 0; fn < 4; ++fn) acc[fm][fn] = mfma32(wb[fm], tb[fn], acc[fm][fn]);
     }
   };
 
@@ -963,6 +1050,7 @@ void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w
     cbuf_b = cbuf_b == NSB - 1 ? 0 : cbuf_b + 1;
     if constexpr (kLast) {
       ring_barrier();                            // every wave is past the slab's fragments
+      if constexpr (ADAPT) add_adapter(cc);
       load_zb(cc);
       wait_vmcnt<0>();
       store_tile(cc, released + (uint32_t)wave * 4096u);
@@ -1123,12 +1211,23 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t s) {
   const int tiles_m = (int)((a.d_out + BM - 1) / BM);
   const int64_t grid = tiles_m * ((a.N + BN - 1) / BN);
   if (!grid_fits(grid, 256)) return hipErrorInvalidConfiguration;
-  return launch_kernel(ikbo_gemm_tile<BM, BN, BK, S, HAS_ADD, WVM>, dim3((uint32_t)grid), dim3(256), s,
+  return launch_kernel(ikbo_gemm_tile<BM, BN, BK, S, HAS_ADD, WVM, false>, dim3((uint32_t)grid), dim3(256), s,
                        static_cast<const bf16_t*>(a.x_cand),
                        static_cast<const bf16_t*>(a.x_cand_add),
                        static_cast<const bf16_t*>(a.w_cand), a.k_req > 0 ? a.z : a.bias,
                        a.k_req > 0 ? a.ids : nullptr, static_cast<bf16_t*>(a.out), a.N,
-                       (int)a.k_cand, (int)a.d_out, tiles_m, (int)a.relu, (int)a.R);
+                       (int)a.k_cand, (int)a.d_out, tiles_m, (int)a.relu, (int)a.R, LowRank{});
+}
+
+template <int BM, int BN, int BK, int S>
+hipError_t launch_adapter_tile(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
+  const int tiles_m = (a.D + BM - 1) / BM;
+  const int64_t grid = tiles_m * ((a.N + BN - 1) / BN);
+  if (!grid_fits(grid, 256)) return hipErrorInvalidConfiguration;
+  return launch_kernel(ikbo_gemm_tile<BM, BN, BK, S, false, 2, true>, dim3((uint32_t)grid), dim3(256), s,
+                       static_cast<const bf16_t*>(a.x), static_cast<const bf16_t*>(nullptr),
+                       static_cast<const bf16_t*>(a.w), a.bias, static_cast<const int32_t*>(nullptr),
+                       static_cast<bf16_t*>(a.out), a.N, a.K, a.D, tiles_m, a.relu, 1, lr);
 }
 
 template <typename T>
@@ -1261,7 +1360,7 @@ hipError_t launch_linear(const LinearArgs& a, bool fast, hipStream_t s) {
     auto go = [&](auto kernel) {
       return launch_kernel(kernel, dim3((uint32_t)grid), dim3(512), s, x, w, zb, off, o,
                            (int)a.R, a.N, (int)a.k_cand, (int)a.d_out, tiles_m, (int)slots, step,
-                           fr);
+                           fr, LowRank{});
     };
     if (fused)
       return a.relu ? go(ikbo_gemm_stream<true, true, true>) : go(ikbo_gemm_stream<true, false, true>);
@@ -1283,6 +1382,30 @@ hipError_t launch_linear(const LinearArgs& a, bool fast, hipStream_t s) {
                            : launch_tile<128, 128, 32, 2, true>(a, s);
   }
   return small ? launch_tile<64, 64, 64, 3, false>(a, s) : launch_tile<128, 128, 32, 3, false>(a, s);
+}
+
+// The projection of an adapter call, with t and the rows' adapters formed.
+hipError_t launch_adapter_gemm(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
+  int cus = 0;
+  const hipError_t ce = current_cu_count(&cus);
+  if (ce != hipSuccess) return ce;
+  const int64_t slots = stream_slots(a.N, a.R), tiles_m = (a.D + kStreamBM - 1) / kStreamBM;
+  const bool can_stream = a.x_stride == a.K && a.K % kStreamBK == 0 && slots * tiles_m < (int64_t(1) << 31);
+  if (can_stream && stream_pays(a.N, a.D, a.K, a.R, cus)) {
+    const int64_t n_tiles = slots * tiles_m;
+    const int grid = (int)(n_tiles < cus ? n_tiles : cus);
+    const StreamStep step{(int)(grid / tiles_m), (int)(grid % tiles_m)};
+    auto go = [&](auto kernel) {
+      return launch_kernel(kernel, dim3((uint32_t)grid), dim3(512), s, static_cast<const bf16_t*>(a.x),
+                           static_cast<const bf16_t*>(a.w), a.bias, a.off, static_cast<bf16_t*>(a.out),
+                           a.R, a.N, a.K, a.D, (int)tiles_m, (int)slots, step, FusedRequest{}, lr);
+    };
+    if (a.bias != nullptr)
+      return a.relu ? go(ikbo_gemm_stream<true, true, false, true>) : go(ikbo_gemm_stream<true, false, false, true>);
+    return a.relu ? go(ikbo_gemm_stream<false, true, false, true>) : go(ikbo_gemm_stream<false, false, false, true>);
+  }
+  const bool small = (int64_t)((a.D + 127) / 128) * ((a.N + 127) / 128) < cus;
+  return small ? launch_adapter_tile<64, 64, 64, 3>(a, lr, s) : launch_adapter_tile<128, 128, 32, 3>(a, lr, s);
 }
 
 }  // namespace rocs
