@@ -117,94 +117,175 @@ __global__ __launch_bounds__(256) void adapter_general(const AdapterArgs a, int 
 // bf16 step of the adapter's part of the result, and lets its product with B run at
 // the bf16 rate), and the rows' adapters.
 //
-// A workgroup takes 32 RB rows of one request (tiles as in common.h: tile_base) and all
-// of the rank, 32 RK columns at a time; its eight waves split K, operands straight from
-// global memory, and add up through LDS in a fixed order.
+// Requests of few rows: a workgroup takes 32 rows of one request (tiles as in common.h:
+// tile_base) and all of the rank, 32 RK columns at a time; its eight waves split K,
+// operands straight from global memory, and add up through LDS in a fixed order.
+// Requests of many rows take the tiled linear (linear.hip: SHRINK).
 // ---------------------------------------------------------------------------
-template <int RB, int RK>
-__global__ __launch_bounds__(512) void shrink_rows(const AdapterArgs a, bf16_t* __restrict__ t,
-                                                   int32_t* __restrict__ aid, int cols) {
-  constexpr int TILE = 32 * RB;
-  constexpr int U = RB == 1 ? 8 : 2;           // steps of a wave in flight
+template <int RK>
+__global__ __launch_bounds__(512) void shrink_rows(const AdapterArgs a, const LowRank lr) {
+  constexpr int U = 8 / RK;                    // steps of a wave in flight
   __shared__ f32x4 red[8][4][kWave];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hh = lane >> 5;
-  const int r = request_of_slot(a.off, a.R, blockIdx.x, 1, TILE);
+  const int r = request_of_slot(a.off, a.R, blockIdx.x, 1, 32);
   const int64_t end = min((int64_t)a.off[r + 1], a.N);
-  const int64_t n0 = a.off[r] + ((int64_t)blockIdx.x - tile_base(a.off, r, 1, TILE)) * TILE;
-  const int rows = (int)max(min(end - n0, (int64_t)TILE), (int64_t)0);
+  const int64_t n0 = a.off[r] + ((int64_t)blockIdx.x - tile_base(a.off, r, 1, 32)) * 32;
+  const int rows = (int)max(min(end - n0, (int64_t)32), (int64_t)0);
   if (rows == 0) return;
   const int given = a.ids[r], id = (uint32_t)given < (uint32_t)a.A ? given : -1;
-  for (int i = tid; i < rows; i += 512) aid[n0 + i] = id;
+  if (tid < rows) lr.aid[n0 + tid] = id;
   if (id < 0) return;
   const float scale = a.scales != nullptr ? a.scales[id] : 1.f;
-  const bf16_t* x[RB];
-#pragma unroll
-  for (int b = 0; b < RB; ++b)
-    x[b] = static_cast<const bf16_t*>(a.x) + (n0 + min(32 * b + l32, rows - 1)) * a.x_stride + 8 * hh;
+  bf16_t* const t = const_cast<bf16_t*>(lr.t);
+  const bf16_t* x = static_cast<const bf16_t*>(a.x) + (n0 + min(l32, rows - 1)) * a.x_stride + 8 * hh;
   for (int j0 = 0; j0 < a.rank; j0 += 32 * RK) {
     const bf16_t* w[RK];
 #pragma unroll
     for (int k = 0; k < RK; ++k)
       w[k] = static_cast<const bf16_t*>(a.a) + ((int64_t)id * a.rank + min(j0 + 32 * k + l32, a.rank - 1)) * a.K + 8 * hh;
-    f32x16 acc[RK][RB];
+    f32x16 acc[RK];
 #pragma unroll
-    for (int k = 0; k < RK; ++k)
-#pragma unroll
-      for (int b = 0; b < RB; ++b) acc[k][b] = f32x16{};
-    for (int k0 = 16 * wave; k0 < a.K; k0 += 128 * U) {
-      u32x4 av[U][RK], xv[U][RB];
+    for (int k = 0; k < RK; ++k) acc[k] = f32x16{};
+    // Step s of a wave: 16 k; four steps are a 128-byte line of each row.
+    auto k_of = [&](int s) { return 512 * (s / 4) + 64 * wave + 16 * (s % 4); };
+    for (int s = 0; k_of(s) < a.K; s += U) {
+      u32x4 av[U][RK], xv[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int k = k0 + 128 * u;
+        const int k = k_of(s + u);
         const bool ok = k + 8 * hh < a.K;
 #pragma unroll
         for (int i = 0; i < RK; ++i) av[u][i] = load16(w[i] + k, ok);
-#pragma unroll
-        for (int b = 0; b < RB; ++b) xv[u][b] = load16(x[b] + k, ok);
+        xv[u] = load16(x + k, ok);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (k0 + 128 * u >= a.K) break;
+        if (k_of(s + u) >= a.K) break;
 #pragma unroll
-        for (int i = 0; i < RK; ++i)
-#pragma unroll
-          for (int b = 0; b < RB; ++b) acc[i][b] = mfma32(as_bf16x8(av[u][i]), as_bf16x8(xv[u][b]), acc[i][b]);
+        for (int i = 0; i < RK; ++i) acc[i] = mfma32(as_bf16x8(av[u][i]), as_bf16x8(xv[u]), acc[i]);
       }
     }
     // Quad q of a block: columns 8 q + 4 hh .. + 3 of row l32.
 #pragma unroll
-    for (int i = 0; i < RK; ++i)
+    for (int i = 0; i < RK; ++i) {
 #pragma unroll
-      for (int b = 0; b < RB; ++b) {
+      for (int q = 0; q < 4; ++q)
+        red[wave][q][lane] = f32x4{acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
+      __syncthreads();
+      if (tid < 256) {
+        const int q = tid >> 6;
+        f32x4 s = red[0][q][lane];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          red[wave][q][lane] = f32x4{acc[i][b][4 * q], acc[i][b][4 * q + 1], acc[i][b][4 * q + 2], acc[i][b][4 * q + 3]};
-        __syncthreads();
-        if (tid < 256) {
-          const int q = tid >> 6;
-          f32x4 s = red[0][q][lane];
-#pragma unroll
-          for (int w8 = 1; w8 < 8; ++w8) s += red[w8][q][lane];
-          const int j = j0 + 32 * i + 8 * q + 4 * hh;
-          if (j >= a.rank) s = f32x4{0.f, 0.f, 0.f, 0.f};       // the rank is a multiple of 8
-          else s *= scale;
-          if (32 * b + l32 < rows && j < cols)
-            *reinterpret_cast<u32x2*>(t + (n0 + 32 * b + l32) * cols + j) =
-                u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
-        }
-        __syncthreads();
+        for (int w8 = 1; w8 < 8; ++w8) s += red[w8][q][lane];
+        const int j = j0 + 32 * i + 8 * q + 4 * hh;
+        if (l32 < rows && j < a.rank)
+          *reinterpret_cast<u32x2*>(t + (n0 + l32) * lr.cols + j) =
+              u32x2{pack_bf16x2(s[0] * scale, s[1] * scale), pack_bf16x2(s[2] * scale, s[3] * scale)};
       }
+      __syncthreads();
+    }
   }
 }
 
-template <int RB, int RK>
-hipError_t launch_shrink(const AdapterArgs& a, bf16_t* t, int32_t* aid, hipStream_t s) {
-  const int64_t slots = a.R + (a.N + 32 * RB - 1) / (32 * RB);
+template <int RK>
+hipError_t launch_shrink(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
+  const int64_t slots = a.R + (a.N + 31) / 32;
   if (!grid_fits(slots, 512)) return hipErrorInvalidConfiguration;
-  return launch_kernel(shrink_rows<RB, RK>, dim3((uint32_t)slots), dim3(512), s, a, t, aid,
-                       adapter_cols(a.rank));
+  return launch_kernel(shrink_rows<RK>, dim3((uint32_t)slots), dim3(512), s, a, lr);
+}
+
+// ---------------------------------------------------------------------------
+// Fast path, few rows: 32 features x 32 rows a workgroup, whose four waves split K
+// and then the rows' adapters; operands straight from global memory, partial sums
+// added up through LDS in a fixed order. A row keeps the products of its own adapter
+// by a select.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void adapter_few(const AdapterArgs a, const LowRank lr, int tiles_m) {
+  constexpr int U = 8;                         // steps of a wave in flight
+  __shared__ f32x4 red[4][4][kWave];
+  __shared__ int list[4][32];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, hh = lane >> 5;
+  const int d0 = (int)(blockIdx.x % (uint32_t)tiles_m) * 32;
+  const int64_t n0 = (int64_t)(blockIdx.x / (uint32_t)tiles_m) * 32;
+  const int64_t n_rows = rows_of(a);
+  if (n0 >= n_rows) return;
+  const int64_t n = min(n0 + l32, n_rows - 1);
+  const int d = min(d0 + l32, a.D - 1);
+  const int mine = n0 + l32 < n_rows ? lr.aid[n] : -1;
+  const bf16_t* x = static_cast<const bf16_t*>(a.x) + n * a.x_stride + 8 * hh;
+  const bf16_t* w = static_cast<const bf16_t*>(a.w) + (int64_t)d * a.K + 8 * hh;
+  f32x16 acc = {};
+  auto k_of = [&](int s) { return 256 * (s / 4) + 64 * wave + 16 * (s % 4); };
+  for (int s = 0; k_of(s) < a.K; s += U) {
+    u32x4 wv[U], xv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k_of(s + u);
+      const bool ok = k + 8 * hh < a.K;
+      wv[u] = load16(w + k, ok);
+      xv[u] = load16(x + k, ok);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k_of(s + u) >= a.K) break;
+      acc = mfma32(as_bf16x8(wv[u]), as_bf16x8(xv[u]), acc);
+    }
+  }
+  int count = 0;
+  for (uint64_t todo = __ballot(mine >= 0); todo != 0; ++count) {
+    const int id = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
+    todo &= ~__ballot(mine == id);
+    if (lane == 0) list[wave][count] = id;
+  }
+  wait_lgkmcnt0();                             // the list is in LDS (one wave's own)
+  asm volatile("" ::: "memory");
+  const int steps = lr.cols / 16, pairs = count * steps;
+  const bf16_t* t = lr.t + n * lr.cols + 8 * hh;
+  for (int p0 = wave; p0 < pairs; p0 += 4 * U) {
+    u32x4 wv[U], tv[U];
+    int id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = min(p0 + 4 * u, pairs - 1), at = 16 * (p % steps);
+      id[u] = __builtin_amdgcn_readfirstlane(list[wave][p / steps]);
+      const bool ok = at + 8 * hh < lr.rank;
+      wv[u] = load16(lr.b + ((int64_t)id[u] * a.D + d) * lr.rank + at + 8 * hh, ok);
+      tv[u] = load16(t + at, ok && mine == id[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p0 + 4 * u >= pairs) break;
+      const f32x16 y = mfma32(as_bf16x8(wv[u]), as_bf16x8(tv[u]), acc);
+      const bool own = mine == id[u];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[e] = own ? y[e] : acc[e];
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    red[wave][q][lane] = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+  __syncthreads();
+  // Quad `wave`: features 8 wave + 4 hh .. + 3 of row l32.
+  f32x4 s = ((red[0][wave][lane] + red[1][wave][lane]) + red[2][wave][lane]) + red[3][wave][lane];
+  const int df = d0 + 8 * wave + 4 * hh;
+  if (n0 + l32 >= n_rows || df >= a.D) return;
+  if (a.bias != nullptr)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] += a.bias[df + i];
+  const uint32_t lo = act_floor(a.relu);
+  *reinterpret_cast<u32x2*>(static_cast<bf16_t*>(a.out) + n * a.D + df) =
+      u32x2{act_bf16x2(pack_bf16x2(s[0], s[1]), lo), act_bf16x2(pack_bf16x2(s[2], s[3]), lo)};
+}
+
+hipError_t launch_few(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
+  const int tiles_m = (a.D + 31) / 32;
+  const int64_t blocks = (a.N + 31) / 32 * tiles_m;
+  if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+  return launch_kernel(adapter_few, dim3((uint32_t)blocks), dim3(256), s, a, lr, tiles_m);
 }
 
 template <typename T>
@@ -232,13 +313,14 @@ hipError_t launch_adapter(const AdapterArgs& a, bool fast, hipStream_t s) {
   if (!fast) return a.bf16 ? launch_general<bf16_t>(a, s) : launch_general<float>(a, s);
   bf16_t* t = static_cast<bf16_t*>(a.t);
   int32_t* aid = reinterpret_cast<int32_t*>(static_cast<char*>(a.t) + adapter_t_bytes(a.N, a.rank));
-  const bool tall = a.N / a.R >= 128;
-  const hipError_t e = tall ? (a.rank > 32 ? launch_shrink<4, 2>(a, t, aid, s) : launch_shrink<4, 1>(a, t, aid, s))
-                            : (a.rank > 32 ? launch_shrink<1, 2>(a, t, aid, s) : launch_shrink<1, 1>(a, t, aid, s));
+  const LowRank lr{t, static_cast<const bf16_t*>(a.b), aid, a.off, a.x_stride, adapter_cols(a.rank), a.rank,
+                   a.A, a.R};
+  const hipError_t e = a.N / a.R >= 64 ? launch_adapter_shrink(a, lr, s)
+                       : a.rank > 32   ? launch_shrink<2>(a, lr, s)
+                                       : launch_shrink<1>(a, lr, s);
   if (e != hipSuccess) return e;
-  const LowRank lr{t, static_cast<const bf16_t*>(a.b), aid, a.ids, a.off, a.x_stride, adapter_cols(a.rank),
-                   a.rank, a.A, a.R};
-  return launch_adapter_gemm(a, lr, s);
+  const int64_t tiles = (int64_t)((a.N + 63) / 64) * ((a.D + 63) / 64);
+  return tiles < 128 ? launch_few(a, lr, s) : launch_adapter_gemm(a, lr, s);
 }
 
 }  // namespace rocs

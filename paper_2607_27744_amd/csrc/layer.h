@@ -63,14 +63,14 @@ hipError_t launch_adapter(const AdapterArgs& a, bool fast, hipStream_t s);
 
 // What the fast path's product reads beside x and W.
 struct LowRank {
-  const __bf16* t;          // [N, cols]: s A x, rounded; zeros from rank on
+  const __bf16* t;          // [N, cols]: s A x, rounded; nothing from rank on
   const __bf16* b;          // [A, D, rank]
-  const int32_t* aid;       // [N] each row's adapter, or -1
-  const int32_t* ids;       // [R]
+  int32_t* aid;             // [N] each row's adapter, or -1
   const int32_t* off;       // [R + 1]
   int64_t x_stride;
   int cols, rank, adapters, R;
 };
+hipError_t launch_adapter_shrink(const AdapterArgs& a, const LowRank& lr, hipStream_t s);
 hipError_t launch_adapter_gemm(const AdapterArgs& a, const LowRank& lr, hipStream_t s);
 // Bytes of t in the workspace; the rows' adapters [N] lie behind them on the fast path.
 inline size_t adapter_t_bytes(int64_t N, int rank) { return ((size_t)N * adapter_cols(rank) * 4 + 255) & ~size_t(255); }

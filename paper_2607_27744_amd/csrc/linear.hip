@@ -237,10 +237,10 @@ hipError_t launch_request(const LinearArgs& a, int cus, int tiles_d, int req_til
 // segments.
 // ADAPT: the low-rank adapters of the rows' requests (adapter.hip) as further columns
 // of K, with operands straight from global memory: B_a's rows and t's. A block
-// of 32 rows takes the adapters that its rows have one after the other, four steps of
-// loads in flight; a row keeps the products of its own (a select, not a zero in t:
-// an infinity in another request's adapter stays there). Rows behind the last request are
-// not stored.
+// of 32 rows takes the adapters that its rows have one after the other, with t
+// zero for the others' rows. Rows behind the last request are not stored.
+// SHRINK: t itself: W is the adapter A_a of the tile's request, tiles do not straddle two,
+// and the rows' adapters are written beside it.
 //
 // What bounds it: reads of the two operands through L2 (each 128 x 128 tile
 // reads 256 rows of K) and the output stores; the slab depth, the request rows
@@ -253,7 +253,40 @@ hipError_t launch_request(const LinearArgs& a, int cus, int tiles_d, int req_til
 // ---------------------------------------------------------------------------
 __device__ __constant__ u32x4 g_zero_chunk = {0u, 0u, 0u, 0u};
 
-template <int BM, int BN, int BK, int S, bool HAS_ADD, int WVM, bool ADAPT>
+// Rows of a tile whose block met an infinity or NaN in another row's adapter (0 times
+// either is NaN), formed again one by one: `mask` of the 32 rows from n0, features from
+// d0, a lane each. Slow (a wave's dot products from global memory).
+__device__ __noinline__ void adapter_rows_again(const bf16_t* x, const bf16_t* w, const float* bias,
+                                                bf16_t* out, const LowRank lr, int64_t n0, uint32_t mask,
+                                                int d0, int width, int K, int D, int relu) {
+  const int lane = (int)(threadIdx.x & 63), d = d0 + lane;
+  const bool dok = lane < width && d < D;
+  while (mask != 0) {
+    const int64_t n = n0 + __builtin_ctz(mask);
+    mask &= mask - 1;
+    const int id = lr.aid[n];
+    if (!dok) continue;
+    float sum = 0.f;
+    for (int k = 0; k < K; ++k) sum += load_f32(x + n * lr.x_stride + k) * load_f32(w + (int64_t)d * K + k);
+    if (id >= 0)
+      for (int j = 0; j < lr.rank; ++j)
+        sum += load_f32(lr.t + n * lr.cols + j) * load_f32(lr.b + ((int64_t)id * D + d) * lr.rank + j);
+    if (bias != nullptr) sum += bias[d];
+    const uint32_t p = act_bf16x2(pack_bf16x2(sum, 0.f), act_floor(relu));
+    reinterpret_cast<uint16_t*>(out)[n * D + d] = (uint16_t)p;
+  }
+}
+
+// Whether one of eight bf16 values is an infinity or NaN.
+__device__ __forceinline__ bool any_odd(u32x4 v) {
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    odd = odd || (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
+  return odd;
+}
+
+template <int BM, int BN, int BK, int S, bool HAS_ADD, int WVM, bool ADAPT = false, bool SHRINK = false>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 void ikbo_gemm_tile(
     const bf16_t* __restrict__ x, const bf16_t* __restrict__ xadd, const bf16_t* __restrict__ w,
@@ -280,11 +313,28 @@ void ikbo_gemm_tile(
   const int l32 = lane & 31, hh = lane >> 5;
   const uint32_t tile = xcd_remap(blockIdx.x, gridDim.x);
   const int m0 = (int)(tile % (uint32_t)tiles_m) * BM;
-  const int64_t n0 = (int64_t)(tile / (uint32_t)tiles_m) * BN;
+  int64_t n0 = (int64_t)(tile / (uint32_t)tiles_m) * BN;
   const int wm0 = wave % WVM * WM, wn0 = wave / WVM * WN;
-  const int64_t xs = ADAPT ? lr.x_stride : K;
-  const int64_t n_rows = ADAPT ? min(N, (int64_t)lr.off[lr.R]) : N;
-  if (ADAPT && n0 >= n_rows) return;
+  const int64_t xs = ADAPT || SHRINK ? lr.x_stride : K;
+  int64_t n_rows = N;
+  float scale = 1.f;
+  if constexpr (ADAPT) {
+    n_rows = min(N, (int64_t)lr.off[lr.R]);
+    if (n0 >= n_rows) return;
+  }
+  if constexpr (SHRINK) {
+    const int64_t slot = tile / (uint32_t)tiles_m;
+    const int r = request_of_slot(lr.off, lr.R, slot, 1, BN);
+    n0 = lr.off[r] + (slot - tile_base(lr.off, r, 1, BN)) * BN;
+    n_rows = min(min((int64_t)lr.off[r + 1], n0 + BN), N);
+    if (n0 >= n_rows) return;
+    const int given = ids[r], id = (uint32_t)given < (uint32_t)lr.adapters ? given : -1;
+    if (m0 == 0)
+      for (int i = tid; i < (int)(n_rows - n0); i += 256) lr.aid[n0 + i] = id;
+    if (id < 0) return;
+    if (z != nullptr) scale = z[id];
+    w += (int64_t)id * D * K;
+  }
   const uint32_t lbase = lds_addr(lds);
   auto swz = [](int row) { return CPR == 8 ? (row >> 1) & 7 : (row >> 2) & 3; };
 
@@ -303,7 +353,7 @@ void ikbo_gemm_tile(
   for (int i = 0; i < NB; ++i) {
     const int row = RPI * (NB * wave + i) + lane / CPR;
     chunk_b[i] = 8 * ((lane % CPR) ^ swz(row));
-    pb[i] = reinterpret_cast<const char*>(x + min(n0 + row, N - 1) * xs + chunk_b[i]);
+    pb[i] = reinterpret_cast<const char*>(x + min(n0 + row, (SHRINK ? n_rows : N) - 1) * xs + chunk_b[i]);
   }
   const int64_t to_add = HAS_ADD ? reinterpret_cast<const char*>(xadd) - reinterpret_cast<const char*>(x) : 0;
   const char* const zeros = reinterpret_cast<const char*>(&g_zero_chunk);
@@ -332,7 +382,7 @@ void ikbo_gemm_tile(
 #pragma unroll
   for (int fn = 0; fn < FN; ++fn) {
     const int64_t n = min(n0 + wn0 + 32 * fn + l32, N - 1);
-    rq[fn] = ids != nullptr ? (int)min((uint32_t)ids[n], (uint32_t)(R - 1)) : 0;
+    rq[fn] = !SHRINK && ids != nullptr ? (int)min((uint32_t)ids[n], (uint32_t)(R - 1)) : 0;
   }
 #pragma unroll
   for (int s = 0; s < S - 1; ++s)
@@ -345,7 +395,7 @@ void ikbo_gemm_tile(
       for (int q = 0; q < 4; ++q) {
         const int d = m0 + wm0 + 32 * fm + 8 * q + 4 * hh;
         zv[fn % ZFN][fm][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (z != nullptr && d < D)
+        if (!SHRINK && z != nullptr && d < D)
           zv[fn % ZFN][fm][q] = *reinterpret_cast<const f32x4*>(z + (int64_t)rq[fn] * D + d);
       }
   };
@@ -402,6 +452,7 @@ void ikbo_gemm_tile(
   }
   ring_barrier();                              // the ring is free
 
+  uint32_t again = 0;                          // bits: blocks of 32 rows to form again
   if constexpr (ADAPT) {
     __shared__ int list[4][32];                // adapters of this wave's 32 rows
     const int steps = lr.cols / 16;
@@ -416,34 +467,33 @@ void ikbo_gemm_tile(
         todo &= ~__ballot(mine == id);
         if (lane == 0) list[wave][count] = id;
       }
+      const bool mixed = count > 1 || (count == 1 && __ballot(n < n_rows && mine < 0) != 0);
       wait_lgkmcnt0();                         // the list is in LDS (one wave's own)
       asm volatile("" ::: "memory");
       constexpr int U = FM == 1 ? 4 : 2;       // steps in flight
       for (int p0 = 0; p0 < count * steps; p0 += U) {
         u32x4 wb[U][FM], tb[U];
-        int id[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int p = min(p0 + u, count * steps - 1), at = p % steps;
-          id[u] = __builtin_amdgcn_readfirstlane(list[wave][p / steps]);
+          const int id = __builtin_amdgcn_readfirstlane(list[wave][p / steps]);
+          const bool ok = 16 * at + 8 * hh < lr.rank;
 #pragma unroll
           for (int fm = 0; fm < FM; ++fm) {
             const int d = min(m0 + wm0 + 32 * fm + l32, D - 1);
-            wb[u][fm] = load16(lr.b + ((int64_t)id[u] * D + d) * lr.rank + 16 * at + 8 * hh,
-                               16 * at + 8 * hh < lr.rank);
+            wb[u][fm] = load16(lr.b + ((int64_t)id * D + d) * lr.rank + 16 * at + 8 * hh, ok);
           }
-          tb[u] = *reinterpret_cast<const u32x4*>(t + 16 * at);
+          tb[u] = load16(t + 16 * at, ok && mine == id && p0 + u < count * steps);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          if (p0 + u >= count * steps) break;
-          const bool own = mine == id[u];
+          bool odd = false;
 #pragma unroll
           for (int fm = 0; fm < FM; ++fm) {
-            const f32x16 y = mfma32(as_bf16x8(wb[u][fm]), as_bf16x8(tb[u]), acc[fm][fn]);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[fm][fn][e] = own ? y[e] : acc[fm][fn][e];
+            odd = odd || any_odd(wb[u][fm]);
+            acc[fm][fn] = mfma32(as_bf16x8(wb[u][fm]), as_bf16x8(tb[u]), acc[fm][fn]);
           }
+          if (__builtin_expect(mixed && __ballot(odd) != 0, 0)) again |= 1u << fn;
         }
       }
     }
@@ -456,6 +506,7 @@ void ikbo_gemm_tile(
   const uint32_t st = (uint32_t)(wave * 32 * ORB);
   const int64_t nw = n0 + wn0;
   const int dw = m0 + wm0;
+  const int os = SHRINK ? lr.cols : D;         // elements of an output row
   const uint32_t lo = act_floor(relu);
 #pragma unroll
   for (int fn = 0; fn < FN; ++fn) {
@@ -470,8 +521,13 @@ void ikbo_gemm_tile(
           const f32x16& a = acc[fm][fn];
           const f32x4 zq = zv[fn % ZFN][fm][2 * j + u];
           const int e = 4 * (2 * j + u);
-          p[u][0] = pack_bf16x2(a[e] + zq[0], a[e + 1] + zq[1]);
-          p[u][1] = pack_bf16x2(a[e + 2] + zq[2], a[e + 3] + zq[3]);
+          if constexpr (SHRINK) {
+            p[u][0] = pack_bf16x2(a[e] * scale, a[e + 1] * scale);
+            p[u][1] = pack_bf16x2(a[e + 2] * scale, a[e + 3] * scale);
+          } else {
+            p[u][0] = pack_bf16x2(a[e] + zq[0], a[e + 1] + zq[1]);
+            p[u][1] = pack_bf16x2(a[e + 2] + zq[2], a[e + 3] + zq[3]);
+          }
           p[u][0] = act_bf16x2(p[u][0], lo);
           p[u][1] = act_bf16x2(p[u][1], lo);
         }
@@ -491,7 +547,7 @@ void ikbo_gemm_tile(
             lds3 + st + r * ORB + 16 * (c ^ (r & (ORB / 16 - 1))));
         const int64_t n = nw + 32 * fn + r;
         const int d = dw + 8 * c;
-        if (n < n_rows && d < D) *reinterpret_cast<u32x4*>(out + n * D + d) = v;
+        if (n < n_rows && d < D) *reinterpret_cast<u32x4*>(out + n * os + d) = v;
       }
     } else {
       constexpr int LPR = ORB / 8;
@@ -502,7 +558,17 @@ void ikbo_gemm_tile(
             lds3 + st + r * ORB + 16 * ((c >> 1) ^ (r & (ORB / 16 - 1))) + 8 * (c & 1));
         const int64_t n = nw + 32 * fn + r;
         const int d = dw + 4 * c;
-        if (n < n_rows && d < D) *reinterpret_cast<u32x2*>(out + n * D + d) = v;
+        if (n < n_rows && d < D) *reinterpret_cast<u32x2*>(out + n * os + d) = v;
+      }
+    }
+  }
+  if constexpr (ADAPT) {
+    if (__builtin_expect(again != 0, 0)) {
+      wait_vmcnt<0>();                         // the rows' first stores are done
+      for (int fn = 0; fn < FN; ++fn) {
+        const int64_t left = n_rows - (nw + 32 * fn);
+        if ((again >> fn & 1) != 0 && left > 0)
+          adapter_rows_again(x, w, z, out, lr, nw + 32 * fn, left < 32 ? (1u << left) - 1u : ~0u, dw, WM, K, D, relu);
       }
     }
   }
@@ -549,9 +615,11 @@ void ikbo_gemm_tile(
 // written in that layout, read back row-contiguous, and stored as 8 rows x
 // 128 bytes per instruction.
 //
-// ADAPT: tiles hold rows of one request, so all of a tile's rows have one low-rank adapter
-// (adapter.hip): rank / 16 further steps after the tile's last, operands (B_a's rows and
-// t's) straight from global memory.
+// ADAPT: the low-rank adapters of the rows' requests (adapter.hip), rank / 16 further
+// steps after the tile's last, operands (B_a's rows and t's) straight from global memory.
+// Tiles cover the rows contiguously (in tiles that end with a request, 16 ragged
+// histories of 32,768 rows would take five rounds of the chip for four): a wave takes
+// the adapters of its 128 rows one by one, with t zero for the others' rows.
 //
 // Rows past the tile's end are clamped loads whose results are not stored.
 // ---------------------------------------------------------------------------
@@ -647,8 +715,8 @@ template <bool HAS_ZB, bool RELU, bool FUSED, bool ADAPT = false>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w,
                       const float* __restrict__ zb, const int32_t* __restrict__ off_g,
-                      bf16_t* __restrict__ out, int R, int64_t N, int K, int D, int tiles_m,
-                      int n_slots, StreamStep step_g, FusedRequest fr, LowRank lr) {
+                      bf16_t* __restrict__ out, int R, int64_t N_g, int K, int D, int tiles_m,
+                      int n_slots_g, StreamStep step_g, FusedRequest fr, LowRank lr) {
   constexpr int BM = kStreamBM, BN = kStreamBN, BK = kStreamBK;
   constexpr int NSA = 2, NSB = 3;                // ring depths: weights, candidates
   constexpr int ROWB = BK * 2;                   // bytes of one slab row (128)
@@ -664,6 +732,9 @@ void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w
   // the constant address space (scalar loads).
   const __attribute__((address_space(4))) int32_t* off =
       (const __attribute__((address_space(4))) int32_t*)off_g;
+  // Rows behind the last request are left as they are.
+  const int64_t N = ADAPT ? min(N_g, (int64_t)lr.off[lr.R]) : N_g;
+  const int n_slots = ADAPT ? (int)((N + kStreamBN - 1) / kStreamBN) : n_slots_g;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -862,29 +933,49 @@ void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w
     }
   };
 
-  // The adapter of the tile's request, added to the tile's sums.
-  auto add_adapter = [&](const StreamTile& c) __attribute__((always_inline)) {
-    const int id = __builtin_amdgcn_readfirstlane(lr.ids[c.r]);
-    if ((uint32_t)id >= (uint32_t)lr.adapters) return;
-    const bf16_t* pb[2];
-    const bf16_t* pt[4];
+  // The adapters of the wave's rows, added to its sums. Returns whether to form them
+  // again (see adapter_rows_again).
+  auto add_adapters = [&](const StreamTile& c) __attribute__((always_inline)) -> bool {
+    int mine[4];
 #pragma unroll
-    for (int fm = 0; fm < 2; ++fm)
-      pb[fm] = lr.b + ((int64_t)id * D + min(c.m0 + wm0 + 32 * fm + l32, D - 1)) * lr.rank + 8 * hh;
+    for (int fn = 0; fn < 4; ++fn) mine[fn] = lr.aid[c.n0 + min(wn0 + 32 * fn + l32, c.rows - 1)];
+    const bf16_t* pt[4];
 #pragma unroll
     for (int fn = 0; fn < 4; ++fn)
       pt[fn] = lr.t + (c.n0 + min(wn0 + 32 * fn + l32, c.rows - 1)) * lr.cols + 8 * hh;
-    for (int j = 0; j < lr.rank; j += 16) {
-      bf16x8 wb[2], tb[4];
+    uint64_t todo[4];
 #pragma unroll
-      for (int fm = 0; fm < 2; ++fm) wb[fm] = as_bf16x8(load16(pb[fm] + j, j + 8 * hh < lr.rank));
+    for (int fn = 0; fn < 4; ++fn) todo[fn] = __ballot(mine[fn] >= 0);
+    const int one = __builtin_amdgcn_readfirstlane(mine[0]);
+    const bool mixed = __ballot(mine[0] != one || mine[1] != one || mine[2] != one || mine[3] != one) != 0;
+    uint32_t again = 0;
+    while ((todo[0] | todo[1] | todo[2] | todo[3]) != 0) {
+      int id = 0;
 #pragma unroll
-      for (int fn = 0; fn < 4; ++fn) tb[fn] = *reinterpret_cast<const bf16x8*>(pt[fn] + j);
+      for (int fn = 3; fn >= 0; --fn)
+        if (todo[fn] != 0) id = __builtin_amdgcn_readlane(mine[fn], __builtin_ctzll(todo[fn]));
+      bool own[4];
 #pragma unroll
-      for (int fm = 0; fm < 2; ++fm)
+      for (int fn = 0; fn < 4; ++fn) {
+        own[fn] = mine[fn] == id;
+        todo[fn] &= ~__ballot(own[fn]);
+      }
+      for (int j = 0; j < lr.rank; j += 16) {
+        const bool in = j + 8 * hh < lr.rank;
+        u32x4 wb[2], tb[4];
 #pragma unroll
-        for (int fn = 0; fn < 4; ++fn) acc[fm][fn] = mfma32(wb[fm], tb[fn], acc[fm][fn]);
+        for (int fm = 0; fm < 2; ++fm)
+          wb[fm] = load16(lr.b + ((int64_t)id * D + min(c.m0 + wm0 + 32 * fm + l32, D - 1)) * lr.rank + j + 8 * hh, in);
+#pragma unroll
+        for (int fn = 0; fn < 4; ++fn) tb[fn] = load16(pt[fn] + j, in && own[fn]);
+        if (mixed && __ballot(any_odd(wb[0]) || any_odd(wb[1])) != 0) again = 1;
+#pragma unroll
+        for (int fm = 0; fm < 2; ++fm)
+#pragma unroll
+          for (int fn = 0; fn < 4; ++fn) acc[fm][fn] = mfma32(as_bf16x8(wb[fm]), as_bf16x8(tb[fn]), acc[fm][fn]);
+      }
     }
+    return again != 0;
   };
 
   // Combined kernel: wait (bounded) until every Zb tile's flag carries this
@@ -1050,10 +1141,22 @@ void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w
     cbuf_b = cbuf_b == NSB - 1 ? 0 : cbuf_b + 1;
     if constexpr (kLast) {
       ring_barrier();                            // every wave is past the slab's fragments
-      if constexpr (ADAPT) add_adapter(cc);
+      bool again = false;
+      if constexpr (ADAPT) again = add_adapters(cc);
       load_zb(cc);
       wait_vmcnt<0>();
       store_tile(cc, released + (uint32_t)wave * 4096u);
+      if constexpr (ADAPT) {
+        if (__builtin_expect(again, 0)) {
+          wait_vmcnt<0>();                       // the rows' first stores are done
+          for (int fn = 0; fn < 4; ++fn) {
+            const int left = cc.rows - (wn0 + 32 * fn);
+            if (left > 0)
+              adapter_rows_again(x, w, zb, out, lr, cc.n0 + wn0 + 32 * fn, left < 32 ? (1u << left) - 1u : ~0u,
+                                 cc.m0 + wm0, 64, K, D, RELU);
+          }
+        }
+      }
       if (b_next) {
         plan_b();
         dma_all(pb_src, pb_lim, pb_dst);
@@ -1211,7 +1314,7 @@ hipError_t launch_tile(const LinearArgs& a, hipStream_t s) {
   const int tiles_m = (int)((a.d_out + BM - 1) / BM);
   const int64_t grid = tiles_m * ((a.N + BN - 1) / BN);
   if (!grid_fits(grid, 256)) return hipErrorInvalidConfiguration;
-  return launch_kernel(ikbo_gemm_tile<BM, BN, BK, S, HAS_ADD, WVM, false>, dim3((uint32_t)grid), dim3(256), s,
+  return launch_kernel(ikbo_gemm_tile<BM, BN, BK, S, HAS_ADD, WVM>, dim3((uint32_t)grid), dim3(256), s,
                        static_cast<const bf16_t*>(a.x_cand),
                        static_cast<const bf16_t*>(a.x_cand_add),
                        static_cast<const bf16_t*>(a.w_cand), a.k_req > 0 ? a.z : a.bias,
@@ -1384,21 +1487,36 @@ hipError_t launch_linear(const LinearArgs& a, bool fast, hipStream_t s) {
   return small ? launch_tile<64, 64, 64, 3, false>(a, s) : launch_tile<128, 128, 32, 3, false>(a, s);
 }
 
+// t of an adapter call, and the rows' adapters.
+template <int BM, int BN, int WVM>
+static hipError_t launch_shrink_tile(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
+  const int tiles_m = (a.rank + BM - 1) / BM;
+  const int64_t grid = tiles_m * (a.R + (a.N + BN - 1) / BN);
+  if (!grid_fits(grid, 256)) return hipErrorInvalidConfiguration;
+  return launch_kernel(ikbo_gemm_tile<BM, BN, 64, 3, false, WVM, false, true>, dim3((uint32_t)grid), dim3(256), s,
+                       static_cast<const bf16_t*>(a.x), static_cast<const bf16_t*>(nullptr),
+                       static_cast<const bf16_t*>(a.a), a.scales, a.ids, const_cast<bf16_t*>(lr.t), a.N, a.K, a.rank,
+                       tiles_m, 0, 1, lr);
+}
+hipError_t launch_adapter_shrink(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
+  return a.rank <= 32 ? launch_shrink_tile<32, 128, 1>(a, lr, s) : launch_shrink_tile<64, 64, 2>(a, lr, s);
+}
+
 // The projection of an adapter call, with t and the rows' adapters formed.
 hipError_t launch_adapter_gemm(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
   int cus = 0;
   const hipError_t ce = current_cu_count(&cus);
   if (ce != hipSuccess) return ce;
-  const int64_t slots = stream_slots(a.N, a.R), tiles_m = (a.D + kStreamBM - 1) / kStreamBM;
+  const int64_t slots = stream_slots(a.N, 0), tiles_m = (a.D + kStreamBM - 1) / kStreamBM;
   const bool can_stream = a.x_stride == a.K && a.K % kStreamBK == 0 && slots * tiles_m < (int64_t(1) << 31);
-  if (can_stream && stream_pays(a.N, a.D, a.K, a.R, cus)) {
+  if (can_stream && stream_pays(a.N, a.D, a.K, 0, cus)) {
     const int64_t n_tiles = slots * tiles_m;
     const int grid = (int)(n_tiles < cus ? n_tiles : cus);
     const StreamStep step{(int)(grid / tiles_m), (int)(grid % tiles_m)};
     auto go = [&](auto kernel) {
       return launch_kernel(kernel, dim3((uint32_t)grid), dim3(512), s, static_cast<const bf16_t*>(a.x),
-                           static_cast<const bf16_t*>(a.w), a.bias, a.off, static_cast<bf16_t*>(a.out),
-                           a.R, a.N, a.K, a.D, (int)tiles_m, (int)slots, step, FusedRequest{}, lr);
+                           static_cast<const bf16_t*>(a.w), a.bias, static_cast<const int32_t*>(nullptr),
+                           static_cast<bf16_t*>(a.out), 0, a.N, a.K, a.D, (int)tiles_m, (int)slots, step, FusedRequest{}, lr);
     };
     if (a.bias != nullptr)
       return a.relu ? go(ikbo_gemm_stream<true, true, false, true>) : go(ikbo_gemm_stream<true, false, false, true>);

@@ -65,6 +65,10 @@ CASES = [  # counts, ids, k, d, rank, adapters, dtype
     ([700, 900], [0, 1], 320, 260, 64, 2, BF),
     ([130, 5, 300], [1, 1, 0], 128, 256, 136, 2, BF),
     ([40, 60], [0, 1], 64, 64, 256, 2, BF),
+    ([1] * 700 + [90, 3], [i % 41 - 1 for i in range(702)], 192, 900, 24, 40, BF),   # tiles of many adapters
+    ([1100, 1, 30, 900], [0, 2, -1, 1], 256, 1030 // 2 * 2, 40, 3, BF),
+    ([3000, 1, 0, 1999, 64, 2900], [1, 0, 0, 2, -1, 0], 256, 2048, 16, 3, BF),       # the streaming kernel
+    ([100, 28] * 64, [i % 3 - 1 for i in range(128)], 320, 2000, 72, 2, BF),
     ([5, 30], [0, 1], 100, 77, 8, 2, BF),                        # K off the fast path
     ([5, 30], [0, 1], 96, 76, 5, 2, BF), ([9], [0], 7, 3, 1, 1, BF),
     ([1, 20, 0, 3], [1, 0, 0, -1], 101, 77, 5, 2, F32), ([64, 64], [0, 1], 128, 64, 16, 2, F32),
@@ -101,7 +105,7 @@ def test_strided_rows_and_a_padded_batch(gpu_lib, dtype, k):
 
 def test_rows_without_an_adapter_are_the_projection(gpu_lib):
     # The same rows in a call with adapters and one without: rows of no adapter have the same bits.
-    for n, k, d in ((40, 256, 192), (900, 512, 256)):
+    for n, k, d in ((40, 256, 192), (900, 512, 256), (2000, 128, 1024), (8001, 256, 2048)):
         counts, ids = [n // 2, n - n // 2], [-1, 0]
         c, kw = make(counts, ids, k, d, 16, 1, BF, seed=n)
         with_one = ops.adapter_linear(**c, **kw)
@@ -125,6 +129,29 @@ def test_an_odd_row_stays_by_itself(gpu_lib):
         got = ops.adapter_linear(**{**c, "x": x, "a": a, "b": b}, **kw)
         keep = torch.arange(51) != 20
         assert torch.equal(got[keep], want[keep]) and torch.all(torch.isnan(got[20]))
+
+
+@pytest.mark.parametrize("n, k, d", [(1500, 128, 1024), (1500, 128, 516), (8100, 256, 2048), (8100, 256, 2020)])
+def test_an_odd_adapter_among_many_rows(gpu_lib, n, k, d):
+    # Blocks of rows that meet another request's infinities and NaN are formed again.
+    counts, ids = [n // 2 - 20, 21, 1, 0, n // 2 - 2], [0, 1, -1, 1, 0]
+    c, kw = make(counts, ids, k, d, 16, 2, BF, bias=True)
+    bad = c["b"].clone()
+    bad[1, 5:9], bad[1, 100, 3] = float("nan"), float("inf")
+    got = ops.adapter_linear(**{**c, "b": bad}, **kw, activation="relu")
+    mine = torch.zeros(n, dtype=torch.bool)
+    mine[n // 2 - 20:n // 2 + 1] = True
+    odd = torch.zeros(n, d, dtype=torch.bool)
+    odd[mine, 5:9] = True
+    odd[mine, 100] = True
+    shown = got.cpu()
+    assert torch.all(torch.isfinite(shown[~odd]))
+    assert torch.all(~torch.isfinite(shown[mine][:, 100]) | (shown[mine][:, 100] == 0))   # inf, or its ReLU
+    zero = c["b"].clone()
+    zero[1, 5:9], zero[1, 100] = 0, 0
+    fixed = got.clone()
+    fixed[odd.cuda()] = ops.adapter_linear(**{**c, "b": zero}, **kw, activation="relu")[odd.cuda()]
+    check({**c, "b": zero}, kw, counts, ids, fixed, relu=True)
 
 
 def test_calls_that_share_a_workspace(gpu_lib):
