@@ -197,31 +197,30 @@ hipError_t launch_shrink(const AdapterArgs& a, const LowRank& lr, hipStream_t s)
 }
 
 // ---------------------------------------------------------------------------
-// Fast path, few rows: 32 features x 32 rows a workgroup, whose four waves split K
-// and then the rows' adapters; operands straight from global memory, partial sums
-// added up through LDS in a fixed order. A row keeps the products of its own adapter
-// by a select.
+// Fast path, few rows: 32 features x 32 rows a workgroup, whose eight waves split K;
+// then a wave adds the adapters of four of the rows, one after the other with t zero for
+// all rows but its own of them, and a row keeps what is its own by a select. Operands come
+// straight from global memory, partial sums are added up through LDS in a fixed order.
+// Bound by latency: the first loads depend on nothing (rows up to num_rows are read; those
+// behind the last request are dropped), and B's are issued before the first products.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void adapter_few(const AdapterArgs a, const LowRank lr, int tiles_m) {
+__global__ __launch_bounds__(512) void adapter_few(const AdapterArgs a, const LowRank lr, int tiles_m) {
   constexpr int U = 8;                         // steps of a wave in flight
-  __shared__ f32x4 red[4][4][kWave];
-  __shared__ int list[4][32];
+  __shared__ f32x4 red[8][4][kWave];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hh = lane >> 5;
   const int d0 = (int)(blockIdx.x % (uint32_t)tiles_m) * 32;
   const int64_t n0 = (int64_t)(blockIdx.x / (uint32_t)tiles_m) * 32;
-  const int64_t n_rows = rows_of(a);
-  if (n0 >= n_rows) return;
-  const int64_t n = min(n0 + l32, n_rows - 1);
+  const int64_t n = min(n0 + l32, a.N - 1);
   const int d = min(d0 + l32, a.D - 1);
-  const int mine = n0 + l32 < n_rows ? lr.aid[n] : -1;
+  int mine = lr.aid[n];
+  const int64_t n_rows = rows_of(a);
   const bf16_t* x = static_cast<const bf16_t*>(a.x) + n * a.x_stride + 8 * hh;
   const bf16_t* w = static_cast<const bf16_t*>(a.w) + (int64_t)d * a.K + 8 * hh;
-  f32x16 acc = {};
-  auto k_of = [&](int s) { return 256 * (s / 4) + 64 * wave + 16 * (s % 4); };
-  for (int s = 0; k_of(s) < a.K; s += U) {
-    u32x4 wv[U], xv[U];
+  auto k_of = [&](int s) { return 512 * (s / 4) + 64 * wave + 16 * (s % 4); };
+  u32x4 wv[U], xv[U];
+  auto load_k = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = k_of(s + u);
@@ -229,48 +228,63 @@ __global__ __launch_bounds__(256) void adapter_few(const AdapterArgs a, const Lo
       wv[u] = load16(w + k, ok);
       xv[u] = load16(x + k, ok);
     }
+  };
+  load_k(0);
+  if (n0 >= n_rows) return;
+  if (n0 + l32 >= n_rows) mine = -1;
+  // Pair p of this wave: step p / 4 of the adapter of its row p % 4.
+  constexpr int V = 4;                         // pairs in flight
+  const int pairs = lr.cols / 16 * 4;
+  int ids[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ids[i] = __builtin_amdgcn_readlane(mine, 4 * wave + i);
+  const bool in_wave = (l32 >> 2) == wave;
+  const bf16_t* t = lr.t + n * lr.cols + 8 * hh;
+  const bf16_t* b = lr.b + (int64_t)d * lr.rank + 8 * hh;
+  u32x4 bv[V], tv[V];
+  auto load_b = [&](int p0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int at = p0 / 4 * 16;
+      const bool ok = ids[i] >= 0 && at + 8 * hh < lr.rank;
+      bv[i] = load16(b + (int64_t)ids[i] * a.D * lr.rank + at, ok);
+      tv[i] = load16(t + at, ok && in_wave && mine == ids[i]);
+    }
+  };
+  static_assert(V == 4, "a pair of each row");
+  load_b(0);
+  f32x16 acc = {};
+  for (int s = 0; k_of(s) < a.K; s += U) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (k_of(s + u) >= a.K) break;
       acc = mfma32(as_bf16x8(wv[u]), as_bf16x8(xv[u]), acc);
     }
+    if (k_of(s + U) < a.K) load_k(s + U);
   }
-  int count = 0;
-  for (uint64_t todo = __ballot(mine >= 0); todo != 0; ++count) {
-    const int id = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
-    todo &= ~__ballot(mine == id);
-    if (lane == 0) list[wave][count] = id;
-  }
-  wait_lgkmcnt0();                             // the list is in LDS (one wave's own)
-  asm volatile("" ::: "memory");
-  const int steps = lr.cols / 16, pairs = count * steps;
-  const bf16_t* t = lr.t + n * lr.cols + 8 * hh;
-  for (int p0 = wave; p0 < pairs; p0 += 4 * U) {
-    u32x4 wv[U], tv[U];
-    int id[U];
+  for (int p0 = 0; p0 < pairs; p0 += V) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int p = min(p0 + 4 * u, pairs - 1), at = 16 * (p % steps);
-      id[u] = __builtin_amdgcn_readfirstlane(list[wave][p / steps]);
-      const bool ok = at + 8 * hh < lr.rank;
-      wv[u] = load16(lr.b + ((int64_t)id[u] * a.D + d) * lr.rank + at + 8 * hh, ok);
-      tv[u] = load16(t + at, ok && mine == id[u]);
-    }
+    for (int i = 0; i < 4; ++i) {
+      bool again = ids[i] < 0;                 // none, or a row before it has the same
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (p0 + 4 * u >= pairs) break;
-      const f32x16 y = mfma32(as_bf16x8(wv[u]), as_bf16x8(tv[u]), acc);
-      const bool own = mine == id[u];
+      for (int e = 0; e < i; ++e) again = again || ids[e] == ids[i];
+      if (again) continue;
+      const f32x16 y = mfma32(as_bf16x8(bv[i]), as_bf16x8(tv[i]), acc);
+      const bool own = in_wave && mine == ids[i];
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[e] = own ? y[e] : acc[e];
     }
+    if (p0 + V < pairs) load_b(p0 + V);
   }
 #pragma unroll
   for (int q = 0; q < 4; ++q)
     red[wave][q][lane] = f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
   __syncthreads();
+  if (wave >= 4) return;
   // Quad `wave`: features 8 wave + 4 hh .. + 3 of row l32.
-  f32x4 s = ((red[0][wave][lane] + red[1][wave][lane]) + red[2][wave][lane]) + red[3][wave][lane];
+  f32x4 s = red[0][wave][lane];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) s += red[i][wave][lane];
   const int df = d0 + 8 * wave + 4 * hh;
   if (n0 + l32 >= n_rows || df >= a.D) return;
   if (a.bias != nullptr)
@@ -284,8 +298,8 @@ __global__ __launch_bounds__(256) void adapter_few(const AdapterArgs a, const Lo
 hipError_t launch_few(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
   const int tiles_m = (a.D + 31) / 32;
   const int64_t blocks = (a.N + 31) / 32 * tiles_m;
-  if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-  return launch_kernel(adapter_few, dim3((uint32_t)blocks), dim3(256), s, a, lr, tiles_m);
+  if (!grid_fits(blocks, 512)) return hipErrorInvalidConfiguration;
+  return launch_kernel(adapter_few, dim3((uint32_t)blocks), dim3(512), s, a, lr, tiles_m);
 }
 
 template <typename T>
