@@ -803,6 +803,74 @@ PyObject* adapter(PyObject* const* a) {
   return result(a[9], out);
 }
 
+// A rotation's arguments.
+struct Turn {
+  int64_t rot = 0, r = 0, slots = 0;
+};
+Turn turn_of(const Ten& freqs, const Ten& pos, const Ten& off, const Ten& slots, const Ten& lens,
+             int64_t m, int64_t d) {
+  Turn x;
+  int_vector(pos, m);
+  if (freqs) {
+    need(freqs->scalar_type() == c10::kFloat && freqs->dim() == 1 && freqs->is_contiguous() &&
+         2 * freqs->numel() <= d);
+    x.rot = 2 * freqs->numel();
+  }
+  if (off) {
+    x.r = off->numel() - 1;
+    need(x.r >= 0);
+    offsets(off, x.r);
+    int_vector(slots, x.r);
+    if (lens) {
+      x.slots = lens->numel();
+      int_vector(lens, x.slots);
+      need(slots || x.r <= x.slots);
+    }
+  } else {
+    need(!slots && !lens);
+  }
+  need(x.rot == 0 || pos || (off && lens));
+  return x;
+}
+
+// x, freqs, positions, offsets, slots, lens, interleaved, out, stream
+PyObject* rotate(PyObject* const* a) {
+  Call c(a[8]);
+  const Ten x = c.must(a[0]), freqs = c.get(a[1]), pos = c.get(a[2]), off = c.get(a[3]),
+            slots = c.get(a[4]), lens = c.get(a[5]);
+  on_current_device(c);
+  need(x->dim() == 3 && x->size(1) >= 1 && x->size(2) >= 1 && x->size(1) <= INT32_MAX &&
+       x->size(2) <= INT32_MAX);
+  const int64_t m = x->size(0), h = x->size(1), d = x->size(2);
+  const int32_t code = dtype_code(x), inter = truth(a[6]);
+  const Turn t = turn_of(freqs, pos, off, slots, lens, m, d);
+  const int64_t stride = row_stride(x);
+  const Ten out = c.or_new(a[7], x->sizes(), x->scalar_type());
+  void* s = stream_of(c.stream);
+  run("rocs_rotate", rocs_rotate, x.ptr(), stride, freqs.f32(), (int32_t)t.rot, inter, pos.i32(),
+      off.i32(), slots.i32(), lens.i32(), t.r, t.slots, m, (int32_t)h, (int32_t)d, code, data(out), s);
+  return result(a[7], out);
+}
+
+// rows, pool, kv_heads, head_dim, bf16, out, stream
+PyObject* read_fp4(PyObject* const* a) {
+  Call c(a[6]);
+  const Ten rows = c.must(a[0]), pool = c.must(a[1]);
+  on_current_device(c);
+  const int64_t hk = integer(a[2]), d = integer(a[3]), m = rows->numel();
+  need(hk >= 1 && hk <= INT32_MAX && d >= 1 && d <= INT32_MAX);
+  const int64_t row = (int64_t)rocs_fp4_row_bytes((int32_t)hk, (int32_t)d);
+  need(row > 0 && pool->scalar_type() == c10::kByte && pool->dim() == 3 && pool->is_contiguous() &&
+       pool->size(2) == row && pool->size(0) >= 1 && pool->size(1) >= 1);
+  int_vector(rows, m);
+  const bool bf16 = truth(a[4]) != 0;
+  const Ten out = c.or_new(a[5], {m, 2, hk, d}, bf16 ? c10::kBFloat16 : c10::kFloat);
+  void* s = stream_of(c.stream);
+  run("rocs_cache_read_fp4", rocs_cache_read_fp4, rows.i32(), m, pool.ptr(), pool->size(0) * pool->size(1),
+      (int32_t)hk, (int32_t)d, bf16 ? ROCS_DTYPE_BF16 : ROCS_DTYPE_F32, data(out), s);
+  return result(a[5], out);
+}
+
 // k, v, rows, pool, freqs, q, positions, offsets, slots, lens, interleaved,
 // q_out, stream
 PyObject* append(PyObject* const* a) {
@@ -818,27 +886,7 @@ PyObject* append(PyObject* const* a) {
   const int64_t stride = row_stride(k);
   need(row_stride(v) == stride);
   int_vector(rows, m);
-  int_vector(pos, m);
-  int64_t rot = 0, r = 0, n_slots = 0;
-  if (freqs) {
-    need(freqs->scalar_type() == c10::kFloat && freqs->dim() == 1 && freqs->is_contiguous() &&
-         2 * freqs->numel() <= d);
-    rot = 2 * freqs->numel();
-  }
-  if (off) {
-    r = off->numel() - 1;
-    need(r >= 0);
-    offsets(off, r);
-    int_vector(slots, r);
-    if (lens) {
-      n_slots = lens->numel();
-      int_vector(lens, n_slots);
-      need(slots || r <= n_slots);
-    }
-  } else {
-    need(!slots && !lens);
-  }
-  need(rot == 0 || pos || (off && lens));
+  const Turn t = turn_of(freqs, pos, off, slots, lens, m, d);
   int32_t form = ROCS_POOL_ROWS;
   need(pool->is_contiguous() && pool->dim() >= 3 && pool->size(0) >= 1 && pool->size(1) >= 1);
   const int64_t pool_rows = pool->size(0) * pool->size(1);
@@ -862,8 +910,8 @@ PyObject* append(PyObject* const* a) {
   }
   void* s = stream_of(c.stream);
   run("rocs_cache_append", rocs_cache_append, q.ptr(), q_stride, k.ptr(), v.ptr(), stride,
-      rows.i32(), freqs.f32(), (int32_t)rot, inter, pos.i32(), off.i32(), slots.i32(), lens.i32(), r,
-      n_slots, m, (int32_t)h, (int32_t)hk, (int32_t)d, code, pool.ptr(), pool_rows, form,
+      rows.i32(), freqs.f32(), (int32_t)t.rot, inter, pos.i32(), off.i32(), slots.i32(), lens.i32(), t.r,
+      t.slots, m, (int32_t)h, (int32_t)hk, (int32_t)d, code, pool.ptr(), pool_rows, form,
       data(q_out), s);
   if (!q) Py_RETURN_TRUE;
   return result(a[11], q_out);
@@ -921,6 +969,7 @@ PyMethodDef g_methods[] = {
     ROCS_ENTRY(cache_reserve, 11), ROCS_ENTRY(cache_write, 4), ROCS_ENTRY(cache_fork, 9),
     ROCS_ENTRY(cache_free, 6), ROCS_ENTRY(cache_compact, 7),
     ROCS_ENTRY(adapter, 12),  ROCS_ENTRY(append, 13),     ROCS_ENTRY(paged_fp4, 16),
+    ROCS_ENTRY(rotate, 9),    ROCS_ENTRY(read_fp4, 7),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};

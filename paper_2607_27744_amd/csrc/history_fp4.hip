@@ -2,11 +2,14 @@
 // rows (token, head of the group) of one request a wave.
 //
 // A call over single events is a read of the cache, of which 4 bits leave a
-// quarter of the bytes: what a byte costs in instructions decides. K goes from
-// memory to the matrix cores through registers alone: lane (l16, g) holds key l16's
-// dims from D / 4 g on (16 bytes at head_dim 128: one block of a scale), which
-// the conversion instruction turns into the A operands of D / 32 products; the
-// order of a product's inner dims is free as long as q's fragments follow it.
+// quarter of the bytes: what a byte costs in instructions decides. K goes to the
+// matrix cores as it is stored: lane (l16, g) holds key l16's dims from D / 4 g on
+// (16 bytes at head_dim 128: one block of a scale), which the conversion instruction
+// turns into the A operands of D / 32 products; the order of a product's inner dims is
+// free as long as q's fragments follow it. Loads have neighbouring lanes on
+// neighbouring bytes (loaded in the operands' order, each lane's 16 bytes are a cache
+// access of their own: 33 million of them in 128 histories of 3,125 rows, 8 heads, which
+// kept the address units busy for half of 151 us), so K's change lanes through LDS.
 // V's products run over keys, and a lane has them for one dim: V is converted a
 // block a lane (its scale with it) and turned around through LDS, 32 keys at a time, by
 // the transposing read. (Turned as codes, a quarter of the LDS bytes, a scale would
@@ -36,7 +39,6 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   constexpr int kRows = 16 * NR;
   constexpr int KS = D / 32, DB = D / 16;   // products of a score, output blocks
   constexpr int BPR = D / kFp4Block;        // blocks of a key: V's loads of a lane and stage
-  constexpr int KW32 = D / 32;              // 32-bit words of a lane's part of a K row
   constexpr int ROWB = 2 * D;               // a staged V row
   constexpr int STAGE = 32 * ROWB > kRows * D * 4 ? 32 * ROWB : kRows * D * 4;
   __shared__ __attribute__((aligned(1024))) char lds[kWaves * STAGE];
@@ -79,44 +81,47 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   const bool alone = tile_alone(a, most), direct = a.splits == 1 || alone;
   if (alone && split > 0) return;
 
-  // This lane's places in a row: its part of K and that part's scale; the block of
-  // V (the n-th of a stage: key 64 / BPR n + lane / BPR) and its scale. Below the
-  // kernel's own width the head's last ones stand in (q is 0 there, or the result is not stored).
+  // This lane's block of a row. Below the kernel's own width the head's last ones stand
+  // in (q is 0 there, or the result is not stored).
   const Fp4Row fr{a.Hk, a.D};
   const char* const base = static_cast<const char*>(a.k);
-  const int k_at = fr.values(0, hk) + min(D / 8 * g, a.D / 2 - D / 8);
-  const int ks_at = fr.scales(0, hk) + min(D / 4 * g / kFp4Block, a.D / kFp4Block - 1);
   const int vb = min(lane % BPR, a.D / kFp4Block - 1);
-  const int v_at = fr.values(1, hk) + 16 * vb, vs_at = fr.scales(1, hk) + vb;
+  const int k_at = fr.values(0, hk) + 16 * vb, v_at = fr.values(1, hk) + 16 * vb;
   const uint32_t row_bytes = (uint32_t)a.kv_stride;
+  const uint32_t st0 = (uint32_t)(wave * STAGE);
 
-  uint32_t kw[4][KW32], kse[4];
-  u32x4 vw[BPR];
-  uint32_t vse[BPR];
-  auto load_k = [&](int rows) __attribute__((always_inline)) {
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-      const char* p = base + (uint64_t)(uint32_t)__shfl(rows, 16 * kb + l16) * row_bytes;
-      if constexpr (KW32 == 4) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(p + k_at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) kw[kb][i] = x[i];
-      } else {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(p + k_at);
-        kw[kb][0] = x[0];
-        kw[kb][1] = x[1];
-      }
-      kse[kb] = (uint8_t)p[ks_at];
+  // A stage: 64 keys, loaded a block a lane (the n-th: key 64 / BPR n + lane / BPR); the
+  // scales of lane's key, a byte a block.
+  u32x4 kw[BPR], vw[BPR];
+  uint32_t kse, vse;
+  auto key_scales = [&](const char* p) __attribute__((always_inline)) -> uint32_t {
+    if constexpr (D == 128) {
+      if (a.D == 128) return *reinterpret_cast<const uint32_t*>(p);
+      const uint32_t e2 = (uint8_t)p[2];                        // 96
+      return (uint8_t)p[0] | (uint32_t)(uint8_t)p[1] << 8 | e2 << 16 | e2 << 24;
+    } else {
+      if (a.D == 64) return *reinterpret_cast<const uint16_t*>(p);
+      return (uint8_t)p[0] * 0x101u;                            // 32
     }
+  };
+  auto load_k = [&](int rows) __attribute__((always_inline)) {
+    kse = key_scales(base + (uint64_t)(uint32_t)rows * row_bytes + fr.scales(0, hk));
+#pragma unroll
+    for (int n = 0; n < BPR; ++n)
+      kw[n] = *reinterpret_cast<const u32x4*>(
+          base + (uint64_t)(uint32_t)__shfl(rows, 64 / BPR * n + lane / BPR) * row_bytes + k_at);
   };
   auto load_v = [&](int rows) __attribute__((always_inline)) {
+    vse = key_scales(base + (uint64_t)(uint32_t)rows * row_bytes + fr.scales(1, hk));
 #pragma unroll
-    for (int n = 0; n < BPR; ++n) {
-      const char* p = base + (uint64_t)(uint32_t)__shfl(rows, 64 / BPR * n + lane / BPR) * row_bytes;
-      vw[n] = *reinterpret_cast<const u32x4*>(p + v_at);
-      vse[n] = (uint8_t)p[vs_at];
-    }
+    for (int n = 0; n < BPR; ++n)
+      vw[n] = *reinterpret_cast<const u32x4*>(
+          base + (uint64_t)(uint32_t)__shfl(rows, 64 / BPR * n + lane / BPR) * row_bytes + v_at);
   };
+  // Staged K codes: rows of D / 2 bytes, chunk c of `key` at c ^ k_swz: the 16 rows that a
+  // quarter wave reads (or writes four chunks of) fall on distinct banks.
+  auto k_swz = [](int key) { return BPR == 4 ? (key >> 2) & 3 : (key >> 3) & 1; };
+  constexpr int KWW = D / 32;               // words of a lane's quarter of a key
   auto rows_of = [&](int at) __attribute__((always_inline)) { return pool_row(a, t.pages, min(at + lane, hi - 1)); };
 
   float m[NR], l_part[NR];
@@ -128,7 +133,6 @@ history_fp4_few(const HistArgs a, int64_t slots) {
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[r][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const uint32_t st0 = (uint32_t)(wave * STAGE);
   // Transposing reads of V^T: rows 16 x + 4 g + jl / 4 of the staged 32, 16 dims.
   uint32_t va[2];
 #pragma unroll
@@ -149,13 +153,34 @@ history_fp4_few(const HistArgs a, int64_t slots) {
     const bool more = at + 64 * KW < hi;
     f32x4 s[NR][4];
 #pragma unroll
+    for (int n = 0; n < BPR; ++n) {
+      const int key = 64 / BPR * n + lane / BPR;
+      *reinterpret_cast<ROCS_LDS u32x4*>(lds3 + st0 + key * (D / 2) + 16 * ((lane % BPR) ^ k_swz(key))) = kw[n];
+    }
+    uint32_t kc[4][KWW];
+#pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
-      const float scale = fp4_scale(kse[kb]);
+      const int key = 16 * kb + l16;
+      if constexpr (D == 128) {
+        const u32x4 x = *reinterpret_cast<const ROCS_LDS u32x4*>(lds3 + st0 + key * 64 + 16 * (g ^ k_swz(key)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kc[kb][i] = x[i];
+      } else {
+        const u32x2 x = *reinterpret_cast<const ROCS_LDS u32x2*>(
+            lds3 + st0 + key * 32 + 16 * ((g >> 1) ^ k_swz(key)) + 8 * (g & 1));
+        kc[kb][0] = x[0];
+        kc[kb][1] = x[1];
+      }
+    }
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      const uint32_t e = (uint32_t)__shfl((int)kse, 16 * kb + l16) >> (8 * (D / 4 * g / kFp4Block));
+      const float scale = fp4_scale(e & 255u);
 #pragma unroll
       for (int r = 0; r < NR; ++r) s[r][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 kf = as_bf16x8(fp4_to_bf16x8(kw[kb][ks], scale));
+        const bf16x8 kf = as_bf16x8(fp4_to_bf16x8(kc[kb][ks], scale));
 #pragma unroll
         for (int r = 0; r < NR; ++r) s[r][kb] = mfma16(kf, qf[r][ks], s[r][kb]);
       }
@@ -170,7 +195,7 @@ history_fp4_few(const HistArgs a, int64_t slots) {
 #pragma unroll
       for (int n = BPR / 2 * half; n < BPR / 2 * (half + 1); ++n) {
         const int key = 64 / BPR * n + lane / BPR - 32 * half;
-        const float scale = fp4_scale(vse[n]);
+        const float scale = fp4_scale((uint32_t)__shfl((int)vse, 64 / BPR * n + lane / BPR) >> (8 * (lane % BPR)) & 255u);
         const uint32_t to = st0 + (uint32_t)(key * ROWB);
         const int c0 = 4 * (lane % BPR), sw = v_swizzle<D>(key);
 #pragma unroll

@@ -54,7 +54,7 @@ class _PythonPath:
 
     linear = glm_linear = mlp2 = fm_linear = lcb = plan = attention = _none
     history = paged = cache_reserve = cache_write = cache_fork = cache_free = cache_compact = _none
-    adapter = append = paged_fp4 = _none
+    adapter = append = paged_fp4 = rotate = read_fp4 = _none
 
 
 def _native():
@@ -1215,6 +1215,10 @@ def rotate(x, freqs, *, positions=None, offsets=None, slots=None, lens=None, int
     position * freqs[i] (float32, radians). Positions are `positions` (int32 [M]), or those of the
     last rows of each request's history: offsets int32 [R + 1], slots int32 [R] (None: request r is
     slot r), lens int32 [slots], as paged_attention takes them."""
+    done = (_binding or _native()).rotate(x, freqs, positions, offsets, slots, lens, interleaved, out,
+                                          stream)
+    if done is not None:
+        return done
     _need(x.dim() == 3 and x.shape[1] >= 1 and x.shape[2] >= 1, "x must be [M, heads, d]")
     m, h, d = x.shape
     code = _dtype_code(x)
@@ -1311,6 +1315,10 @@ def cache_read_fp4(rows, pool, kv_heads, head_dim, *, dtype=torch.bfloat16, out=
     """rocs_cache_read_fp4: rows rows[m] (int32 [M]) of one layer's 4-bit pool as values [M, 2,
     kv_heads, head_dim] (K, then V) in bfloat16 (exactly) or float32; a row outside the pool is
     zero."""
+    done = (_binding or _native()).read_fp4(rows, pool, kv_heads, head_dim, dtype == torch.bfloat16, out,
+                                            stream) if dtype in (torch.bfloat16, torch.float32) else None
+    if done is not None:
+        return done
     _need(dtype in (torch.bfloat16, torch.float32), "dtype must be bfloat16 or float32")
     pool_rows = _pool_rows_fp4(pool, kv_heads, head_dim)
     m = rows.numel()
