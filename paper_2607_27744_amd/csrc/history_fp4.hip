@@ -48,12 +48,17 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const uint32_t b8 = blockIdx.x & ~7u;     // as in history_split
-  const uint32_t work = b8 + 8 > gridDim.x ? blockIdx.x : b8 + ((blockIdx.x + (blockIdx.x >> 3)) & 7u);
+  // Head groups of the same keys share cache lines: they follow each other on one XCD.
+  // Parts of a history go to XCDs in turn, rotated as in history_split.
   const int HW = a.heads, KW = kWaves / HW;
-  const uint32_t groups_n = (uint32_t)(a.Hk / HW);
-  const int hk0 = (int)(work % groups_n) * HW, hk = hk0 + wave % HW;
-  const uint32_t rest = work / groups_n;
+  const uint32_t groups_n = (uint32_t)(a.Hk / HW), eight = kNumXcd * groups_n;
+  uint32_t group = blockIdx.x % groups_n, rest = blockIdx.x / groups_n;
+  if (blockIdx.x < gridDim.x / eight * eight) {
+    const uint32_t i = blockIdx.x / kNumXcd, turn = i / groups_n;
+    group = i % groups_n;
+    rest = turn * kNumXcd + ((blockIdx.x + turn) % kNumXcd);
+  }
+  const int hk0 = (int)group * HW, hk = hk0 + wave % HW;
   const int split = (int)(rest % (uint32_t)a.splits);
   const HistTile t = hist_tile(a, slots - 1 - rest / (uint32_t)a.splits, kRows);
   if (t.rows <= 0) return;
@@ -94,15 +99,15 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   // scales of lane's key, a byte a block.
   u32x4 kw[BPR], vw[BPR];
   uint32_t kse, vse;
+  // (Below the kernel's width one byte ahead of the scales and their last byte instead of one
+  // behind, which could lie past the pool.)
+  const int ahead = a.D == D ? 0 : 1;
+  const int k_byte = min(D / 4 * g / kFp4Block, a.D / kFp4Block - 1) + ahead, v_byte = vb + ahead;
   auto key_scales = [&](const char* p) __attribute__((always_inline)) -> uint32_t {
-    if constexpr (D == 128) {
-      if (a.D == 128) return *reinterpret_cast<const uint32_t*>(p);
-      const uint32_t e2 = (uint8_t)p[2];                        // 96
-      return (uint8_t)p[0] | (uint32_t)(uint8_t)p[1] << 8 | e2 << 16 | e2 << 24;
-    } else {
-      if (a.D == 64) return *reinterpret_cast<const uint16_t*>(p);
-      return (uint8_t)p[0] * 0x101u;                            // 32
-    }
+    typedef uint32_t u32u __attribute__((aligned(1)));
+    typedef uint16_t u16u __attribute__((aligned(1)));
+    if constexpr (D == 128) return *reinterpret_cast<const u32u*>(p - ahead);
+    else return *reinterpret_cast<const u16u*>(p - ahead);
   };
   auto load_k = [&](int rows) __attribute__((always_inline)) {
     kse = key_scales(base + (uint64_t)(uint32_t)rows * row_bytes + fr.scales(0, hk));
@@ -122,7 +127,12 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   // quarter wave reads (or writes four chunks of) fall on distinct banks.
   auto k_swz = [](int key) { return BPR == 4 ? (key >> 2) & 3 : (key >> 3) & 1; };
   constexpr int KWW = D / 32;               // words of a lane's quarter of a key
-  auto rows_of = [&](int at) __attribute__((always_inline)) { return pool_row(a, t.pages, min(at + lane, hi - 1)); };
+  // The row of a stage's key `lane` in two steps: the page table's entry, a stage ahead,
+  // and the row from it where it is needed (formed at once it would wait for every load
+  // before it). Past the end the last key stands in, and the last stage loads one of
+  // that alone: in a branch the loads could not be counted, and each wait would be for all.
+  PoolKey next_key;
+  auto look_up = [&](int at) __attribute__((always_inline)) { next_key = pool_key(a, t.pages, min(at + lane, hi - 1)); };
 
   float m[NR], l_part[NR];
   f32x4 o[NR][DB];
@@ -142,15 +152,15 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   }
 
   int at = lo + 64 * (wave / HW);
-  int rows_now = 0, rows_next = 0;
+  int rows_now = 0;
   if (at < hi) {
-    rows_now = rows_of(at);
+    look_up(at);
+    rows_now = pool_row(a, next_key);
+    look_up(at + 64 * KW);
     load_k(rows_now);
     load_v(rows_now);
-    rows_next = rows_of(at + 64 * KW);
   }
   for (; at < hi; at += 64 * KW) {
-    const bool more = at + 64 * KW < hi;
     f32x4 s[NR][4];
 #pragma unroll
     for (int n = 0; n < BPR; ++n) {
@@ -174,7 +184,7 @@ history_fp4_few(const HistArgs a, int64_t slots) {
     }
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
-      const uint32_t e = (uint32_t)__shfl((int)kse, 16 * kb + l16) >> (8 * (D / 4 * g / kFp4Block));
+      const uint32_t e = (uint32_t)__shfl((int)kse, 16 * kb + l16) >> (8 * k_byte);
       const float scale = fp4_scale(e & 255u);
 #pragma unroll
       for (int r = 0; r < NR; ++r) s[r][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -185,17 +195,15 @@ history_fp4_few(const HistArgs a, int64_t slots) {
         for (int r = 0; r < NR; ++r) s[r][kb] = mfma16(kf, qf[r][ks], s[r][kb]);
       }
     }
-    rows_now = rows_next;
-    if (more) {
-      load_k(rows_now);
-      rows_next = rows_of(at + 128 * KW);
-    }
+    rows_now = pool_row(a, next_key);
+    look_up(at + 128 * KW);
+    load_k(rows_now);
     // V's first 32 keys, a block a lane.
     auto stage_v = [&](int half) __attribute__((always_inline)) {
 #pragma unroll
       for (int n = BPR / 2 * half; n < BPR / 2 * (half + 1); ++n) {
         const int key = 64 / BPR * n + lane / BPR - 32 * half;
-        const float scale = fp4_scale((uint32_t)__shfl((int)vse, 64 / BPR * n + lane / BPR) >> (8 * (lane % BPR)) & 255u);
+        const float scale = fp4_scale((uint32_t)__shfl((int)vse, 64 / BPR * n + lane / BPR) >> (8 * v_byte) & 255u);
         const uint32_t to = st0 + (uint32_t)(key * ROWB);
         const int c0 = 4 * (lane % BPR), sw = v_swizzle<D>(key);
 #pragma unroll
@@ -288,7 +296,7 @@ history_fp4_few(const HistArgs a, int64_t slots) {
                                                 pk[r][2 * half + 1][0], pk[r][2 * half + 1][1]}), o[r][db]);
       }
     }
-    if (more) load_v(rows_now);
+    load_v(rows_now);
   }
 
   // This wave's partial softmax into its staging area, 16-byte pieces of a row

@@ -56,10 +56,16 @@ inline void set_page_divisor(HistArgs& a) {
   a.page_magic = a.page_size > 1 ? (uint32_t)((uint64_t(1) << (31 + l)) / (uint64_t)a.page_size + 1) : 0;
   a.page_shift = l > 0 ? l - 1 : 0;
 }
-__device__ __forceinline__ int pool_row(const HistArgs& a, const int32_t* pages, int j) {
+struct PoolKey {
+  int entry, in_page;        // the page table's entry as it stands; row in the page
+};
+__device__ __forceinline__ PoolKey pool_key(const HistArgs& a, const int32_t* pages, int j) {
   const int c = a.page_size == 1 ? j : (int)(__umulhi((uint32_t)j, a.page_magic) >> a.page_shift);
-  const uint32_t p = min((uint32_t)pages[c], (uint32_t)(a.pages - 1));
-  return (int)(p * (uint32_t)a.page_size) + (j - c * a.page_size);
+  return {pages[c], j - c * a.page_size};
+}
+__device__ __forceinline__ int pool_row(const HistArgs& a, const PoolKey& k) {
+  const uint32_t p = min((uint32_t)k.entry, (uint32_t)(a.pages - 1));
+  return (int)(p * (uint32_t)a.page_size) + k.in_page;
 }
 
 // ---------------------------------------------------------------------------

@@ -150,7 +150,7 @@ history_tile(const HistArgs a, int64_t slots) {
   // the last key stands in.
   auto group_of = [&](int base) __attribute__((always_inline)) -> int64_t {
     if constexpr (FP4)                       // the thread's own row
-      return (int64_t)pool_row(a, t.pages, min(base + fkey, hi - 1)) * (uint32_t)a.kv_stride;
+      return (int64_t)pool_row(a, pool_key(a, t.pages, min(base + fkey, hi - 1))) * (uint32_t)a.kv_stride;
     return feed.group(min(base + 16 * wave, (hi - 1) & ~15));
   };
   auto issue = [&](const char* src, int base, int64_t off, uint32_t dst) __attribute__((always_inline)) {
