@@ -98,7 +98,7 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   // A stage: 64 keys, loaded a block a lane (the n-th: key 64 / BPR n + lane / BPR); the
   // scales of lane's key, a byte a block.
   u32x4 kw[BPR], vw[BPR];
-  uint32_t kse, vse;
+  uint32_t kse, vse, vsn;
   // (Below the kernel's width one byte ahead of the scales and their last byte instead of one
   // behind, which could lie past the pool.)
   const int ahead = a.D == D ? 0 : 1;
@@ -110,14 +110,17 @@ history_fp4_few(const HistArgs a, int64_t slots) {
     else return *reinterpret_cast<const u16u*>(p - ahead);
   };
   auto load_k = [&](int rows) __attribute__((always_inline)) {
-    kse = key_scales(base + (uint64_t)(uint32_t)rows * row_bytes + fr.scales(0, hk));
+    // V's with K's: they lie in the same cache lines.
+    const char* p = base + (uint64_t)(uint32_t)rows * row_bytes;
+    kse = key_scales(p + fr.scales(0, hk));
+    vsn = key_scales(p + fr.scales(1, hk));
 #pragma unroll
     for (int n = 0; n < BPR; ++n)
       kw[n] = *reinterpret_cast<const u32x4*>(
           base + (uint64_t)(uint32_t)__shfl(rows, 64 / BPR * n + lane / BPR) * row_bytes + k_at);
   };
   auto load_v = [&](int rows) __attribute__((always_inline)) {
-    vse = key_scales(base + (uint64_t)(uint32_t)rows * row_bytes + fr.scales(1, hk));
+    vse = vsn;
 #pragma unroll
     for (int n = 0; n < BPR; ++n)
       vw[n] = *reinterpret_cast<const u32x4*>(
