@@ -173,14 +173,18 @@ __global__ __launch_bounds__(256) void append_rows(const AppendArgs a, int rb) {
   const int pieces = (D + 7) / 8;
   const int heads = (a.q != nullptr ? H : 0) + (a.k != nullptr ? 2 * Hk : 0);
   const int qh = a.q != nullptr ? H : 0;
-  const int total = rb * heads * pieces;
   const Fp4Row fr{Hk, D};
-  for (int idx = tid; idx < total; idx += 256) {
-    const int piece = idx % pieces, rest = idx / pieces;
-    const int head = rest % heads, i = rest / heads;
+  // A thread keeps its piece and steps over the (row, head) pairs, so that nothing is
+  // divided in the loop; threads past the last whole head of 256 have none.
+  const int step = 256 / pieces, piece = tid % pieces;
+  const int d0 = 8 * piece, n = min(D - d0, 8);
+  int head = tid / pieces, i = 0;
+  if (head >= step) return;
+  for (;; head += step) {
+    for (; head >= heads; head -= heads) ++i;
+    if (i >= rb) break;
     const int64_t m = m0 + i;
     if (!known[i]) continue;
-    const int d0 = 8 * piece, n = min(D - d0, 8);
     float x[8];
     if (head < qh) {
       turned<T, VEC>(static_cast<const T*>(a.q) + m * a.q_stride + (int64_t)head * D, d0, D, a.half,
@@ -197,9 +201,8 @@ __global__ __launch_bounds__(256) void append_rows(const AppendArgs a, int rb) {
     else
       load8<T, VEC>(static_cast<const T*>(a.v) + m * a.kv_stride + (int64_t)h * D + d0, n, x);
     if constexpr (FP4) {
-      // Four lanes hold a block (pieces are a multiple of four, and so is the
-      // first index of every turn of the loop). A NaN is not the largest of anything:
-      // it is looked for by itself.
+      // Four lanes hold a block (pieces are a multiple of four). A NaN is not the largest
+      // of anything: it is looked for by itself.
       float most = 0.f;
       bool odd = false;
 #pragma unroll
