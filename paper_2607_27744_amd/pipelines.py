@@ -8,7 +8,9 @@ then enqueues one pass of the hot path on the current stream and allocates
 nothing. Host work here is argument marshalling only.
 
 `history_step` is a batch of ranking over histories that are kept, projected,
-in a paged cache between batches (`prepare_history_cache`).
+in a paged cache between batches (`prepare_history_cache`); `adapted_step` the same
+with each request's adapters, rotated positions and a cache in 4 bits
+(`prepare_adapted_cache`).
 """
 
 from types import SimpleNamespace
@@ -251,4 +253,43 @@ def history_step(p, slots, s_new, offsets, e_c, cand_offsets, max_kv_len=None):
                                  slopes=p.slopes, max_kv_len=max_kv_len)
     cands = ops.paged_attention(q_c, k, v, p.table, p.lens, cand_offsets, slots=slots,
                                 causal=False, max_kv_len=max_kv_len)
+    return {"events": events, "candidates": cands, "status": status}
+
+
+def prepare_adapted_cache(w, adapters, *, pages, page_size=64, table_width=64, slots=None,
+                          base=10000.0, device="cuda"):
+    """Upload the weights of a `history_case` and its `adapters_of`, and make an empty cache in 4
+    bits for its histories. Event rows are projected to queries, K and V in one product; heads are
+    turned whole, with frequencies base^(-i / (d / 2))."""
+    dev = torch.device(device)
+    d = w.head_dim
+    p = SimpleNamespace(h=w.heads, hk=w.kv_heads, d=d, page=page_size,
+                        wqkv=_bf16(np.concatenate([w.wq_s, w.wkv]), dev), wq_c=_bf16(w.wq_c, dev),
+                        a=_bf16(adapters.a, dev), b=_bf16(adapters.b, dev),
+                        scales=_f32(adapters.scales, dev),
+                        freqs=_f32(base ** (-np.arange(d // 2) / (d // 2)), dev))
+    p.pool, p.table, p.lens, p.refs = ops.cache_pool_fp4(
+        1, pages, page_size, w.kv_heads, d, slots=slots or w.n_req, table_width=table_width,
+        device=dev)
+    return p
+
+
+def adapted_step(p, slots, adapter_ids, s_new, offsets, e_c, cand_offsets, max_kv_len=None):
+    """One batch of ranking over histories cached in 4 bits: request r is cache slot slots[r] and has
+    adapter adapter_ids[r] (none if it is out of range). Its new events are projected with the adapter
+    beside the shared weights, turned by their positions and appended, and attend over the whole
+    history; its candidates stand one position behind the history's end and attend over all of it.
+    Returns {"events", "candidates", "status"}; see ops.cache_check for the status."""
+    m, n, h, hk, d = s_new.shape[0], e_c.shape[0], p.h, p.hk, p.d
+    qkv = ops.adapter_linear(s_new, p.wqkv, p.a, p.b, offsets, adapter_ids, scales=p.scales)
+    q, k, v = (x.unflatten(1, (-1, d)) for x in qkv.split([h * d, hk * d, hk * d], dim=1))
+    rows, status = ops.cache_reserve(slots, offsets, m, p.table, p.lens, p.refs, p.page)
+    q = ops.cache_append(k, v, rows, p.pool[0], p.freqs, q=q, offsets=offsets, slots=slots,
+                         lens=p.lens)
+    events = ops.paged_attention_fp4(q, p.pool[0], p.table, p.lens, offsets, kv_heads=hk, slots=slots,
+                                     max_kv_len=max_kv_len)
+    ends = p.lens[slots.long()][ops.request_ids(cand_offsets, n).long()]
+    q_c = ops.rotate(ops.ikbo_linear(e_c, p.wq_c).view(n, h, d), p.freqs, positions=ends)
+    cands = ops.paged_attention_fp4(q_c, p.pool[0], p.table, p.lens, cand_offsets, kv_heads=hk,
+                                    slots=slots, causal=False, max_kv_len=max_kv_len)
     return {"events": events, "candidates": cands, "status": status}

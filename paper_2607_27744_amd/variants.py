@@ -44,6 +44,11 @@ line with the call's algorithmic FLOPs and bytes against the MI355X peaks.
   history_step      a batch of ranking over cached histories: append 4 events of
                     each of 64 users, encode them, 200 candidates each over
                     the pages (4 heads x 64, history 1024)
+  adapter_linear    16 histories of 2,048 rows, 1024 -> 1536, eight adapters of
+                    rank 32 beside the weights (and the weights alone)
+  paged_step_fp4    paged_step over a cache in 4 bits
+  adapted_step      history_step with each request's adapter, rotated positions and
+                    a cache in 4 bits
 """
 
 
@@ -59,7 +64,7 @@ PEAK_HBM_GBS = 8000.0
 NAMES = ("lcb", "dca_tq32", "dca_tq64", "dca_mapped", "dca_request", "linear_mapped",
          "linear_combined",
          "glm_linear", "dca_layer", "mlp2", "fm_linear", "history_attention", "paged_step",
-         "history_step")
+         "history_step", "adapter_linear", "paged_step_fp4", "adapted_step")
 
 
 def _bf16(a):
@@ -385,6 +390,74 @@ def _history_step(steps, warmup):
                  ms, flops, byts, "mfma", n, "candidates")
 
 
+def _adapter_linear(steps, warmup):
+    r, n, k, d, rank, count = 16, 16 * 2048, 1024, 1536, 32, 8
+    g = torch.Generator(device="cuda").manual_seed(9)
+    mk = lambda *s: (torch.randn(s, generator=g, device="cuda") * s[-1] ** -0.5).to(torch.bfloat16)  # noqa: E731
+    x, w, a, b = mk(n, k) * k ** 0.5, mk(d, k), mk(count, rank, k), mk(count, d, rank)
+    off, ids = _i32(np.arange(r + 1) * (n // r)), _i32(np.arange(r) % count)
+    out = torch.empty((n, d), dtype=torch.bfloat16, device="cuda")
+    ms = _time(lambda: ops.adapter_linear(x, w, a, b, off, ids, out=out), steps, warmup)
+    ms_plain = _time(lambda: ops.ikbo_linear(x, w, out=out), steps, warmup)
+    return _line("adapter_linear", {"requests": r, "rows": n, "k": k, "d_out": d, "rank": rank,
+                                    "adapters": count},
+                 ms, 2.0 * n * (k * d + rank * (k + d)),
+                 2.0 * (n * (k + d) + k * d + count * rank * (k + d)), "mfma", n, "rows",
+                 {"without_adapters_ms": round(ms_plain, 4)})
+
+
+def _adapted_cache(r, length, new, steps_ahead, h, hk, d, page):
+    """A 4-bit cache of r histories of `length` events, with room for the timed steps' events."""
+    from . import pipelines
+    w = wl.history_case([200] * r, [[length] * r, [new] * r], heads=h, kv_heads=hk, head_dim=d,
+                        seed=8)
+    width = -(-(length + new * steps_ahead) // page)
+    p = pipelines.prepare_adapted_cache(w, wl.adapters_of(w, 8, 16), pages=r * width,
+                                        page_size=page, table_width=width)
+    slots = _i32(np.random.default_rng(8).permutation(r))
+    ids = _i32(np.arange(r) % 9)                          # one request in nine has no adapter
+    first, b = w.batches
+    fill = pipelines.adapted_step(p, slots, ids, _bf16(first.s), _i32(first.offsets), _bf16(first.e_c),
+                                  _i32(first.cand_offsets))
+    ops.cache_check(fill["status"])
+    return p, slots, ids, (_bf16(b.s), _i32(b.offsets), _bf16(b.e_c), _i32(b.cand_offsets))
+
+
+def _paged_step_fp4(steps, warmup):
+    r, length, h, hk, d, page = 128, 2048, 8, 8, 128, 64
+    p, slots, _, (_, offsets, _, _) = _adapted_cache(r, length, 1, 1, h, hk, d, page)
+    q = torch.randn((r, h, d), device="cuda").to(torch.bfloat16)
+    out = torch.empty_like(q)
+    ms = _time(lambda: ops.paged_attention_fp4(q, p.pool[0], p.table, p.lens, offsets, kv_heads=hk,
+                                               slots=slots, max_kv_len=length, out=out),
+               steps, warmup)
+    return _line("paged_step_fp4", {"requests": r, "history": length, "heads": h, "kv_heads": hk,
+                                    "head_dim": d, "page_size": page, "rows_per_request": 1},
+                 ms, 4.0 * r * length * h * d, 1.0 * r * length * p.pool.shape[3] + 4.0 * r * h * d,
+                 "hbm", r, "events")
+
+
+def _adapted_step(steps, warmup):
+    from . import pipelines
+    r, length, new, h, hk, d, page = 64, 1024, 4, 4, 4, 64, 64
+    p, slots, ids, b = _adapted_cache(r, length, new, steps + warmup, h, hk, d, page)
+    last = {}
+
+    def step():
+        last.update(pipelines.adapted_step(p, slots, ids, *b,
+                                           max_kv_len=length + new * (steps + warmup)))
+    ms = _time(step, steps, warmup)
+    ops.cache_check(last["status"])
+    n, d_seq = r * 200, 256
+    flops = (4.0 * (r * 200 + r * new) * length * h * d + 2.0 * n * d_seq * h * d
+             + 2.0 * r * new * d_seq * (h + 2 * hk) * d)
+    byts = 1.0 * r * length * p.pool.shape[3] + 2.0 * n * (d_seq + h * d)
+    return _line("adapted_step", {"requests": r, "candidates_per_request": 200, "history": length,
+                                  "new_events_per_request": new, "heads": h, "head_dim": d,
+                                  "page_size": page, "adapters": 8, "rank": 16},
+                 ms, flops, byts, "mfma", n, "candidates")
+
+
 def run(name, steps=20, warmup=3):
     """Time one variant; returns its JSON-ready record."""
     ops.load_library()
@@ -416,4 +489,10 @@ def run(name, steps=20, warmup=3):
         return _paged_step(steps, warmup)
     if name == "history_step":
         return _history_step(steps, warmup)
+    if name == "adapter_linear":
+        return _adapter_linear(steps, warmup)
+    if name == "paged_step_fp4":
+        return _paged_step_fp4(steps, warmup)
+    if name == "adapted_step":
+        return _adapted_step(steps, warmup)
     raise ValueError(f"variant must be one of {NAMES}")

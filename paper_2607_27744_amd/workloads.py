@@ -266,6 +266,16 @@ def history_case(counts, events, *, heads=4, kv_heads=2, head_dim=64, d_seq=256,
         slopes=np.float32(2.0) ** -np.arange(2, 2 + heads, dtype=np.float32))
 
 
+def adapters_of(w, count, rank, seed=0, config_id=801):
+    """Low-rank adapters (A [count, rank, d_seq], B [count, D, rank], scales [count]) of a history_case's
+    event projection, D its stacked query, K and V rows."""
+    rng = lambda t: tensor_rng(seed, config_id, t)   # noqa: E731
+    d_seq, d_out = w.wq_s.shape[1], w.wq_s.shape[0] + w.wkv.shape[0]
+    return SimpleNamespace(a=normal(rng(1), (count, rank, d_seq), 1.0 / np.sqrt(d_seq)),
+                           b=normal(rng(2), (count, d_out, rank), 0.5 / np.sqrt(rank)),
+                           scales=rng(3).uniform(0.5, 2.0, count).astype(np.float32))
+
+
 def _weights(seed, cid, tid, d_out, fan_in, bf16=True):
     return normal(tensor_rng(seed, cid, tid), (d_out, fan_in),
                   std=1.0 / np.sqrt(fan_in), bf16=bf16)
