@@ -40,7 +40,9 @@ extern "C" {
  * Fast path (bf16 MFMA kernels): K, rank and x_row_stride multiples of 8, D a
  * multiple of 4, x, w, a and b 16-byte aligned, out 16-byte aligned. Other
  * cases run a general kernel (fp32 matrix instructions).
- * Limits: rank <= 256; K, D < 2^22; N < 2^31, R < 2^31, N * rank < 2^40.
+ * An infinity or NaN in one request's rows or adapter does not reach another's; where
+ * one stands in B, the rows that share its tiles of 32 are formed again by a slow path.
+ * Limits: rank <= 256; K, D < 2^22; R + N / 32 < 2^23 and N / 128 * D / 128 < 2^24.
  * ---------------------------------------------------------------------------
  */
 size_t rocs_adapter_workspace_size(int64_t num_requests, int64_t num_rows, int64_t k, int64_t d_out,
@@ -82,8 +84,8 @@ int32_t rocs_adapter_linear(const void* x, int64_t x_row_stride, const void* w, 
  *   ROCS_POOL_ROWS  a row is [2, kv_heads, head_dim] of dtype: K, then V
  *   ROCS_POOL_FP4   a row is rocs_fp4_row_bytes(kv_heads, head_dim) bytes, in 4
  *                   bits a value, see below; the pool 16-byte aligned
- * Limits: head_dim <= 256, num_heads, kv_heads < 2^16, num_rows * heads <=
- * 2^30 (of q, and of k with v), num_pool_rows < 2^31.
+ * Limits: head_dim <= 256, num_heads, kv_heads < 2^16, num_rows < 2^24, num_rows *
+ * heads <= 2^30 (of q, and of k with v), num_pool_rows < 2^31.
  *
  * The 4-bit form (OCP's MXFP4 element and scale). head_dim is a multiple of 32.
  * A block of 32 values of a head shares a scale byte E; a value is the sign and
@@ -121,7 +123,8 @@ int32_t rocs_cache_append(const void* q, int64_t q_row_stride, const void* k, co
 size_t rocs_fp4_row_bytes(int32_t kv_heads, int32_t head_dim);
 
 /* Rows rows[m] of a 4-bit pool as values: out [num_rows, 2, kv_heads, head_dim]
- * (K, then V; dense). A row number outside the pool gives zeros. */
+ * (K, then V; dense; 16-byte aligned, as the pool is). A row number outside the
+ * pool gives zeros. */
 int32_t rocs_cache_read_fp4(const int32_t* rows, int64_t num_rows, const void* pool,
                             int64_t num_pool_rows, int32_t kv_heads, int32_t head_dim,
                             int32_t dtype, void* out, void* stream);

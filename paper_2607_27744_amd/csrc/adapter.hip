@@ -3,9 +3,8 @@
 //   out[n] = act( W x[n] + bias + B_a t[n] ),  t[n] = s_a A_a x[n],  a = ids[request of n]
 //
 // t comes first, in a launch of its own (every output column needs all of it).
-#include "common.h"
+#include "adapter.h"
 #include "launch.h"
-#include "layer.h"
 
 namespace rocs {
 namespace {
@@ -214,7 +213,7 @@ __global__ __launch_bounds__(512) void adapter_few(const AdapterArgs a, const Lo
   const int64_t n0 = (int64_t)(blockIdx.x / (uint32_t)tiles_m) * 32;
   const int64_t n = min(n0 + l32, a.N - 1);
   const int d = min(d0 + l32, a.D - 1);
-  int mine = lr.aid[n];
+  int mine = adapter_at(lr, n);
   const int64_t n_rows = rows_of(a);
   const bf16_t* x = static_cast<const bf16_t*>(a.x) + n * a.x_stride + 8 * hh;
   const bf16_t* w = static_cast<const bf16_t*>(a.w) + (int64_t)d * a.K + 8 * hh;

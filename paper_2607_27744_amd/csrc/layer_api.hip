@@ -16,6 +16,8 @@ namespace {
 
 // Limits that keep the kernels' 32-bit indices in range (see rocs_history.h).
 constexpr int64_t kMaxRows = int64_t(1) << 30;
+// Rows of a rotation: a workgroup may have one alone, and a grid fewer than 2^24.
+constexpr int64_t kMaxTurned = (int64_t(1) << 24) - 1;
 constexpr int64_t kMaxKeys = (int64_t(1) << 31) - 4096;
 
 struct Span {
@@ -49,7 +51,7 @@ int32_t check_turn(const char* name, AppendArgs& a, int32_t rot_dim, int64_t R, 
   if (a.M < 0 || a.H < 0 || a.Hk < 0 || a.D < 1 || a.q_stride < 0 || a.kv_stride < 0 || R < 0 || S < 0)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: a size is out of range", name);
   if (a.D > 256) return fail(ROCS_ERR_UNSUPPORTED, "%s: head_dim %d > 256", name, a.D);
-  if (a.H > 65535 || a.Hk > 65535 || R > kMaxI32 || S > kMaxI32 || a.M > kMaxI32 ||
+  if (a.H > 65535 || a.Hk > 65535 || R > kMaxI32 || S > kMaxI32 || a.M > kMaxTurned ||
       a.M * a.H > kMaxRows || a.M * 2 * a.Hk > kMaxRows)
     return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
   if (rot_dim < 0 || rot_dim % 2 != 0 || rot_dim > a.D)
@@ -100,7 +102,7 @@ int32_t rocs_adapter_linear(const void* x, int64_t x_row_stride, const void* w, 
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: a size is out of range", name);
   if (rank > 256) return fail(ROCS_ERR_UNSUPPORTED, "%s: rank %d > 256", name, rank);
   if (R > kMaxI32 || N > kMaxI32 || K >= (1 << 22) || D >= (1 << 22) || num_adapters > kMaxI32 ||
-      N * rank >= (int64_t(1) << 40) || x_row_stride > (int64_t(1) << 31))
+      R + N / 32 >= (1 << 23) - 1 || (N / 128 + 1) * (D / 128 + 1) >= (1 << 24) || x_row_stride > (int64_t(1) << 31))
     return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
   if (x_row_stride != 0 && x_row_stride < K)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: x_row_stride < K", name);

@@ -13,10 +13,9 @@
 // The general path (fp32, sizes or pointers off the fast path's alignment) runs
 // on the fp32 matrix instructions: two steps for large calls, for small ones a
 // single launch that takes the request term into the candidates' product.
-#include "common.h"
+#include "adapter.h"
 #include "kernels.h"
 #include "launch.h"
-#include "layer.h"
 #include "linear_rule.h"
 
 #include <atomic>
@@ -264,7 +263,7 @@ __device__ __noinline__ void adapter_rows_again(const bf16_t* x, const bf16_t* w
   while (mask != 0) {
     const int64_t n = n0 + __builtin_ctz(mask);
     mask &= mask - 1;
-    const int id = lr.aid[n];
+    const int id = adapter_at(lr, n);
     if (!dok) continue;
     float sum = 0.f;
     for (int k = 0; k < K; ++k) sum += load_f32(x + n * lr.x_stride + k) * load_f32(w + (int64_t)d * K + k);
@@ -459,7 +458,7 @@ void ikbo_gemm_tile(
 #pragma unroll
     for (int fn = 0; fn < FN; ++fn) {
       const int64_t n = n0 + wn0 + 32 * fn + l32;
-      const int mine = n < n_rows ? lr.aid[n] : -1;
+      const int mine = n < n_rows ? adapter_at(lr, n) : -1;
       const bf16_t* t = lr.t + min(n, n_rows - 1) * lr.cols + 8 * hh;
       int count = 0;
       for (uint64_t todo = __ballot(mine >= 0); todo != 0; ++count) {
@@ -938,7 +937,7 @@ void ikbo_gemm_stream(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w
   auto add_adapters = [&](const StreamTile& c) __attribute__((always_inline)) -> bool {
     int mine[4];
 #pragma unroll
-    for (int fn = 0; fn < 4; ++fn) mine[fn] = lr.aid[c.n0 + min(wn0 + 32 * fn + l32, c.rows - 1)];
+    for (int fn = 0; fn < 4; ++fn) mine[fn] = adapter_at(lr, c.n0 + min(wn0 + 32 * fn + l32, c.rows - 1));
     const bf16_t* pt[4];
 #pragma unroll
     for (int fn = 0; fn < 4; ++fn)

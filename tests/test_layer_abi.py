@@ -58,7 +58,8 @@ def _adapter(lib, **kw):
 @no_gpu
 @pytest.mark.parametrize("bad, status", [
     (dict(dtype=3), BAD), (dict(act=5), BAD), (dict(N=-1), BAD), (dict(K=0), BAD), (dict(rank=0), BAD),
-    (dict(rank=257), UNS), (dict(K=1 << 22), UNS), (dict(N=1 << 31), UNS), (dict(xs=63), BAD),
+    (dict(rank=257), UNS), (dict(K=1 << 22), UNS), (dict(N=1 << 31), UNS), (dict(N=1 << 28), UNS),
+    (dict(R=1 << 23), UNS), (dict(N=1 << 22, D=1 << 20, ws_bytes=1 << 40), UNS), (dict(xs=63), BAD),
     (dict(R=0), BAD), (dict(x=None), BAD), (dict(w=None), BAD), (dict(a=None), BAD), (dict(b=None), BAD),
     (dict(off=None), BAD), (dict(ids=None), BAD), (dict(out=None), BAD), (dict(count=-1), BAD),
     (dict(ws=None), _lib.WORKSPACE_TOO_SMALL), (dict(ws_bytes=8), _lib.WORKSPACE_TOO_SMALL),
@@ -88,7 +89,7 @@ def _append(lib, **kw):
     (dict(ks=127), BAD), (dict(qs=255), BAD), (dict(pool_rows=-1), BAD), (dict(pool_rows=1 << 31), UNS),
     (dict(D=48, rot=48, form=1), UNS), (dict(form=1, pool=P(0x80000008)), BAD),
     (dict(pool=FAKE[1]), BAD), (dict(pool=FAKE[3]), BAD), (dict(qo=FAKE[0]), BAD), (dict(qo=FAKE[8]), BAD),
-    (dict(qo=FAKE[7]), BAD), (dict(M=1 << 30), UNS), (dict(M=0), _lib.OK)])
+    (dict(qo=FAKE[7]), BAD), (dict(M=1 << 24), UNS), (dict(M=1 << 20, H=2048), UNS), (dict(M=0), _lib.OK)])
 def test_append_refusals(lib, bad, status):
     assert _append(lib, **bad) == status
     assert (lib.rocs_last_error_message() == b"") == (status == _lib.OK)
@@ -207,3 +208,19 @@ def test_ops_paged_fp4_checks():
                        (dict(causal=2), "causal"), (dict(out=_t(2, 4, 32)), "out must"), (dict(), "on the GPU")):
         with pytest.raises(ValueError, match=match):
             ops.paged_attention_fp4(**{**ok, **bad})
+
+
+def test_fp4_workspaces_have_a_bound(lib):
+    # The header's bound for one workspace under calls of many sizes.
+    size, tight = lib.rocs_paged_fp4_workspace_size, 0.0
+    for dtype, d in ((1, 128), (1, 64), (1, 96), (1, 160), (0, 64)):
+        c = 524288 if dtype == 1 and d <= 128 else 8192
+        for h, hk in ((8, 8), (8, 2), (16, 1), (64, 8), (5, 5)):
+            for n in (1, 3, 40, 500, 7000):
+                for most in (1, 300, 5000, 70000, 3000000):
+                    bound = 4 * (d + 2) * min(h * n * min(256, -(-most // 256)), c) + 512
+                    for r in (1, 2, 7, 64, 129, 1000, 7000):
+                        need = size(r, n, h, hk, d, most, dtype)
+                        assert need <= bound, (dtype, d, h, hk, n, most, r)
+                        tight = max(tight, need / bound)
+    assert tight > 0.5
