@@ -118,31 +118,72 @@ __attribute__((amdgpu_waves_per_eu(DP == 256 && sizeof(T) == 4 ? 1 : 2))) void h
     // the result is not stored.
     const Fp4Row fr{a.Hk, D};
     const char* base = static_cast<const char*>(a.k);
+    // The next block's words load while this one is computed, where registers allow it: fp32 q, 128
+    // single rows over 3,100 keys of 8 heads of 128, 587 us and 759 without; of 256 it spills in bf16
+    // (1,711 and 1,246).
+    constexpr bool AHEAD = DP <= 128;
     constexpr int WORDS = (DP / 4 + 7) / 8, VW = (NB + 7) / 8;
-    for (int kb = lo + 16 * wave; kb < hi; kb += 64) {
-      const char* kr = base + key_row(a, t, min(kb + l16, hi - 1));
-      const char* vr[4];
+    uint32_t kn[WORDS], vn[4][VW], ken[WORDS], ven[4][VW];
+    PoolKey at[5];                         // key l16, and V's 4 g .. + 3
+    auto look_up = [&](int kb) __attribute__((always_inline)) {
+      at[4] = pool_key(a, t.pages, min(kb + l16, hi - 1));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vr[i] = base + key_row(a, t, min(kb + 4 * g + i, hi - 1));
-      uint32_t vw[4][VW];
-      float vs[4][VW];
+      for (int i = 0; i < 4; ++i) at[i] = pool_key(a, t.pages, min(kb + 4 * g + i, hi - 1));
+    };
+    auto load = [&]() __attribute__((always_inline)) {
+      const char* kr = base + (int64_t)pool_row(a, at[4]) * a.kv_stride;
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) {
+        const int d = min(DP / 4 * g + 8 * w, D - 8);
+        kn[w] = *reinterpret_cast<const uint32_t*>(kr + fr.values(0, hk) + d / 2);
+        ken[w] = (uint8_t)kr[fr.scales(0, hk) + d / kFp4Block];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const char* vr = base + (int64_t)pool_row(a, at[i]) * a.kv_stride;
+#pragma unroll
+        for (int c = 0; c < VW; ++c) {
+          const int d = min(NB * l16 + 8 * c, D - 1);
+          vn[i][c] = *reinterpret_cast<const uint32_t*>(vr + fr.values(1, hk) + d / 8 * 4);
+          ven[i][c] = (uint8_t)vr[fr.scales(1, hk) + d / kFp4Block];
+        }
+      }
+    };
+    const int first = lo + 16 * wave;
+    if (AHEAD && first < hi) {
+      look_up(first);
+      load();
+      look_up(first + 64);
+    }
+    for (int kb = first; kb < hi; kb += 64) {
+      uint32_t kw[WORDS], vw[4][VW];
+      float ks[WORDS], vs[4][VW];
+      if constexpr (!AHEAD) {
+        look_up(kb);
+        load();
+      }
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) {
+        kw[w] = kn[w];
+        ks[w] = fp4_scale(ken[w]);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int c = 0; c < VW; ++c) {
-          const int d = min(NB * l16 + 8 * c, D - 1);
-          vw[i][c] = *reinterpret_cast<const uint32_t*>(vr[i] + fr.values(1, hk) + d / 8 * 4) >> (4 * (d % 8));
-          vs[i][c] = fp4_scale((uint8_t)vr[i][fr.scales(1, hk) + d / kFp4Block]);
+          vw[i][c] = vn[i][c] >> (4 * (min(NB * l16 + 8 * c, D - 1) % 8));
+          vs[i][c] = fp4_scale(ven[i][c]);
         }
+      if constexpr (AHEAD) {
+        load();                            // the next block; past the end the last key
+        look_up(kb + 128);
+      }
       f32x4 part[4] = {};
 #pragma unroll
       for (int w = 0; w < WORDS; ++w) {
-        const int d = min(DP / 4 * g + 8 * w, D - 8);
-        const uint32_t word = *reinterpret_cast<const uint32_t*>(kr + fr.values(0, hk) + d / 2);
-        const float ks = fp4_scale((uint8_t)kr[fr.scales(0, hk) + d / kFp4Block]);
 #pragma unroll
         for (int i = 0; i < (DP / 4 < 8 ? DP / 4 : 8); ++i)
-          part[i % 4] = __builtin_amdgcn_mfma_f32_16x16x4f32(fp4_value(word, i, ks), qf[2 * w + i / 4][i % 4],
+          part[i % 4] = __builtin_amdgcn_mfma_f32_16x16x4f32(fp4_value(kw[w], i, ks[w]), qf[2 * w + i / 4][i % 4],
                                                              part[i % 4], 0, 0, 0);
       }
       f32x4 p;
@@ -368,7 +409,9 @@ hipError_t launch_general(const HistArgs& a, hipStream_t s) {
 // A 4-bit cache: head_dim is a multiple of 32, so q's rows are aligned to four
 // elements if its pointer and stride are.
 template <typename T, int DP>
-hipError_t launch_general_fp4(const HistArgs& a, hipStream_t s) {
+hipError_t launch_general_fp4(const HistArgs& args, hipStream_t s) {
+  HistArgs a = args;
+  set_page_divisor(a);
   const int64_t slots = a.R + (a.N * a.G + kGenTile - 1) / kGenTile;
   if (!grid_fits(slots, 256)) return hipErrorInvalidConfiguration;
   const bool vec = a.q_stride % 4 == 0 && reinterpret_cast<uintptr_t>(a.q) % (4 * sizeof(T)) == 0;

@@ -73,6 +73,27 @@ __device__ __forceinline__ int64_t key_row(const HistArgs& a, const HistTile& t,
   return p * a.page_stride + (int64_t)(j - c * a.page_size) * a.kv_stride;
 }
 
+// A 4-bit pool has dense rows and pages, of any page size: the row number of key j, a
+// lane each. j / page_size for j below 2^31 is a product's upper half and a shift: with
+// l = ceil(log2 page_size), floor(2^(31 + l) / page_size) + 1 is exact.
+inline void set_page_divisor(HistArgs& a) {
+  int l = 0;
+  while ((int64_t(1) << l) < a.page_size) ++l;
+  a.page_magic = a.page_size > 1 ? (uint32_t)((uint64_t(1) << (31 + l)) / (uint64_t)a.page_size + 1) : 0;
+  a.page_shift = l > 0 ? l - 1 : 0;
+}
+struct PoolKey {
+  int entry, in_page;        // the page table's entry as it stands; row in the page
+};
+__device__ __forceinline__ PoolKey pool_key(const HistArgs& a, const int32_t* pages, int j) {
+  const int c = a.page_size == 1 ? j : (int)(__umulhi((uint32_t)j, a.page_magic) >> a.page_shift);
+  return {pages[c], j - c * a.page_size};
+}
+__device__ __forceinline__ int pool_row(const HistArgs& a, const PoolKey& k) {
+  const uint32_t p = min((uint32_t)k.entry, (uint32_t)(a.pages - 1));
+  return (int)(p * (uint32_t)a.page_size) + k.in_page;
+}
+
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
