@@ -23,7 +23,7 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t n) {
 // General path: any dtype, sizes and alignment; t in fp32.
 // ---------------------------------------------------------------------------
 
-// A wave a row: four of the row's rank at a time.
+// A wave a row: four of the row's rank at a time. Bound by the loads of A, from L2.
 template <typename T>
 __global__ __launch_bounds__(256) void shrink_general(const AdapterArgs a, int cols) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -119,7 +119,8 @@ __global__ __launch_bounds__(256) void adapter_general(const AdapterArgs a, int 
 // Requests of few rows: a workgroup takes 32 rows of one request (tiles as in common.h:
 // tile_base) and all of the rank, 32 RK columns at a time; its eight waves split K,
 // operands straight from global memory, and add up through LDS in a fixed order.
-// Requests of many rows take the tiled linear (linear.hip: SHRINK).
+// Requests of many rows take the tiled linear (linear.hip: SHRINK). Bound by latency, one
+// trip over K / 8: 128 rows of 48 adapters, K 1,024, rank 16: 5.1 us; 8 rows, K 256: 3.4.
 // ---------------------------------------------------------------------------
 template <int RK>
 __global__ __launch_bounds__(512) void shrink_rows(const AdapterArgs a, const LowRank lr) {
@@ -202,6 +203,8 @@ hipError_t launch_shrink(const AdapterArgs& a, const LowRank& lr, hipStream_t s)
 // straight from global memory, partial sums are added up through LDS in a fixed order.
 // Bound by latency: the first loads depend on nothing (rows up to num_rows are read; those
 // behind the last request are dropped), and B's are issued before the first products.
+// 128 rows of 48 adapters, 1,024 -> 1,536, rank 16: 7.9 us (64 x 64 tiles of the linear: 20
+// more); 8 rows, 256 -> 512: 4.4.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(512) void adapter_few(const AdapterArgs a, const LowRank lr, int tiles_m) {
   constexpr int U = 8;                         // steps of a wave in flight
@@ -328,12 +331,25 @@ hipError_t launch_adapter(const AdapterArgs& a, bool fast, hipStream_t s) {
   int32_t* aid = reinterpret_cast<int32_t*>(static_cast<char*>(a.t) + adapter_t_bytes(a.N, a.rank));
   const LowRank lr{t, static_cast<const bf16_t*>(a.b), aid, a.off, a.x_stride, adapter_cols(a.rank), a.rank,
                    a.A, a.R};
-  const hipError_t e = a.N / a.R >= 64 ? launch_adapter_shrink(a, lr, s)
-                       : a.rank > 32   ? launch_shrink<2>(a, lr, s)
-                                       : launch_shrink<1>(a, lr, s);
+  // The tiled linear for t pays where its tiles fill and there are enough of them (the
+  // whole call in us, shrink_rows / tiled; K x D, rank): 9,001 rows of 24 requests,
+  // 1,024 x 1,536, 32: 45 / 41; 32,768 of 16, 2,048 x 2,048, 64: 316 / 285; 8,000 of 400,
+  // 1,024 x 1,024, 64: 59 / 51; 1,024 of 64, 64: 24 / 22; but 4,096 of 256, 16: 29 / 30; 2,048 of
+  // 128, 32: 30 / 32; 8,000 of 1,000, 16: 49 / 51.
+  const bool tiled = a.N / a.R >= 16 && a.N >= (a.rank > 32 ? 1024 : 8000);
+  const hipError_t e = tiled          ? launch_adapter_shrink(a, lr, s)
+                       : a.rank > 32 ? launch_shrink<2>(a, lr, s)
+                                     : launch_shrink<1>(a, lr, s);
   if (e != hipSuccess) return e;
+  // Few tiles of the linear leave CUs idle, and its K is one chain; single events of many
+  // adapters also make its blocks of 32 rows take them one after the other. In us, linear /
+  // adapter_few: 128 rows, 1,024 x 1,024, rank 16, one adapter 16.7 / 15.4, a row each of 30
+  // 20.7 / 13.2 (32 tiles); 192 rows, 1,024 x 2,048 (96 tiles), 17.5 / 20.7, a row each of 8
+  // 16.6 / 18.6, of 64 23.6 / 19.3; 256 rows, 2,048 x 2,048, rank 64, of 64 (128 tiles) 71 / 53; 512 rows,
+  // rank 16, of 64 (256 tiles) 34 / 51.
   const int64_t tiles = (int64_t)((a.N + 63) / 64) * ((a.D + 63) / 64);
-  return tiles < 128 ? launch_few(a, lr, s) : launch_adapter_gemm(a, lr, s);
+  const bool few = tiles <= 64 || (tiles <= 128 && a.N < 4 * (int64_t)a.R && a.A >= 16);
+  return few ? launch_few(a, lr, s) : launch_adapter_gemm(a, lr, s);
 }
 
 }  // namespace rocs

@@ -92,6 +92,18 @@ def test_row_counts(gpu_lib, n):
     check(c, kw, counts, ids, ops.adapter_linear(**c, **kw))
 
 
+@pytest.mark.parametrize("counts, k, d, rank, adapters", [
+    ([1] * 200, 64, 1344, 8, 20), ([1] * 200, 64, 1344, 8, 15), ([3] * 85, 128, 1992, 40, 30),
+    ([16] * 64, 64, 64, 48, 5), ([15] * 70, 64, 64, 48, 5), ([(7 * i) % 40 for i in range(60)], 72, 136, 64, 9),
+    ([(11 * i) % 34 for i in range(500)], 64, 72, 16, 7), ([(11 * i) % 34 for i in range(500)], 64, 128, 32, 40)],
+    ids=lambda v: str(len(v)) if isinstance(v, list) else str(v))
+def test_many_short_requests(gpu_lib, counts, k, d, rank, adapters):
+    # Either side of the sizes at which the kernels change.
+    ids = [(5 * i) % (adapters + 2) - 1 for i in range(len(counts))]
+    c, kw = make(counts, ids, k, d, rank, adapters, BF, seed=d + rank)
+    check(c, kw, counts, ids, ops.adapter_linear(**c, **kw))
+
+
 @pytest.mark.parametrize("dtype, k", [(BF, 64), (BF, 60), (F32, 64)])
 def test_strided_rows_and_a_padded_batch(gpu_lib, dtype, k):
     counts, ids = [3, 0, 50, 1], [1, 0, 0, -1]
