@@ -514,6 +514,15 @@ hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hip
   return bf16 ? launch_join<bf16_t>(a, s) : launch_join<float>(a, s);
 }
 
+// bf16: history_fp4_few up to 32 rows of a request and K/V head, two tiles of its 16 read the
+// keys twice through L2 (32 rows a wave cost more: registers for two of the three waves of a SIMD;
+// 64 requests, 3,125 keys, 8 heads on 2 x 128: 32 rows 60 us, by 16 55), then the 128-row tiles. In us,
+// few / tiles, 8 heads on 2 x 128, by the rows of a request and head: 64 requests over 3,125 keys
+// 16: 41 / 56, 24: 47 / 54, 32: 55 / 48, 40: 63 / 54, 64: 90 / 57; 128 requests 32: 92 / 113, 40: 107 / 109,
+// 48: 121 / 113; 8 on 8 x 64, 64 requests, 32: 105 / 133, 48: 133 / 122; one history of 8,000 rows 14 / 14
+// throughout. The cut of few rows is that of history_plan, with chunks of 512 keys in either
+// case: 128 single rows over 3,125 keys, 8 heads x 128: by four heads a workgroup 129 us, two 136,
+// one 207; chunks of 256 to 1,536 keys 128 to 164.
 HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
   const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head
   if (bf16 && D <= 128 && each > 32) return history_plan(R, N, H, Hk, D, max_len, true);
@@ -523,7 +532,7 @@ HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, b
     return general;
   }
   HistPlan p{};
-  p.rows = each <= 16 ? 16 : 32;
+  p.rows = 16;
   const auto parts = [max_len](int64_t most, int64_t least_keys) {
     const int64_t n = (max_len + least_keys - 1) / least_keys;
     return n < most ? n : most;
@@ -539,7 +548,7 @@ HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, b
 
 hipError_t launch_history_fp4(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s) {
   const hipError_t e = fast && rows == 128 ? launch_history_fp4_tile(a, s)
-                       : fast && rows > 0  ? launch_history_fp4_few(a, rows, s)
+                       : fast && rows > 0  ? launch_history_fp4_few(a, s)
                        : bf16              ? launch_general_fp4<bf16_t>(a, s)
                                            : launch_general_fp4<float>(a, s);
   if (e != hipSuccess || a.splits == 1) return e;

@@ -1,4 +1,4 @@
-// Attention over a cache held in 4 bits: the tiled kernel's launch, and the bf16 kernel for few rows: 16 or 32
+// Attention over a cache held in 4 bits: the tiled kernel's launch, and the bf16 kernel for few rows: 16
 // rows (token, head of the group) of one request a wave.
 //
 // A call over single events is a read of the cache, of which 4 bits leave a
@@ -16,13 +16,20 @@
 // have to go into the weights, of another block and key in each.)
 // 16 x 16 x 32 products: the heads of a group rarely fill more rows, and a score
 // costs an exponential. Waves and parts share a call as in history_split.
+// 128 single rows over 3,125 keys on average, 8 heads x 128: 125 us, 3.4 TB/s (a cache in
+// bf16: 287 us at 5.7 TB/s); 48 over 18,750, 16 heads on 2, capped: 91; 1 over 4,099: 8.2.
+// What bounds it: the loads of a stage and the work on it overlap only over the three
+// waves of a SIMD; without the work the loads take 88 us and 20 more for the scales, the
+// work alone 78. Two stages of registers (150 us), V's loads before K's products (136),
+// equal shares of stages for each workgroup (149) and K's and V's scales in one load (130 with
+// the join, 131 without) did not help.
 #include "history_tile.h"
 #include "launch.h"
 
 namespace rocs {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kFewRows = 16;
 
 // 16-byte chunk of a staged V row at which chunk c of `key` stands: c ^ this. The
 // eight rows of a half wave's transposing read and the quarter wave of a write fall on
@@ -33,17 +40,16 @@ __device__ __forceinline__ int v_swizzle(int key) {
   else return ((key >> 1) & 3) | (((key >> 1) & 1) << 2);
 }
 
-template <int D, int SCORE, int NR>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NR == 1 ? 3 : 2))) void
+template <int D, int SCORE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void
 history_fp4_few(const HistArgs a, int64_t slots) {
-  constexpr int kRows = 16 * NR;
   constexpr int KS = D / 32, DB = D / 16;   // products of a score, output blocks
   constexpr int BPR = D / kFp4Block;        // blocks of a key: V's loads of a lane and stage
   constexpr int ROWB = 2 * D;               // a staged V row
-  constexpr int STAGE = 32 * ROWB > kRows * D * 4 ? 32 * ROWB : kRows * D * 4;
+  constexpr int STAGE = 32 * ROWB > kFewRows * D * 4 ? 32 * ROWB : kFewRows * D * 4;
   __shared__ __attribute__((aligned(1024))) char lds[kWaves * STAGE];
-  __shared__ float pm[kWaves][kRows], pl[kWaves][kRows];
-  __shared__ int odd[kWaves][kRows];        // by head and row: to form again
+  __shared__ float pm[kWaves][kFewRows], pl[kWaves][kFewRows];
+  __shared__ int odd[kWaves][kFewRows];        // by head and row: to form again
   ROCS_LDS char* const lds3 = (ROCS_LDS char*)lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -60,25 +66,22 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   }
   const int hk0 = (int)group * HW, hk = hk0 + wave % HW;
   const int split = (int)(rest % (uint32_t)a.splits);
-  const HistTile t = hist_tile(a, slots - 1 - rest / (uint32_t)a.splits, kRows);
+  const HistTile t = hist_tile(a, slots - 1 - rest / (uint32_t)a.splits, kFewRows);
   if (t.rows <= 0) return;
-  for (int i = tid; i < kWaves * kRows; i += 256) odd[i / kRows][i % kRows] = 0;
+  for (int i = tid; i < kWaves * kFewRows; i += 256) odd[i / kFewRows][i % kFewRows] = 0;
 
-  RowRule rule[NR];
-  bf16x8 qf[NR][KS];
+  const int row = t.row0 + min(l16, t.rows - 1);              // clamped; extra rows never stored
+  const int token = row / a.G, head = hk * a.G + row % a.G;
+  RowRule rr;
+  score_rules<SCORE>(rr, a, head);
+  rr.pos = position_of(t, token);
+  rr.lim = limit_of(a, t, token);
+  bf16x8 qf[KS];
+  const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * a.D;
 #pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const int row = t.row0 + min(16 * r + l16, t.rows - 1);     // clamped; extra rows never stored
-    const int token = row / a.G, head = hk * a.G + row % a.G;
-    score_rules<SCORE>(rule[r], a, head);
-    rule[r].pos = position_of(t, token);
-    rule[r].lim = limit_of(a, t, token);
-    const bf16_t* q = static_cast<const bf16_t*>(a.q) + (t.q0 + token) * a.q_stride + (int64_t)head * a.D;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int d = D / 4 * g + 8 * ks;
-      qf[r][ks] = as_bf16x8(load16(q + d, d < a.D));
-    }
+  for (int ks = 0; ks < KS; ++ks) {
+    const int d = D / 4 * g + 8 * ks;
+    qf[ks] = as_bf16x8(load16(q + d, d < a.D));
   }
   const int lim_lo = limit_of(a, t, t.row0 / a.G);
   const int most = limit_of(a, t, (t.row0 + t.rows - 1) / a.G);
@@ -137,15 +140,10 @@ history_fp4_few(const HistArgs a, int64_t slots) {
   PoolKey next_key;
   auto look_up = [&](int at) __attribute__((always_inline)) { next_key = pool_key(a, t.pages, min(at + lane, hi - 1)); };
 
-  float m[NR], l_part[NR];
-  f32x4 o[NR][DB];
+  float m = -INFINITY, l_part = 0.f;
+  f32x4 o[DB];
 #pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    m[r] = -INFINITY;
-    l_part[r] = 0.f;
-#pragma unroll
-    for (int db = 0; db < DB; ++db) o[r][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   // Transposing reads of V^T: rows 16 x + 4 g + jl / 4 of the staged 32, 16 dims.
   uint32_t va[2];
 #pragma unroll
@@ -164,7 +162,7 @@ history_fp4_few(const HistArgs a, int64_t slots) {
     load_v(rows_now);
   }
   for (; at < hi; at += 64 * KW) {
-    f32x4 s[NR][4];
+    f32x4 s[4];
 #pragma unroll
     for (int n = 0; n < BPR; ++n) {
       const int key = 64 / BPR * n + lane / BPR;
@@ -189,14 +187,10 @@ history_fp4_few(const HistArgs a, int64_t slots) {
     for (int kb = 0; kb < 4; ++kb) {
       const uint32_t e = (uint32_t)__shfl((int)kse, 16 * kb + l16) >> (8 * k_byte);
       const float scale = fp4_scale(e & 255u);
+      s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int r = 0; r < NR; ++r) s[r][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 kf = as_bf16x8(fp4_to_bf16x8(kc[kb][ks], scale));
-#pragma unroll
-        for (int r = 0; r < NR; ++r) s[r][kb] = mfma16(kf, qf[r][ks], s[r][kb]);
-      }
+      for (int ks = 0; ks < KS; ++ks)
+        s[kb] = mfma16(as_bf16x8(fp4_to_bf16x8(kc[kb][ks], scale)), qf[ks], s[kb]);
     }
     rows_now = pool_row(a, next_key);
     look_up(at + 128 * KW);
@@ -215,74 +209,69 @@ history_fp4_few(const HistArgs a, int64_t slots) {
       }
     };
     stage_v(0);
-    uint32_t pk[NR][4][2];
+    uint32_t pk[4][2];
+    if constexpr (SCORE != 0) {
+      const float rel = (float)(rr.pos - at - 4 * g);
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      const RowRule& rr = rule[r];
-      f32x4(&sr)[4] = s[r];
-      if constexpr (SCORE != 0) {
-        const float rel = (float)(rr.pos - at - 4 * g);
+      for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float shift = (SCORE & kCap) != 0 ? rr.cap2 : 0.f;
-            if constexpr ((SCORE & kBias) != 0) shift = fmaf(-rr.slope2, fabsf(rel - (float)(16 * kb + i)), shift);
-            const float x = sr[kb][i];
-            if constexpr ((SCORE & kCap) != 0)
-              sr[kb][i] = fmaf(-2.0f * rr.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * rr.cap_in)), shift);
-            else if constexpr ((SCORE & kWideCap) != 0)
-              sr[kb][i] = wide_cap(x, rr) + shift;
-            else
-              sr[kb][i] = fmaf(x, rr.scale2, shift);
-          }
-      }
-      if (at + 64 > lim_lo) {
-        const int seen = rr.lim - at - 4 * g;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (16 * kb + i >= seen) sr[kb][i] = -INFINITY;
-      }
-      const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
-      auto weights = [&](float ms) __attribute__((always_inline)) {
-        float sum = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            float e0 = sr[kb][2 * w], e1 = sr[kb][2 * w + 1];
-            if constexpr (SCORE == 0) {
-              e0 = fmaf(e0, rr.scale2, -ms);
-              e1 = fmaf(e1, rr.scale2, -ms);
-            } else {
-              e0 -= ms;
-              e1 -= ms;
-            }
-            pk[r][kb][w] = pack_bf16x2(__builtin_amdgcn_exp2f(e0), __builtin_amdgcn_exp2f(e1));
-            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[r][kb][w]), ones, sum, false);
-          }
-        return sum;
-      };
-      float sum = weights(m[r]);
-      if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
-        float mx = sr[0][0];
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sr[kb][i]);
-        mx = max_across_rows(mx) * (SCORE == 0 ? rr.scale2 : 1.0f);
-        const bool need = mx > m[r] + kLazyMove;
-        const float alpha = need ? exp2f(m[r] - mx) : 1.0f;
-        if (need) m[r] = mx;
-        l_part[r] *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[r][db] *= alpha;
-        sum = weights(m[r] == -INFINITY ? 0.f : m[r]);      // no key seen yet: weights 0
-      }
-      l_part[r] += sum;
+        for (int i = 0; i < 4; ++i) {
+          float shift = (SCORE & kCap) != 0 ? rr.cap2 : 0.f;
+          if constexpr ((SCORE & kBias) != 0) shift = fmaf(-rr.slope2, fabsf(rel - (float)(16 * kb + i)), shift);
+          const float x = s[kb][i];
+          if constexpr ((SCORE & kCap) != 0)
+            s[kb][i] = fmaf(-2.0f * rr.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * rr.cap_in)), shift);
+          else if constexpr ((SCORE & kWideCap) != 0)
+            s[kb][i] = wide_cap(x, rr) + shift;
+          else
+            s[kb][i] = fmaf(x, rr.scale2, shift);
+        }
     }
+    if (at + 64 > lim_lo) {
+      const int seen = rr.lim - at - 4 * g;
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * kb + i >= seen) s[kb][i] = -INFINITY;
+    }
+    const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+    auto weights = [&](float ms) __attribute__((always_inline)) {
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          float e0 = s[kb][2 * w], e1 = s[kb][2 * w + 1];
+          if constexpr (SCORE == 0) {
+            e0 = fmaf(e0, rr.scale2, -ms);
+            e1 = fmaf(e1, rr.scale2, -ms);
+          } else {
+            e0 -= ms;
+            e1 -= ms;
+          }
+          pk[kb][w] = pack_bf16x2(__builtin_amdgcn_exp2f(e0), __builtin_amdgcn_exp2f(e1));
+          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[kb][w]), ones, sum, false);
+        }
+      return sum;
+    };
+    float sum = weights(m);
+    if (__builtin_expect(__ballot(!(sum <= kStageBound)) != 0, 0)) {
+      float mx = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[kb][i]);
+      mx = max_across_rows(mx) * (SCORE == 0 ? rr.scale2 : 1.0f);
+      const bool need = mx > m + kLazyMove;
+      const float alpha = need ? exp2f(m - mx) : 1.0f;
+      if (need) m = mx;
+      l_part *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] *= alpha;
+      sum = weights(m == -INFINITY ? 0.f : m);      // no key seen yet: weights 0
+    }
+    l_part += sum;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       if (half == 1) stage_v(1);
@@ -293,28 +282,23 @@ history_fp4_few(const HistArgs a, int64_t slots) {
         const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (ROCS_LDS i16x4*)(lds3 + (va[1] ^ (32u * db)))));
         const bf16x8 vf = as_bf16x8(u32x4{x[0], x[1], y[0], y[1]});
-#pragma unroll
-        for (int r = 0; r < NR; ++r)
-          o[r][db] = mfma16(vf, as_bf16x8(u32x4{pk[r][2 * half][0], pk[r][2 * half][1],
-                                                pk[r][2 * half + 1][0], pk[r][2 * half + 1][1]}), o[r][db]);
+        o[db] = mfma16(vf, as_bf16x8(u32x4{pk[2 * half][0], pk[2 * half][1], pk[2 * half + 1][0], pk[2 * half + 1][1]}),
+                       o[db]);
       }
     }
     load_v(rows_now);
   }
 
   // This wave's partial softmax into its staging area, 16-byte pieces of a row
-  // swizzled by the row: element i of o[r][db] is O[16 r + l16][16 db + 4 g + i].
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const float l_sum = sum_across_rows(l_part[r]);
-    if (g == 0) {
-      pm[wave][16 * r + l16] = m[r];
-      pl[wave][16 * r + l16] = l_sum;
-    }
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-      *reinterpret_cast<ROCS_LDS f32x4*>(lds3 + st0 + (16 * r + l16) * D * 4 + 16 * ((4 * db + g) ^ l16)) = o[r][db];
+  // swizzled by the row: element i of o[db] is O[l16][16 db + 4 g + i].
+  l_part = sum_across_rows(l_part);
+  if (g == 0) {
+    pm[wave][l16] = m;
+    pl[wave][l16] = l_part;
   }
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+    *reinterpret_cast<ROCS_LDS f32x4*>(lds3 + st0 + l16 * D * 4 + 16 * ((4 * db + g) ^ l16)) = o[db];
   __syncthreads();
   // 16-byte pieces of (head, row); the head's waves are hs, hs + HW, ..
   const int CF = a.D / 4;
@@ -328,7 +312,7 @@ history_fp4_few(const HistArgs a, int64_t slots) {
     for (int w = hs; w < kWaves; w += HW) {
       const float f = exp2f(pm[w][i] - ms);
       l += pl[w][i] * f;
-      y += *reinterpret_cast<const ROCS_LDS f32x4*>(lds3 + w * STAGE + i * D * 4 + 16 * (piece ^ (i & 15))) * f;
+      y += *reinterpret_cast<const ROCS_LDS f32x4*>(lds3 + w * STAGE + i * D * 4 + 16 * (piece ^ i)) * f;
     }
     if (!(finite(y[0]) && finite(y[1]) && finite(y[2]) && finite(y[3])) && may_differ(l, a.D, D)) odd[hs][i] = 1;
     const int rw = t.row0 + i;
@@ -352,31 +336,30 @@ history_fp4_few(const HistArgs a, int64_t slots) {
       redo_row<bf16_t, true>(a, t, t.row0 + i % t.rows, hk0 + i / t.rows, lo, hi, split, direct);
 }
 
-template <int D, int NR>
+template <int D>
 hipError_t launch_few(const HistArgs& a, int64_t slots, int64_t blocks, hipStream_t s) {
   auto go = [&](auto kernel) {
     return launch_kernel(kernel, dim3((uint32_t)blocks), dim3(256), s, a, slots);
   };
   switch (score_of(a)) {
-    case kCap: return go(history_fp4_few<D, kCap, NR>);
-    case kWideCap: return go(history_fp4_few<D, kWideCap, NR>);
-    case kBias: return go(history_fp4_few<D, kBias, NR>);
-    case kCap | kBias: return go(history_fp4_few<D, kCap | kBias, NR>);
-    case kWideCap | kBias: return go(history_fp4_few<D, kWideCap | kBias, NR>);
-    default: return go(history_fp4_few<D, 0, NR>);
+    case kCap: return go(history_fp4_few<D, kCap>);
+    case kWideCap: return go(history_fp4_few<D, kWideCap>);
+    case kBias: return go(history_fp4_few<D, kBias>);
+    case kCap | kBias: return go(history_fp4_few<D, kCap | kBias>);
+    case kWideCap | kBias: return go(history_fp4_few<D, kWideCap | kBias>);
+    default: return go(history_fp4_few<D, 0>);
   }
 }
 
 }  // namespace
 
-hipError_t launch_history_fp4_few(const HistArgs& args, int rows, hipStream_t s) {
+hipError_t launch_history_fp4_few(const HistArgs& args, hipStream_t s) {
   HistArgs a = args;
   set_page_divisor(a);
-  const int64_t slots = a.R + (a.N * a.G + rows - 1) / rows;
+  const int64_t slots = a.R + (a.N * a.G + kFewRows - 1) / kFewRows;
   const int64_t blocks = slots * (a.Hk / a.heads) * a.splits;
   if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-  if (rows == 16) return a.D > 64 ? launch_few<128, 1>(a, slots, blocks, s) : launch_few<64, 1>(a, slots, blocks, s);
-  return a.D > 64 ? launch_few<128, 2>(a, slots, blocks, s) : launch_few<64, 2>(a, slots, blocks, s);
+  return a.D > 64 ? launch_few<128>(a, slots, blocks, s) : launch_few<64>(a, slots, blocks, s);
 }
 
 hipError_t launch_history_fp4_tile(const HistArgs& args, hipStream_t s) {

@@ -79,7 +79,7 @@ inline size_t adapter_t_bytes(int64_t N, int rank) { return ((size_t)N * adapter
 // a row and page_stride = bytes of a page.
 HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16);
 hipError_t launch_history_fp4(const HistArgs& a, int rows, bool bf16, bool fast, hipStream_t s);
-hipError_t launch_history_fp4_few(const HistArgs& a, int rows, hipStream_t s);
+hipError_t launch_history_fp4_few(const HistArgs& a, hipStream_t s);
 hipError_t launch_history_fp4_tile(const HistArgs& a, hipStream_t s);
 
 }  // namespace rocs
