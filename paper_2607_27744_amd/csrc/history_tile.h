@@ -26,7 +26,10 @@
 // A cache in 4 bits (FP4). The stages come through registers instead: a thread
 // takes a block of a key's scale (16 bytes), loaded a step ahead of the LDS slot, and
 // writes it there as bf16, at a step's end. 32 conversions a thread and stage; the
-// rest of the kernel does not know.
+// rest of the kernel does not know. Chunks, 4,003 rows over six histories of 8,300
+// rows on average, 16 heads on 4 x 128: 336 to 391 us by the card, 864 TFLOP/s at best; 6 of 500
+// over 8,000: 272 us, 215 over a cache in bf16. The conversions and the writes to LDS
+// take VALU and LDS cycles that the DMA does not.
 //
 // What bounds it, in long calls: the matrix cores and the VALU together, at a
 // clock that the power holds down (one history of 16,384 rows, 8 heads x 128,

@@ -237,9 +237,12 @@ hipError_t launch_request(const LinearArgs& a, int cus, int tiles_d, int req_til
 // ADAPT: the low-rank adapters of the rows' requests (adapter.hip) as further columns
 // of K, with operands straight from global memory: B_a's rows and t's. A block
 // of 32 rows takes the adapters that its rows have one after the other, with t
-// zero for the others' rows. Rows behind the last request are not stored.
+// zero for the others' rows. Rows behind the last request are not stored. Bound by the
+// latency of those operands where a tile has many adapters (2,000 rows of 250 requests,
+// 1,024 -> 1,536, rank 16, of 64: 25 us with t; of 24 requests: 24), else as below.
 // SHRINK: t itself: W is the adapter A_a of the tile's request, tiles do not straddle two,
-// and the rows' adapters are written beside it.
+// and the rows' adapters are written beside it. Bound by the read of x: 32,768 rows, K
+// 2,048, rank 64: 33 us, 4.1 TB/s; 9,001, K 1,024, rank 32: 8.3.
 //
 // What bounds it: reads of the two operands through L2 (each 128 x 128 tile
 // reads 256 rows of K) and the output stores; the slab depth, the request rows
@@ -618,7 +621,10 @@ void ikbo_gemm_tile(
 // steps after the tile's last, operands (B_a's rows and t's) straight from global memory.
 // Tiles cover the rows contiguously (in tiles that end with a request, 16 ragged
 // histories of 32,768 rows would take five rounds of the chip for four): a wave takes
-// the adapters of its 128 rows one by one, with t zero for the others' rows.
+// the adapters of its 128 rows one by one, with t zero for the others' rows. 32,768 rows of
+// 16 requests, 2,048 -> 2,048, rank 64: 245 to 289 us by the card, 980 to 1,160 TFLOP/s of the
+// projection and B, bound as without them (a large bf16 product on that card: 1,140); 24,000 rows of 12,000
+// requests, 512 -> 1,024, rank 16, of 64 adapters, 185 with t: there by the loop over a wave's 64 adapters.
 //
 // Rows past the tile's end are clamped loads whose results are not stored.
 // ---------------------------------------------------------------------------
