@@ -279,8 +279,11 @@ def adapted_step(p, slots, adapter_ids, s_new, offsets, e_c, cand_offsets, max_k
     adapter adapter_ids[r] (none if it is out of range). Its new events are projected with the adapter
     beside the shared weights, turned by their positions and appended, and attend over the whole
     history; its candidates stand one position behind the history's end and attend over all of it.
-    Returns {"events", "candidates", "status"}; see ops.cache_check for the status."""
+    Returns {"events", "candidates", "status"}; see ops.cache_check for the status (a slot out of range
+    is one of its errors; the reads of the cache clamp it)."""
     m, n, h, hk, d = s_new.shape[0], e_c.shape[0], p.h, p.hk, p.d
+    if cand_offsets.numel() != slots.numel() + 1:
+        raise ValueError("cand_offsets needs an entry for each slot and one more")
     qkv = ops.adapter_linear(s_new, p.wqkv, p.a, p.b, offsets, adapter_ids, scales=p.scales)
     q, k, v = (x.unflatten(1, (-1, d)) for x in qkv.split([h * d, hk * d, hk * d], dim=1))
     rows, status = ops.cache_reserve(slots, offsets, m, p.table, p.lens, p.refs, p.page)
@@ -288,7 +291,9 @@ def adapted_step(p, slots, adapter_ids, s_new, offsets, e_c, cand_offsets, max_k
                          lens=p.lens)
     events = ops.paged_attention_fp4(q, p.pool[0], p.table, p.lens, offsets, kv_heads=hk, slots=slots,
                                      max_kv_len=max_kv_len)
-    ends = p.lens[slots.long()][ops.request_ids(cand_offsets, n).long()]
+    # torch's lookups do not clamp as the cache's operators do: an index out of range ends the process.
+    ends = p.lens.index_select(0, slots.clamp(0, p.lens.numel() - 1))
+    ends = ends.index_select(0, ops.request_ids(cand_offsets, n))
     q_c = ops.rotate(ops.ikbo_linear(e_c, p.wq_c).view(n, h, d), p.freqs, positions=ends)
     cands = ops.paged_attention_fp4(q_c, p.pool[0], p.table, p.lens, cand_offsets, kv_heads=hk,
                                     slots=slots, causal=False, max_kv_len=max_kv_len)

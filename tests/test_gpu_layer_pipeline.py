@@ -98,6 +98,22 @@ def test_a_step_that_finds_no_pages_leaves_the_cache(gpu_lib):
     assert all(torch.equal(x, y) for x, y in zip(kept, (p.pool, p.table, p.lens, p.refs)))
 
 
+@pytest.mark.parametrize("bad", [2, 99, -1, -3])
+def test_a_step_with_a_slot_out_of_range(gpu_lib, bad):
+    # The status says so, the cache is unchanged, and what torch looks up stays within it.
+    w = wl.history_case([2, 2], [[20, 30], [40, 60]], kv_heads=1, head_dim=64)
+    p = pipelines.prepare_adapted_cache(w, wl.adapters_of(w, 2, 8), pages=20, page_size=16, table_width=8)
+    first, second = w.batches
+    call = lambda b, slots: pipelines.adapted_step(  # noqa: E731
+        p, dev_i32(slots), dev_i32([0, 1]), dev_bf16(b.s), dev_i32(b.offsets), dev_bf16(b.e_c),
+        dev_i32(b.cand_offsets))
+    ops.cache_check(call(first, [1, 0])["status"])
+    kept = [x.clone() for x in (p.pool, p.table, p.lens, p.refs)]
+    with pytest.raises(ops.RocsError, match="out of range"):
+        ops.cache_check(call(second, [1, bad])["status"])
+    assert all(torch.equal(x, y) for x, y in zip(kept, (p.pool, p.table, p.lens, p.refs)))
+
+
 def test_a_step_in_a_graph(gpu_lib):
     # The whole step captured, replayed for the next batch's events beside eager work.
     w = wl.history_case([5, 3], [[70, 40], [1, 1], [1, 1], [1, 1]], kv_heads=2, head_dim=64)
