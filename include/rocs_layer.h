@@ -42,7 +42,8 @@ extern "C" {
  * cases run a general kernel (fp32 matrix instructions).
  * An infinity or NaN in one request's rows or adapter does not reach another's; where
  * one stands in B, the rows that share its tiles of 32 are formed again by a slow path.
- * Limits: rank <= 256; K, D < 2^22; R + N / 32 < 2^23 and N / 128 * D / 128 < 2^24.
+ * Limits: rank <= 256; K, D < 2^22; R + ceil(N / 32) < 2^23 and ceil(N / 128) *
+ * ceil(D / 128) < 2^24.
  * ---------------------------------------------------------------------------
  */
 size_t rocs_adapter_workspace_size(int64_t num_requests, int64_t num_rows, int64_t k, int64_t d_out,

@@ -336,8 +336,8 @@ hipError_t launch_adapter(const AdapterArgs& a, bool fast, hipStream_t s) {
   // whole call in us, shrink_rows / tiled; K x D, rank): 9,001 rows of 24 requests,
   // 1,024 x 1,536, 32: 45 / 41; 32,768 of 16, 2,048 x 2,048, 64: 316 / 285; 8,000 of 400,
   // 1,024 x 1,024, 64: 59 / 51; 1,024 of 64, 64: 24 / 22; but 4,096 of 256, 16: 29 / 30; 2,048 of
-  // 128, 32: 30 / 32; 8,000 of 1,000, 16: 49 / 51.
-  const bool tiled = a.N / a.R >= 16 && a.N >= (a.rank > 32 ? 1024 : 8000);
+  // 128, 32: 30 / 32; 8,000 of 1,000, 16: 49 / 51. A grid of shrink_rows holds whatever the limits allow.
+  const bool tiled = a.N / a.R >= 16 && a.N >= (a.rank > 32 ? 1024 : 8000) && adapter_shrink_fits(a);
   const hipError_t e = tiled          ? launch_adapter_shrink(a, lr, s)
                        : a.rank > 32 ? launch_shrink<2>(a, lr, s)
                                      : launch_shrink<1>(a, lr, s);

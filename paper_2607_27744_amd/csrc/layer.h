@@ -70,6 +70,8 @@ struct LowRank {
   int64_t x_stride;
   int cols, rank, adapters, R;
 };
+// Whether the tiled kernel's grid, which grows with the rank, holds the call.
+bool adapter_shrink_fits(const AdapterArgs& a);
 hipError_t launch_adapter_shrink(const AdapterArgs& a, const LowRank& lr, hipStream_t s);
 hipError_t launch_adapter_gemm(const AdapterArgs& a, const LowRank& lr, hipStream_t s);
 // Bytes of t in the workspace; the rows' adapters [N] lie behind them on the fast path.

@@ -102,7 +102,7 @@ int32_t rocs_adapter_linear(const void* x, int64_t x_row_stride, const void* w, 
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: a size is out of range", name);
   if (rank > 256) return fail(ROCS_ERR_UNSUPPORTED, "%s: rank %d > 256", name, rank);
   if (R > kMaxI32 || N > kMaxI32 || K >= (1 << 22) || D >= (1 << 22) || num_adapters > kMaxI32 ||
-      R + N / 32 >= (1 << 23) - 1 || (N / 128 + 1) * (D / 128 + 1) >= (1 << 24) || x_row_stride > (int64_t(1) << 31))
+      R + (N + 31) / 32 >= (1 << 23) || (N + 127) / 128 * ((D + 127) / 128) >= (1 << 24) || x_row_stride > (int64_t(1) << 31))
     return fail(ROCS_ERR_UNSUPPORTED, "%s: batch too large", name);
   if (x_row_stride != 0 && x_row_stride < K)
     return fail(ROCS_ERR_INVALID_ARGUMENT, "%s: x_row_stride < K", name);

@@ -1492,19 +1492,26 @@ hipError_t launch_linear(const LinearArgs& a, bool fast, hipStream_t s) {
   return small ? launch_tile<64, 64, 64, 3, false>(a, s) : launch_tile<128, 128, 32, 3, false>(a, s);
 }
 
-// t of an adapter call, and the rows' adapters.
+// t of an adapter call, and the rows' adapters: tiles of BM columns of t by BN rows.
 template <int BM, int BN, int WVM>
-static hipError_t launch_shrink_tile(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
-  const int tiles_m = (a.rank + BM - 1) / BM;
-  const int64_t grid = tiles_m * (a.R + (a.N + BN - 1) / BN);
-  if (!grid_fits(grid, 256)) return hipErrorInvalidConfiguration;
-  return launch_kernel(ikbo_gemm_tile<BM, BN, 64, 3, false, WVM, false, true>, dim3((uint32_t)grid), dim3(256), s,
-                       static_cast<const bf16_t*>(a.x), static_cast<const bf16_t*>(nullptr),
-                       static_cast<const bf16_t*>(a.a), a.scales, a.ids, const_cast<bf16_t*>(lr.t), a.N, a.K, a.rank,
-                       tiles_m, 0, 1, lr);
+struct ShrinkTile {
+  static int tiles_m(const AdapterArgs& a) { return (a.rank + BM - 1) / BM; }
+  static int64_t grid(const AdapterArgs& a) { return tiles_m(a) * (a.R + (a.N + BN - 1) / BN); }
+  static hipError_t launch(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
+    if (!grid_fits(grid(a), 256)) return hipErrorInvalidConfiguration;
+    return launch_kernel(ikbo_gemm_tile<BM, BN, 64, 3, false, WVM, false, true>, dim3((uint32_t)grid(a)), dim3(256), s,
+                         static_cast<const bf16_t*>(a.x), static_cast<const bf16_t*>(nullptr),
+                         static_cast<const bf16_t*>(a.a), a.scales, a.ids, const_cast<bf16_t*>(lr.t), a.N, a.K, a.rank,
+                         tiles_m(a), 0, 1, lr);
+  }
+};
+using ShrinkNarrow = ShrinkTile<32, 128, 1>;     // ranks up to 32
+using ShrinkWide = ShrinkTile<64, 64, 2>;
+bool adapter_shrink_fits(const AdapterArgs& a) {
+  return grid_fits(a.rank <= 32 ? ShrinkNarrow::grid(a) : ShrinkWide::grid(a), 256);
 }
 hipError_t launch_adapter_shrink(const AdapterArgs& a, const LowRank& lr, hipStream_t s) {
-  return a.rank <= 32 ? launch_shrink_tile<32, 128, 1>(a, lr, s) : launch_shrink_tile<64, 64, 2>(a, lr, s);
+  return a.rank <= 32 ? ShrinkNarrow::launch(a, lr, s) : ShrinkWide::launch(a, lr, s);
 }
 
 // The projection of an adapter call, with t and the rows' adapters formed.

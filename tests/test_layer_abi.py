@@ -71,6 +71,30 @@ def test_adapter_refusals(lib, bad, status):
     assert (lib.rocs_last_error_message() == b"") == (status == _lib.OK)
 
 
+@no_gpu
+@pytest.mark.parametrize("n, r, rank, k, d", [
+    (80_000_000, 5_000_000, 136, 8, 4), (80_000_000, 5_000_000, 256, 8, 4), (88_000_000, 5_500_000, 200, 16, 8),
+    (80_000_000, 5_000_000, 64, 8, 4), (80_000_000, 5_000_000, 32, 8, 4), (250_000_000, 1, 256, 8, 4),
+    (1, (1 << 23) - 2, 256, 8, 4), ((1 << 28) - 64, 1, 16, 8, 4), (1 << 26, 64, 16, 8, 31 * 128), (8_000, 500, 16, 8, 4)])
+def test_adapter_sizes_within_the_limits_are_launched(lib, n, r, rank, k, d):
+    # Calls that the limits allow fit a launch's grid: they fail here for want of a GPU alone.
+    far = [P((i + 1) << 44) for i in range(8)]
+    need = lib.rocs_adapter_workspace_size(r, n, k, d, rank, 1)
+    assert _adapter(lib, x=far[0], w=far[1], a=far[2], b=far[3], off=far[4], ids=far[5], out=far[6], ws=far[7],
+                    R=r, N=n, K=k, D=d, rank=rank, ws_bytes=need) not in (_lib.OK, BAD, UNS)
+    assert b"grid" not in lib.rocs_last_error_message()
+
+
+@no_gpu
+@pytest.mark.parametrize("sizes", [dict(N=(1 << 28) - 63), dict(N=(1 << 28) - 32, R=1), dict(N=33, R=(1 << 23) - 2),
+                                   dict(N=1 << 26, D=32 * 128), dict(N=(1 << 26) - 127, D=31 * 128 + 1)])
+def test_adapter_sizes_past_the_limits(lib, sizes):
+    far = [P((i + 1) << 44) for i in range(8)]
+    assert _adapter(lib, x=far[0], w=far[1], a=far[2], b=far[3], off=far[4], ids=far[5], out=far[6], ws=far[7],
+                    ws_bytes=1 << 42, **sizes) == UNS
+    assert b"batch too large" in lib.rocs_last_error_message()
+
+
 def _append(lib, **kw):
     a = dict(q=FAKE[0], qs=0, k=FAKE[1], v=FAKE[2], ks=0, rows=FAKE[3], freqs=FAKE[4], rot=64, inter=0,
              pos=None, off=FAKE[5], slots=FAKE[6], lens=FAKE[7], R=2, S=4, M=8, H=4, Hk=2, D=64, dtype=1,
