@@ -397,8 +397,12 @@ void ikbo_gemm_tile(
       for (int q = 0; q < 4; ++q) {
         const int d = m0 + wm0 + 32 * fm + 8 * q + 4 * hh;
         zv[fn % ZFN][fm][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (!SHRINK && z != nullptr && d < D)
-          zv[fn % ZFN][fm][q] = *reinterpret_cast<const f32x4*>(z + (int64_t)rq[fn] * D + d);
+        if (!SHRINK && z != nullptr && d < D) {
+          typedef f32x4 f32x4u __attribute__((aligned(4)));
+          const float* zr = z + (int64_t)rq[fn] * D + d;
+          if constexpr (ADAPT) zv[fn % ZFN][fm][q] = *reinterpret_cast<const f32x4u*>(zr);   // a bias at any float
+          else zv[fn % ZFN][fm][q] = *reinterpret_cast<const f32x4*>(zr);
+        }
       }
   };
   if constexpr (!ZLATE) {

@@ -115,6 +115,17 @@ def test_strided_rows_and_a_padded_batch(gpu_lib, dtype, k):
         assert torch.all(out[54:] == 7.0)
 
 
+@pytest.mark.parametrize("n, k, d", [(60, 64, 72), (700, 128, 1024), (1500, 128, 1028), (8100, 256, 2048), (9, 7, 3)])
+def test_a_bias_that_starts_at_any_float(gpu_lib, n, k, d):
+    # The few-rows, tiled, streaming and general kernels.
+    counts, ids = [n // 2, n - n // 2], [1, 0]
+    c, kw = make(counts, ids, k, d, 8, 2, BF, seed=n)
+    wide = torch.randn(d + 3, generator=torch.Generator().manual_seed(n)).cuda()
+    for lo in (1, 2, 3):
+        kw["bias"] = wide[lo:lo + d]
+        check(c, kw, counts, ids, ops.adapter_linear(**c, **kw))
+
+
 def test_rows_without_an_adapter_are_the_projection(gpu_lib):
     # The same rows in a call with adapters and one without: rows of no adapter have the same bits.
     for n, k, d in ((40, 256, 192), (900, 512, 256), (2000, 128, 1024), (8001, 256, 2048)):
