@@ -1,8 +1,9 @@
 // Device side of the cache's 4-bit form (layer.h: Fp4Row): e2m1 values with a
 // power-of-two scale (a byte of exponent) for 32 of them. The conversion
 // instructions take the scale as the exponent of a float: 2^(E - 127) is the bits
-// E << 23, and E = 255 makes NaN of every value (checked on the card, as is that
-// the rounding is to the nearest, ties to the even code, saturating at 6).
+// E << 23, E = 0 (a float of zero) is 2^-127, and E = 255 makes NaN of every value
+// (checked on the card, as is that the rounding is to the nearest, ties to the even
+// code, saturating at 6).
 #pragma once
 
 #include "common.h"

@@ -115,6 +115,29 @@ def test_strided_rows_and_a_padded_batch(gpu_lib, dtype, k):
         assert torch.all(out[54:] == 7.0)
 
 
+@pytest.mark.parametrize("n, k, d, rank", [(1500, 128, 1024, 16), (1500, 128, 1028, 40), (8100, 256, 2048, 16),
+                                           (8100, 256, 2020, 24), (8100, 256, 2048, 72), (700, 128, 900, 16)])
+def test_strides_and_padding_of_large_batches(gpu_lib, n, k, d, rank):
+    # Either product for t, the tiled and the streaming kernel; whole tiles behind the last request.
+    counts, ids = [n // 3, 0, 1, n - n // 3 - 1], [1, 0, -1, 0]
+    for stride, pad in ((8, 0), (0, 700), (64, 13)):
+        c, kw = make(counts, ids, k, d, rank, 2, BF, seed=rank, pad=pad, stride=stride)
+        if pad:
+            c["x"][n:] = float("nan")
+        out = torch.full((n + pad, d), 7.0, dtype=BF, device="cuda")
+        ops.adapter_linear(**c, **kw, out=out)
+        check(c, kw, counts, ids, out)
+        assert torch.all(out[n:] == 7.0)
+
+
+@pytest.mark.parametrize("n, k, d, rank", [(40, 64, 72, 8), (1500, 128, 1024, 40), (8100, 256, 2048, 16), (40, 60, 72, 5)])
+def test_a_batch_of_padding_alone(gpu_lib, n, k, d, rank):
+    c, kw = make([0, 0], [1, 0], k, d, rank, 2, BF, pad=n)
+    out = torch.full((n, d), 7.0, dtype=BF, device="cuda")
+    ops.adapter_linear(**c, **kw, out=out)
+    assert torch.all(out == 7.0)
+
+
 @pytest.mark.parametrize("n, k, d", [(60, 64, 72), (700, 128, 1024), (1500, 128, 1028), (8100, 256, 2048), (9, 7, 3)])
 def test_a_bias_that_starts_at_any_float(gpu_lib, n, k, d):
     # The few-rows, tiled, streaming and general kernels.

@@ -162,6 +162,101 @@ def test_scales_of_any_size(gpu_lib):
         check(ops.paged_attention_fp4(**call), *want, 100, dtype == BF)
 
 
+def held(call, hk, d, kv_len):
+    """K and V of the packed histories as the call's pages hold them."""
+    raw, page = call["pages"].cpu().numpy(), call["pages"].shape[1]
+    table = call["page_table"].cpu().numpy()
+    rows = [raw[table[s, :-(-n // page)]].reshape(-1, raw.shape[2])[:n] for s, n in zip(call["slots"].tolist(), kv_len)]
+    kv = layer.unpack(np.concatenate(rows), hk, d)
+    return kv[:, 0], kv[:, 1]
+
+
+KERNELS = [  # dtype, H, H_kv, d, query rows, history rows: few rows, tiles, and the general kernel
+    (BF, 4, 2, 128, [1, 3], [300, 60]), (BF, 8, 1, 64, [1, 1], [1500, 33]), (BF, 2, 1, 96, [1, 9], [99, 40]),
+    (BF, 2, 1, 128, [40, 90], [700, 90]), (BF, 2, 2, 64, [130, 65], [200, 65]), (BF, 2, 1, 96, [50, 40], [333, 40]),
+    (BF, 2, 1, 256, [1, 30], [70, 200]), (F32, 4, 2, 64, [1, 30], [400, 90]), (F32, 1, 1, 224, [4], [70])]
+kernels = pytest.mark.parametrize("dtype, h, hk, d, q_len, kv_len", KERNELS,
+                                  ids=lambda v: str(v)[6:] if isinstance(v, torch.dtype) else str(v))
+
+
+@kernels
+def test_scale_bytes_of_zero(gpu_lib, dtype, h, hk, d, q_len, kv_len):
+    # E = 0 is 2^-127: K under queries of 2^124, then V. What is below 2^-126 has steps of 2^-133 in
+    # bf16, of which a rounding is off by half.
+    call, k, v = make(dtype, h, hk, d, q_len, kv_len, 16, seed=d)
+    raw = call["pages"].cpu().numpy()
+    at, n = hk * d, hk * d // 32
+    low = raw.copy()
+    low[..., at:at + n] = 0
+    small = {**call, "pages": torch.from_numpy(low).cuda(), "q": call["q"] * 2.0 ** 124}
+    want = oracle.attention(_np(small["q"]), held(small, hk, d, kv_len)[0], v, q_len, kv_len, scale=1.0)
+    check(ops.paged_attention_fp4(**small, scale=1.0), *want, max(kv_len), dtype == BF)
+    low = raw.copy()
+    low[..., at + n:at + 2 * n] = 0
+    small = {**call, "pages": torch.from_numpy(low).cuda()}
+    got = _np(ops.paged_attention_fp4(**small)) * 2.0 ** 127
+    want, mean, err = oracle.attention(_np(call["q"]), k, held(small, hk, d, kv_len)[1] * 2.0 ** 127, q_len, kv_len)
+    step = 2.0 ** -8 if dtype == BF else 0.0
+    longest = max(kv_len)
+    tol = mean * (2 * err[..., None] + 2 * step + (2 * longest + 64) * oracle.U32) + longest * 2.0 ** -22
+    tol = tol + (step if dtype == BF else oracle.U32) * (np.abs(want) + tol) + (2.0 ** -7 if dtype == BF else 0.0)
+    off = np.abs(got - want)
+    assert np.all(off <= tol), (off.max(), np.abs(want).max(), np.abs(got).max())
+
+
+def test_every_scale_byte_reads_back(gpu_lib):
+    # All codes under all scales, 255 among them: a value is what the form says, exactly.
+    hk, d = 2, 128
+    rows = np.zeros((256, layer.row_bytes(hk, d)), np.uint8)
+    pair = np.arange(hk * d, dtype=np.uint8)
+    rows[:, :hk * d] = (pair % 16) | ((pair // 16) << 4)
+    rows[:, hk * d:hk * d + hk * d // 16] = np.arange(256)[:, None]
+    pool = torch.from_numpy(rows.reshape(16, 16, -1)).cuda()
+    at = dev_i32(np.arange(256))
+    want = layer.unpack(rows, hk, d)
+    exact = np.abs(want) < 2.0 ** 128                      # past that the types have no value
+    for dtype in (BF, F32):
+        got = _np(ops.cache_read_fp4(at, pool, hk, d, dtype=dtype))
+        assert np.array_equal(got[exact], want[exact]) and np.all(np.isnan(got[255]))
+        assert np.array_equal(np.signbit(got[exact]), np.signbit(want[exact]))
+
+
+@kernels
+def test_nan_and_infinite_queries_stay_by_themselves(gpu_lib, dtype, h, hk, d, q_len, kv_len):
+    # One head of a row NaN; one at minus infinity in a dim where its keys are positive (no key has
+    # weight: zeros).
+    call, _, v = make(dtype, h, hk, d, q_len, kv_len, 16, seed=d + 1)
+    raw = call["pages"].cpu().numpy()
+    dim = d - 3
+    raw[..., dim // 2] = (raw[..., dim // 2] & 0x0f) | 0x20 if dim % 2 else (raw[..., dim // 2] & 0xf0) | 0x02
+    call["pages"] = torch.from_numpy(raw).cuda()
+    k = held(call, hk, d, kv_len)[0]
+    want, mean, err = oracle.attention(_np(call["q"]), k, v, q_len, kv_len)
+    for value, there in ((float("nan"), np.isnan), (-float("inf"), lambda x: x == 0)):
+        q = call["q"].clone()
+        row = sum(q_len) - 1
+        q[row, 0, dim] = value                              # head 0 reads K/V head 0
+        got = ops.paged_attention_fp4(**{**call, "q": q})
+        assert np.all(there(_np(got)[row, 0]))
+        got[row, 0] = torch.from_numpy(want[row, 0]).to(got)
+        check(got, want, mean, err, max(kv_len), dtype == BF)
+
+
+@pytest.mark.parametrize("h, hk, d, q_len, kv_len", [
+    (8, 8, 64, [1] * 24, [6000, 3] + [50] * 22), (8, 4, 128, [1, 2, 1], [6000, 1, 900]),
+    (2, 1, 64, [70, 33], [5000, 90]), (2, 2, 96, [1, 3], [5000, 70])])
+def test_unaligned_queries_over_split_histories(gpu_lib, h, hk, d, q_len, kv_len):
+    # bf16 queries off 16 bytes, or off 16 bytes a row: the general kernel under the other kernels' plans.
+    call, k, v = make(BF, h, hk, d, q_len, kv_len, 16, seed=h + d)
+    n = sum(q_len)
+    assert ops.paged_fp4_workspace_size(len(q_len), n, h, hk, d, max(kv_len), BF) > 0
+    for lo, pad in ((1, 7), (4, 0), (0, 5)):
+        wide = torch.randn(n, h * d + lo + pad, device="cuda").to(BF)
+        q = wide[:, lo:lo + h * d].unflatten(1, (h, d))
+        got = ops.paged_attention_fp4(**{**call, "q": q}, max_kv_len=max(kv_len))
+        check(got, *oracle.attention(_np(q), k, v, q_len, kv_len), max(kv_len), True)
+
+
 @pytest.mark.parametrize("dtype, h, hk, d, rows", [(BF, 4, 2, 128, 1), (BF, 8, 1, 64, 3), (BF, 2, 2, 64, 80),
                                                    (BF, 2, 1, 96, 40), (F32, 4, 2, 64, 5)])
 def test_nan_blocks_reach_only_the_rows_that_see_them(gpu_lib, dtype, h, hk, d, rows):

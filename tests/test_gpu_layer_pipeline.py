@@ -84,6 +84,32 @@ def test_ranking_with_adapters_over_four_bits(gpu_lib, head_dim, kv_heads, page)
             slot_of[2] = 7
 
 
+def test_pages_copied_between_pools(gpu_lib):
+    # Rows appended to one cache are read and attended to from another that its pages are copied to.
+    g = torch.Generator().manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, generator=g).cuda().bfloat16()   # noqa: E731
+    src, table, lens, refs = ops.cache_pool_fp4(2, 9, 16, 2, 64, slots=1, table_width=6)
+    off = dev_i32([0, 70])
+    rows, status = ops.cache_reserve(dev_i32([0]), off, 70, table, lens, refs, 16)
+    ops.cache_check(status)
+    for one in range(2):
+        ops.cache_append(rnd(70, 2, 64), rnd(70, 2, 64), rows, src[one])
+    dst = torch.full((2, 12, *src.shape[2:]), 255, dtype=torch.uint8, device="cuda")
+    to = dev_i32([11, 0, 7, 3, 5])
+    ops.cache_copy(table[0, :5].contiguous(), to, src, dst)
+    there = torch.full_like(table, -1)
+    there[0, :5] = to
+    j = torch.arange(70, device="cuda")
+    moved = (to[j // 16] * 16 + j % 16).int()
+    q = rnd(3, 4, 64)
+    for one in range(2):
+        assert torch.equal(ops.cache_read_fp4(rows, src[one], 2, 64), ops.cache_read_fp4(moved, dst[one], 2, 64))
+        call = lambda pool, t: ops.paged_attention_fp4(q, pool, t, lens, dev_i32([0, 3]), kv_heads=2)   # noqa: E731
+        assert torch.equal(call(src[one], table), call(dst[one], there))
+    rest = [p for p in range(12) if p not in to.tolist()]
+    assert torch.all(dst[:, rest] == 255)
+
+
 def test_a_step_that_finds_no_pages_leaves_the_cache(gpu_lib):
     w = wl.history_case([2, 2], [[20, 30], [40, 60]], kv_heads=1, head_dim=64)
     p = pipelines.prepare_adapted_cache(w, wl.adapters_of(w, 2, 8), pages=4, page_size=16, table_width=8)
