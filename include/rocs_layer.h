@@ -97,9 +97,13 @@ int32_t rocs_adapter_linear(const void* x, int64_t x_row_stride, const void* w, 
  * padded to a multiple of 16 bytes (padding is not written). Written rows have
  *   E - 127 = floor(log2 m) - 2, or 1 more where m / 2^that > 7, in -126 .. 125,
  * of the block's largest magnitude m; values are rounded to the nearest, ties to
- * the even code, magnitudes past 6 to 6. So a value is off by at most 2^(E -
- * 127), at most 1/3.5 of the block's largest. A block that holds an infinity or
- * NaN gets E = 255 and reads as NaN, all of it.
+ * the even code, magnitudes past 6 to 6. So for m from 3.5 * 2^-126 to 7 * 2^125 a
+ * value is off by at most 2^(E - 127), at most m / 3.5. Past that, where E stays at
+ * its limit: magnitudes above 6 * 2^125 become 6 * 2^125, less than 2^126 off (m / 4);
+ * with a smaller m a value is off by at most 2^-127, and up to 2^-128 it becomes
+ * zero. A block that holds an infinity or NaN gets E = 255 and reads as NaN, all of
+ * it. (Bytes from elsewhere: E = 0 is 2^-127; 4 and 6 under E = 253, and 2 and more
+ * under 254, pass the types' range and have no defined reading.)
  * ---------------------------------------------------------------------------
  */
 #define ROCS_POOL_ROWS 0

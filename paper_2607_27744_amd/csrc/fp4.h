@@ -30,7 +30,8 @@ __device__ __forceinline__ float fp4_value(uint32_t w, int j, float scale) {
 
 // The scale byte of a block whose largest magnitude is m: the exponent that
 // puts m in [4, 8), one more where m would pass 7 (nearer to 8 than to 6: kept
-// at 6 it would be off by more than half the form's largest step).
+// at 6 it would be off by more than half the form's largest step). Kept within
+// 1 .. 252: below, m is the smaller for it; above, values saturate at 6.
 __device__ __forceinline__ uint32_t fp4_exponent(float m) {
   const uint32_t b = __builtin_bit_cast(uint32_t, m) & 0x7fffffffu;
   if (b >= 0x7f800000u) return 255u;

@@ -33,6 +33,23 @@ def test_a_value_is_off_by_at_most_the_scale():
     assert np.all(off.max(-1) <= most / 3.5)
 
 
+def test_rounding_outside_the_scales():
+    # Above 7 x 2^125 the scale stays at 2^125 and values saturate, less than 2^126 off; below
+    # 3.5 x 2^-126 it stays at 2^-126 and a value is off by at most 2^-127, up to 2^-128 all of it.
+    for top, bound in ((7.0, 2.0 ** 125), (7.01, 2.0 ** 126), (7.999, 2.0 ** 126)):
+        x = np.linspace(-top, top, 32)[None] * 2.0 ** 125
+        codes, scale = layer.quantise(x)
+        y = layer.values(codes, scale)
+        assert scale[0, 0] == 252 and np.abs(y).max() == 6 * 2.0 ** 125
+        assert np.abs(y - x).max() <= bound and np.abs(y - x).max() <= np.abs(x).max() / 3.5
+    for top in (3.49, 2.0, 0.3, 0.25, 0.1, 2.0 ** -23):
+        x = np.linspace(-top, top, 32)[None] * 2.0 ** -126
+        codes, scale = layer.quantise(x)
+        y = layer.values(codes, scale)
+        assert scale[0, 0] == 1 and np.abs(y - x).max() <= 2.0 ** -127
+        assert np.array_equal(y == 0, np.abs(x) <= 2.0 ** -128)
+
+
 def test_an_odd_value_makes_its_block_nan():
     for bad in (np.nan, np.inf, -np.inf):
         x = np.ones((1, 2, 1, 64))
