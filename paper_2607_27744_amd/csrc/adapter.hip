@@ -347,7 +347,8 @@ hipError_t launch_adapter(const AdapterArgs& a, bool fast, hipStream_t s) {
   // adapter_few: 128 rows, 1,024 x 1,024, rank 16, one adapter 16.7 / 15.4, a row each of 30
   // 20.7 / 13.2 (32 tiles); 192 rows, 1,024 x 2,048 (96 tiles), 17.5 / 20.7, a row each of 8
   // 16.6 / 18.6, of 64 23.6 / 19.3; 256 rows, 2,048 x 2,048, rank 64, of 64 (128 tiles) 71 / 53; 512 rows,
-  // rank 16, of 64 (256 tiles) 34 / 51.
+  // rank 16, of 64 (256 tiles) 34 / 51. (Both rules go by averages: 127 single rows of 64 adapters and a
+  // chunk of 4,000, 1,024 x 1,536, rank 16, take 58 as one call, 12 + 31 as two.)
   const int64_t tiles = (int64_t)((a.N + 63) / 64) * ((a.D + 63) / 64);
   const bool few = tiles <= 64 || (tiles <= 128 && a.N < 4 * (int64_t)a.R && a.A >= 16);
   return few ? launch_few(a, lr, s) : launch_adapter_gemm(a, lr, s);

@@ -13,11 +13,11 @@
 // bits and rounded once, products and their sum rounded each (no multiply-add), so
 // that a row gets the same codes in 4 bits in every layout of the call.
 // What bounds it: HBM where rows are many: 32,771 rows, 8 query and 8 + 8 heads x 128,
-// into 4 bits: 83 us, 3.7 TB/s of the rows' bytes in and out (a large copy: 5.2); 12,007
-// rows, 16 + 4 + 4 heads x 64, in bf16 16.1 us, in fp32 34 (4.3 TB/s). There eight rows a workgroup,
-// each thread keeping its piece of a head over the rows: 83 us; walking the rows two or
-// four at a time 87; sixteen rows 101; four pieces in flight a thread 96. For single
-// events the launch and the chain lens -> position -> angle: 128 rows 4.8 us.
+// into 4 bits: 73 to 83 us by the card, 3.7 to 4.2 TB/s of the rows' bytes in and out (a large
+// copy: 5.2); 12,007 rows, 16 + 4 + 4 heads x 64, in bf16 16.1 us, in fp32 34 (4.3 TB/s). A thread
+// keeps its piece of a head over the workgroup's rows: where that took 83 us, walking them two
+// or four at a time took 87, four pieces in flight a thread 96, sixteen rows 101. For
+// single events the launch and the chain lens -> position -> angle: 128 rows 4.8 us.
 #include "fp4.h"
 #include "launch.h"
 
@@ -263,8 +263,10 @@ template <typename T>
 hipError_t launch_rows(const AppendArgs& a, hipStream_t s) {
   const int heads = (a.q != nullptr ? a.H : 0) + (a.k != nullptr ? 2 * a.Hk : 0);
   if (heads == 0) return hipSuccess;
-  // Rows a workgroup: a thousand pieces and more, while the rows make two
-  // workgroups a CU.
+  // Rows a workgroup: up to a thousand pieces and more, while the rows make two
+  // workgroups a CU. In us, by this rule / eight rows wherever there are enough: 32,771 rows of 384
+  // pieces (four rows) into 4 bits 73 / 75, into a bf16 pool 85.5 / 92.5; 8,003 of 768 (two
+  // rows) 42 / 49; 12,007 of 192 takes eight by both.
   int64_t rb = 1;
   while (rb < kMaxRb && rb * heads * ((a.D + 7) / 8) < 1024 && a.M / (2 * rb) >= 512) rb *= 2;
   const int64_t blocks = (a.M + rb - 1) / rb;

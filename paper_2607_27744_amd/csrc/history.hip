@@ -520,8 +520,11 @@ hipError_t launch_history(const HistArgs& a, int rows, bool bf16, bool fast, hip
 // few / tiles, 8 heads on 2 x 128, by the rows of a request and head: 64 requests over 3,125 keys
 // 16: 41 / 56, 24: 47 / 54, 32: 55 / 48, 40: 63 / 54, 64: 90 / 57; 128 requests 32: 92 / 113, 40: 107 / 109,
 // 48: 121 / 113; 8 on 8 x 64, 64 requests, 32: 105 / 133, 48: 133 / 122; one history of 8,000 rows 14 / 14
-// throughout. The cut of few rows is that of history_plan, with chunks of 512 keys in either
-// case: 128 single rows over 3,125 keys, 8 heads x 128: by four heads a workgroup 129 us, two 136,
+// throughout. Where one or two K/V heads leave the tiles' grid small already, they win from about 28
+// rows on: one row of 32 heads on 1 x 128, 64 requests 36 / 30, 128 requests 53 / 44 (of 16 heads 24 / 27, 37 /
+// 46); of 64 on 2 x 128, 64 requests 53 / 44, 128 requests 87 / 81; heads of 64 26 / 25, 35 / 32. The border is
+// one for all, between those and 8 K/V heads, which gain at 32. The cut of few rows is that of
+// history_plan, with chunks of 512 keys in either case: 128 single rows over 3,125 keys, 8 heads x 128: by four heads a workgroup 129 us, two 136,
 // one 207; chunks of 256 to 1,536 keys 128 to 164.
 HistPlan fp4_plan(int64_t R, int64_t N, int H, int Hk, int D, int64_t max_len, bool bf16) {
   const int64_t each = (N * (H / Hk) + R - 1) / R;       // rows a request and K/V head

@@ -18,6 +18,9 @@
 // costs an exponential. Waves and parts share a call as in history_split.
 // 128 single rows over 3,125 keys on average, 8 heads x 128: 125 us, 3.4 TB/s (a cache in
 // bf16: 287 us at 5.7 TB/s); 48 over 18,750, 16 heads on 2, capped: 91; 1 over 4,099: 8.2.
+// With 8 rows of a group two lanes hold the same row and form the same exponentials,
+// and K and V are converted for half a tile; the cap costs nothing to speak of (the grouped call with
+// none 90 us, 20: 88, 50: 96, 200: 95).
 // What bounds it: the loads of a stage and the work on it overlap only over the three
 // waves of a SIMD; without the work the loads take 88 us and 20 more for the scales, the
 // work alone 78. Two stages of registers (150 us), V's loads before K's products (136),

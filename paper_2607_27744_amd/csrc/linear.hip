@@ -627,8 +627,11 @@ void ikbo_gemm_tile(
 // histories of 32,768 rows would take five rounds of the chip for four): a wave takes
 // the adapters of its 128 rows one by one, with t zero for the others' rows. 32,768 rows of
 // 16 requests, 2,048 -> 2,048, rank 64: 245 to 289 us by the card, 980 to 1,160 TFLOP/s of the
-// projection and B, bound as without them (a large bf16 product on that card: 1,140); 24,000 rows of 12,000
-// requests, 512 -> 1,024, rank 16, of 64 adapters, 185 with t: there by the loop over a wave's 64 adapters.
+// projection and B (a large bf16 product on that card: 1,140). What the adapters add to a call (32,768
+// rows, us, all rows / none with an adapter / the linear): 1,024 -> 1,536, rank 32: 119 / 101 / 93; 2,048 ->
+// 2,048, rank 64: 274 / 239 / 228; about half of it is t, the rest the chain at a tile's end: rows' adapters, then
+// B and t, then their products. 24,000 rows of 12,000 requests, 512 -> 1,024, rank 16, of 64
+// adapters, 185 to 197 with t: there by the loop over a wave's 64 adapters.
 //
 // Rows past the tile's end are clamped loads whose results are not stored.
 // ---------------------------------------------------------------------------

@@ -1138,8 +1138,9 @@ def adapter_linear(x, w, a, b, offsets, adapter_ids, *, scales=None, bias=None, 
 
     x [N, K] (rows may be strided), w [D, K], a [adapters, rank, K], b [adapters, D, rank], offsets
     int32 [R + 1], adapter_ids int32 [R] (an id outside [0, adapters): no adapter), scales float32
-    [adapters], bias float32 [D]. Rows past offsets[R] stay as they are in `out`. Adapters of other
-    ranks than the array's are padded with zeros."""
+    [adapters], bias float32 [D]. Rows past offsets[R] stay as they are in `out`. Adapters of a
+    smaller rank than the array's are the caller's to pad with zeros; in bfloat16 pad the rank to a
+    multiple of 8 as well, since others run a general kernel, 27 times slower on large calls."""
     done = (_binding or _native()).adapter(x, w, a, b, offsets, adapter_ids, scales, bias, activation,
                                            out, workspace, stream)
     if done is not None:
